@@ -342,6 +342,61 @@ typedef struct {
 } dp_step_desc;
 dp_status dp_step_enqueue(const dp_step_desc* desc, int32_t phases);
 
+/* ---- layer norm (GPT-2's normalisation; no equation of the paper, its gains and shifts are blocks of Eq. 6) ----
+ * Per row x of X [dev, (rows, p)]: h = (x - mean) / sqrt(var + eps) with the biased variance, y = h*gain + shift.
+ * dt: storage type of X, Y and X_hat; gain, shift [dev, p of param_dt, or NULL: 1 and 0].  Y, X_hat (the normalised input,
+ * what dp_vector_norms reads as X of a gain), mean, rstd [dev, rows floats]: each may be NULL, not all of them.  Y or X_hat
+ * may be X itself (same pitch), not both the same.  Any alignment works; 16-byte aligned tensors with p % 8 == 0 and pitches
+ * that are multiples of 16 bytes take the vector path.  p <= 16384, eps >= 0. */
+dp_status dp_layernorm(const void* X, int64_t ldx, dp_dtype dt, int64_t rows, int32_t p, const void* gain, const void* shift,
+                       dp_dtype param_dt, float eps, void* Y, int64_t ldy, void* X_hat, int64_t ldh, float* mean, float* rstd,
+                       void* stream);
+/* Its backward pass, with the reduction of the parameters' gradients by example.  G [dev, (B*T, p)]: gradient at Y; X, mean, rstd:
+ * input of the forward call and what it returned.  With u = G*gain:
+ *   dX = rstd * (u - mean(u) - h*mean(u*h))                                                      [dev, (B*T, p) of dt, or NULL]
+ *   gain_sums[i,:] = sum_t G[i,t,:]*h[i,t,:],  shift_sums[i,:] = sum_t G[i,t,:]                  [dev, (B, p) floats each, or NULL]
+ *   sq[i] += ||gain_sums[i]||^2 + ||shift_sums[i]||^2   (both parameters' blocks of Eq. 6)         [dev, B floats, or NULL]
+ * The sums are the v_i of dp_clip_accumulate_vectors, so their clipped sum is that call on them with T = 1 (DP_F32): G and X are
+ * read once for dX, norms and sums.  dX may be G or X itself (same pitch).  Workspace: dp_layernorm_backward_ws_bytes (0
+ * unless few examples have long sequences). */
+dp_status dp_layernorm_backward(const void* G, int64_t ldg, const void* X, int64_t ldx, dp_dtype dt, int32_t B, int32_t T, int32_t p,
+                                const void* gain, dp_dtype param_dt, const float* mean, const float* rstd, void* dX, int64_t lddx,
+                                float* gain_sums, float* shift_sums, float* sq, void* ws, size_t ws_bytes, void* stream);
+size_t dp_layernorm_backward_ws_bytes(int32_t B, int32_t T, int32_t p);
+
+/* ---- preference loss of paired sequences on the LM head's logits, with the head's G ----
+ * (For fine-tuning on pairs under DP-SGD: an example is a pair.)  logits [dev, (2*B*T, V)]: pair i owns rows 2*T*i ..
+ * 2*T*i+2*T-1, the preferred sequence's T rows first.  targets [dev, (B, 2, T) int32]: the token each row predicts; negative: the row
+ * does not count (prompt, padding), is not read and gets a zero gradient.  A target >= V is flagged (DP_DEV_BAD_ID) and
+ * does not count either.  ref_logp [dev, (B, 2) floats, or NULL: 0]: the sequences' log-probabilities under the reference model, as
+ * `logp` of this call on that model's logits.  With l the sum of log softmax(logits)[target] over a sequence's rows that count,
+ *   h_i = beta * ((l_c - ref_c) - (l_r - ref_r)),   loss[i] = -(1 - smoothing) log s(h_i) - smoothing log s(-h_i)
+ * (s the logistic function), logp [dev, (B, 2) floats] = l, and G [dev, (2*B*T, V) of dt] = scale * d loss / d logits, the G of an
+ * LM head in dp_ghost_norms and dp_clip_accumulate* with sequences of 2*T tokens.  loss, logp, G: each may be NULL, not all; G may
+ * be logits itself (same pitch).  Columns past V are neither read nor written.  Any alignment of whole elements works; beta >= 0,
+ * 0 <= smoothing <= 1. */
+dp_status dp_preference_loss(const void* logits, int64_t ldl, dp_dtype dt, int32_t B, int32_t T, int32_t V, const int32_t* targets,
+                             const float* ref_logp, float beta, float smoothing, float scale, float* loss, float* logp, void* G,
+                             int64_t ldg, void* ws, size_t ws_bytes, int32_t* dev_status, void* stream);
+size_t dp_preference_loss_ws_bytes(int32_t B, int32_t T);
+
+/* ---- orthogonalised updates from noised sums (Newton-Schulz products, as the Muon optimiser takes them) ----
+ * Post-processing of Eq. 3's output, so it costs no privacy.  For every matrix M [dev, (p, d) of dt, pitch ldm]:
+ *   X = M / (||M||_F + eps);  `steps` times  A = X X^T, X <- a X + (b A + c A A) X  with (a, b, c) = coefs[3*k..]  [host, 3*steps];
+ *   out [dev, (p, d) of out_dt, pitch ldo] = scale * X
+ * (of the transpose where p > d: the same X).  All matrices run together.  Products are taken on fp16 operands of two terms (22 bits) with fp32
+ * accumulation.  out may be M.  coefs whose polynomials exceed 1e6 on the singular values that can occur are DP_ERR_INVALID_ARG.
+ * ws: dp_orthogonalize_ws_bytes (M, out and scale are not looked at), on a 16-byte boundary.  p, d <= 2^20. */
+typedef struct {
+  const void* M;  int64_t ldm;
+  void* out;  int64_t ldo;
+  int32_t p, d;
+  float scale;
+} dp_matrix_desc;
+dp_status dp_orthogonalize(const dp_matrix_desc* mats, int32_t n, dp_dtype dt, dp_dtype out_dt, const float* coefs, int32_t steps,
+                           float eps, void* ws, size_t ws_bytes, int32_t* dev_status, void* stream);
+size_t dp_orthogonalize_ws_bytes(const dp_matrix_desc* mats, int32_t n);
+
 /* ---- privacy accounting on the host (no device work) ----
  * The paper calibrates sigma with a Renyi-DP accountant from the target epsilon (3 in the main
  * experiments), delta = N^-1.1, the sampling rate q = batch / N and the number of steps.  One step

@@ -7,6 +7,7 @@ there is no fallback implementation.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
@@ -35,6 +36,11 @@ class _LinearDesc(C.Structure):
                 ("mode", C.c_int32), ("mode_used", C.c_int32)]
 
 
+class _MatrixDesc(C.Structure):
+    _fields_ = [("M", C.c_void_p), ("ldm", C.c_int64), ("out", C.c_void_p), ("ldo", C.c_int64),
+                ("p", C.c_int32), ("d", C.c_int32), ("scale", C.c_float)]
+
+
 class _VectorDesc(C.Structure):
     _fields_ = [("G", C.c_void_p), ("ldg", C.c_int64), ("X", C.c_void_p), ("ldx", C.c_int64),
                 ("p", C.c_int32)]
@@ -56,7 +62,8 @@ EXPORTS = ["dp_vector_norms", "dp_vector_norms_ws_bytes", "dp_clip_accumulate_ve
            "dp_debug_noise_error_scan", "dp_debug_bounds_checked", "dp_debug_bounds_probe",
            "dp_debug_tensor_map_encodes", "dp_debug_set_wait_limit",
            "dp_debug_ghost_single", "dp_set_reserved_sms", "dp_step_enqueue", "dp_step_ws_bytes",
-           "dp_step_vectors_ws_bytes"]
+           "dp_step_vectors_ws_bytes", "dp_layernorm", "dp_layernorm_backward", "dp_layernorm_backward_ws_bytes",
+           "dp_preference_loss", "dp_preference_loss_ws_bytes", "dp_orthogonalize", "dp_orthogonalize_ws_bytes"]
 
 
 def lib_path() -> str:
@@ -127,6 +134,17 @@ def load():
     L.dp_add_noise_slice.argtypes = [vp, i64, i64, f32, f32, f32, C.c_uint64, C.c_uint32, C.c_uint32, vp]
     L.dp_noise_step_device.argtypes = [vp]
     L.dp_step_enqueue.argtypes = [vp, i32]
+    L.dp_layernorm.argtypes = [vp, i64, i32, i64, i32, vp, vp, i32, f32, vp, i64, vp, i64, vp, vp, vp]
+    L.dp_layernorm_backward.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32, vp, i32, vp, vp, vp, i64, vp, vp, vp,
+                                        vp, sz, vp]
+    L.dp_layernorm_backward_ws_bytes.argtypes = [i32, i32, i32]
+    L.dp_layernorm_backward_ws_bytes.restype = sz
+    L.dp_preference_loss.argtypes = [vp, i64, i32, i32, i32, i32, vp, vp, f32, f32, f32, vp, vp, vp, i64, vp, sz, vp, vp]
+    L.dp_preference_loss_ws_bytes.argtypes = [i32, i32]
+    L.dp_preference_loss_ws_bytes.restype = sz
+    L.dp_orthogonalize.argtypes = [C.POINTER(_MatrixDesc), i32, i32, i32, C.POINTER(f32), i32, f32, vp, sz, vp, vp]
+    L.dp_orthogonalize_ws_bytes.argtypes = [C.POINTER(_MatrixDesc), i32]
+    L.dp_orthogonalize_ws_bytes.restype = sz
     L.dp_rdp_epsilon.argtypes = [C.c_double, C.c_double, i64, C.c_double, vp, vp]
     L.dp_sigma_for_epsilon.argtypes = [C.c_double, i64, C.c_double, C.c_double, C.c_double, vp]
     L.dp_status_string.argtypes = [i32]
@@ -589,6 +607,182 @@ def dp_step_enqueue(layers, outs, tensor_ids, vectors, vector_outs, vector_ids, 
                 raise DpGhostError(1, "marshal", f"outputs, norms and clip factors are float32 tensors, not {t.dtype}")
         raise DpGhostError(1, "marshal", "dp_step_enqueue: arguments of the wrong kind or number")
     _check(st, "dp_step_enqueue")
+
+
+def _complain(what: str):
+    raise DpGhostError(1, "marshal", what)
+
+
+def _on_one_device(tensors) -> None:
+    """Complains unless every tensor is on the current CUDA device, where the launches go."""
+    for t in tensors:
+        if t is not None:
+            _ptr(t)
+            if t.device.index != torch.cuda.current_device():
+                _complain(f"tensor on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _dense(t: Optional[torch.Tensor], shape, dtype, what: str) -> None:
+    """Complains unless t is None or a contiguous tensor of this type with as many elements as `shape` has."""
+    if t is not None and (t.dtype != dtype or not t.is_contiguous() or t.numel() != math.prod(shape)):
+        _complain(f"{what}: a contiguous {dtype} tensor of {tuple(shape)} is wanted, not {t.dtype} {tuple(t.shape)}")
+
+
+def _rows(t: Optional[torch.Tensor], rows: int, p: int, dtype, what: str) -> int:
+    """Pitch of a (..., >= p) tensor of `rows` rows at one distance from each other; 0 of None."""
+    if t is None:
+        return 0
+    if t.dtype != dtype or t.dim() < 2 or t.shape[-1] < p or math.prod(t.shape[:-1]) != rows or t.stride(-1) != 1:
+        _complain(f"{what}: {rows} rows of at least {p} consecutive {dtype} elements are wanted, not {t.dtype} {tuple(t.shape)}")
+    ld, at = None, 1
+    for n, st in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n > 1:
+            if ld is None:
+                ld, at = st, n
+                continue
+            if st != ld * at:
+                _complain(f"{what}: rows must be equally spaced, not of strides {t.stride()}")
+            at *= n
+    ld = t.shape[-1] if ld is None else ld           # a single row
+    if ld < p:
+        _complain(f"{what}: rows overlap (strides {t.stride()})")
+    return ld
+
+
+def _scratch(need: int, ws: Optional[torch.Tensor], device, stream) -> torch.Tensor:
+    """The caller's workspace or a new one, which the allocator keeps until `stream` is through with it."""
+    if ws is None:
+        ws = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+        if stream is not None:
+            ws.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream)))
+    elif not ws.is_contiguous():
+        _complain("the workspace must be contiguous")
+    return ws
+
+
+def _ln_params(tensors, p: int) -> int:
+    """The dp_dtype of a norm's gain and shift."""
+    given = [t for t in tensors if t is not None]
+    _one_dtype(given, "gain and shift")
+    for t in given:
+        _dense(t, (p,), t.dtype, "gain and shift")
+    return _dt(given[0]) if given else DP_F32
+
+
+def dp_layernorm(X, gain, shift, eps: float, Y=None, X_hat=None, mean=None, rstd=None, p=None, stream=None):
+    """Y = X_hat*gain + shift and X_hat = (X - mean)*rstd over the last axis (its first p columns); mean, rstd: floats, one per
+    row.  gain, shift: p elements, float32 or bfloat16, or None."""
+    L = load()
+    p = p if p is not None else X.shape[-1]
+    rows = math.prod(X.shape[:-1])
+    _on_one_device((X, gain, shift, Y, X_hat, mean, rstd))
+    pdt = _ln_params((gain, shift), p)
+    ldx, ldy, ldh = (_rows(t, rows, p, X.dtype, n) for t, n in ((X, "X"), (Y, "Y"), (X_hat, "X_hat")))
+    _dense(mean, (rows,), torch.float32, "mean")
+    _dense(rstd, (rows,), torch.float32, "rstd")
+    st = L.dp_layernorm(_ptr(X), ldx, _dt(X), rows, p, _ptr(gain), _ptr(shift), pdt, float(eps), _ptr(Y), ldy, _ptr(X_hat), ldh,
+                        _ptr(mean), _ptr(rstd), _stream(stream))
+    _check(st, "dp_layernorm")
+
+
+def dp_layernorm_backward_ws_bytes(B: int, T: int, p: int) -> int:
+    return int(load().dp_layernorm_backward_ws_bytes(B, T, p))
+
+
+def dp_layernorm_backward(G, X, gain, mean, rstd, dX=None, gain_sums=None, shift_sums=None, sq=None, p=None, ws=None,
+                          stream=None):
+    """Backward pass of dp_layernorm for G (B,T,>=p): dX, every example's sums for gain and shift (B,p), and
+    sq[i] += their squared norms.  The sums' clipped sum: dp_clip_accumulate_vectors on Vector(gain_sums.view(B, 1, p)), T = 1."""
+    L = load()
+    if G.dim() != 3:
+        _complain("G: (B, T, p) is wanted")
+    B, T = G.shape[:2]
+    p = p if p is not None else G.shape[-1]
+    _on_one_device((G, X, gain, mean, rstd, dX, gain_sums, shift_sums, sq, ws))
+    pdt = _ln_params((gain,), p)
+    ldg, ldx, ldd = (_rows(t, B * T, p, G.dtype, n) for t, n in ((G, "G"), (X, "X"), (dX, "dX")))
+    for t, n in ((mean, "mean"), (rstd, "rstd")):
+        _dense(t, (B * T,), torch.float32, n)
+    for t, n in ((gain_sums, "gain_sums"), (shift_sums, "shift_sums")):
+        _dense(t, (B, p), torch.float32, n)
+    _dense(sq, (B,), torch.float32, "sq")
+    ws = _scratch(int(L.dp_layernorm_backward_ws_bytes(B, T, p)), ws, G.device, stream)
+    st = L.dp_layernorm_backward(_ptr(G), ldg, _ptr(X), ldx, _dt(G), B, T, p, _ptr(gain), pdt, _ptr(mean), _ptr(rstd), _ptr(dX), ldd,
+                                 _ptr(gain_sums), _ptr(shift_sums), _ptr(sq), _ptr(ws), ws.numel() * ws.element_size(),
+                                 _stream(stream))
+    _check(st, "dp_layernorm_backward")
+
+
+def dp_preference_loss_ws_bytes(B: int, T: int) -> int:
+    return int(load().dp_preference_loss_ws_bytes(B, T))
+
+
+def dp_preference_loss(logits, targets, ref_logp, beta: float, loss=None, logp=None, G=None, V=None, smoothing: float = 0.0,
+                       scale: float = 1.0, ws=None, dev_status=None, stream=None):
+    """Loss of B pairs and the gradient at their logits.  logits, G (B, 2T, >=V): a pair's preferred sequence, then the
+    other; targets (B, 2, T) int32, negative: the row does not count; ref_logp (B, 2) or None; loss (B,), logp (B, 2) floats."""
+    L = load()
+    if logits.dim() != 3 or targets.dim() != 3 or targets.shape[1] != 2 or logits.shape[:2] != (targets.shape[0], 2 * targets.shape[2]):
+        _complain(f"logits (B, 2T, V) and targets (B, 2, T) are wanted, not {tuple(logits.shape)} and {tuple(targets.shape)}")
+    B, T = targets.shape[0], targets.shape[2]
+    V = V if V is not None else logits.shape[-1]
+    _on_one_device((logits, targets, ref_logp, loss, logp, G, ws, dev_status))
+    ldl, ldg = _rows(logits, 2 * B * T, V, logits.dtype, "logits"), _rows(G, 2 * B * T, V, logits.dtype, "G")
+    _dense(targets, (B, 2, T), torch.int32, "targets")
+    _dense(ref_logp, (B, 2), torch.float32, "ref_logp")
+    _dense(loss, (B,), torch.float32, "loss")
+    _dense(logp, (B, 2), torch.float32, "logp")
+    _dense(dev_status, (1,), torch.int32, "dev_status")
+    ws = _scratch(int(L.dp_preference_loss_ws_bytes(B, T)), ws, logits.device, stream)
+    st = L.dp_preference_loss(_ptr(logits), ldl, _dt(logits), B, T, V, _ptr(targets), _ptr(ref_logp), float(beta), float(smoothing),
+                              float(scale), _ptr(loss), _ptr(logp), _ptr(G), ldg, _ptr(ws), ws.numel() * ws.element_size(),
+                              _ptr(dev_status), _stream(stream))
+    _check(st, "dp_preference_loss")
+
+
+NEWTON_SCHULZ = ((3.4445, -4.7750, 2.0315),) * 5     # the Muon optimiser's quintic, five times
+
+
+def _mdescs(mats, outs=None, scales=None):
+    arr = (_MatrixDesc * len(mats))()
+    for k, m in enumerate(mats):
+        if m.dim() != 2 or m.stride(1) != 1 and m.shape[1] > 1:
+            _complain(f"matrix {k}: two axes with consecutive columns are wanted, not {tuple(m.shape)} of strides {m.stride()}")
+        D = arr[k]
+        D.p, D.d = m.shape
+        D.M, D.ldm = m.data_ptr(), m.stride(0) if m.shape[0] > 1 else m.shape[1]
+        if outs is not None:
+            o = outs[k]
+            if o.shape != m.shape or o.stride(1) != 1 and o.shape[1] > 1:
+                _complain(f"output {k}: {tuple(m.shape)} with consecutive columns is wanted, not {tuple(o.shape)} of strides {o.stride()}")
+            D.out, D.ldo = o.data_ptr(), o.stride(0) if m.shape[0] > 1 else m.shape[1]
+            D.scale = 1.0 if scales is None else float(scales[k])
+    return arr
+
+
+def dp_orthogonalize_ws_bytes(mats: Sequence[torch.Tensor]) -> int:
+    return int(load().dp_orthogonalize_ws_bytes(_mdescs(mats), len(mats)))
+
+
+def dp_orthogonalize(mats: Sequence[torch.Tensor], outs: Sequence[torch.Tensor], scales: Optional[Sequence[float]] = None,
+                     coefs=NEWTON_SCHULZ, eps: float = 1e-7, ws=None, dev_status=None, stream=None):
+    """outs[k] = scales[k] * (mats[k] orthogonalised by the Newton-Schulz products that coefs, one (a, b, c) per step, names)."""
+    L = load()
+    n = len(mats)
+    if n == 0 or len(outs) != n or (scales is not None and len(scales) != n):
+        _complain("as many outputs and scales as matrices are wanted, one at least")
+    _on_one_device((*mats, *outs, ws, dev_status))
+    _one_dtype(mats, "matrices")
+    _one_dtype(outs, "outputs")
+    _dense(dev_status, (1,), torch.int32, "dev_status")
+    arr = _mdescs(mats, outs, scales)
+    flat = [float(c) for step in coefs for c in step]
+    if len(flat) != 3 * len(coefs):
+        _complain("coefs: (a, b, c) for each step")
+    ws = _scratch(int(L.dp_orthogonalize_ws_bytes(arr, n)), ws, mats[0].device, stream)
+    st = L.dp_orthogonalize(arr, n, _dt(mats[0]), _dt(outs[0]), (C.c_float * len(flat))(*flat), len(coefs), float(eps), _ptr(ws),
+                            ws.numel() * ws.element_size(), _ptr(dev_status), _stream(stream))
+    _check(st, "dp_orthogonalize")
 
 
 def dp_rdp_epsilon(q: float, sigma: float, steps: int, delta: float):

@@ -36,6 +36,8 @@ inline dp_status cuda_fail(cudaError_t e) {
   } while (0)
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+// whether each pointer (nullptr too) lies on a multiple of n bytes, n a power of two
+template <typename... P> inline bool on_boundary(size_t n, P... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) & (n - 1)) == 0; }
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 

@@ -1,0 +1,733 @@
+// Orthogonalised updates: Newton-Schulz products on the noised sums of weight matrices.
+//
+//   X_0 = M / (|M|_F + eps),   A = X X^T,   B = b A + c A A,   X <- a X + B X   (once per step, coefficients per step)
+//
+// turns a matrix into the nearest one with orthonormal rows (columns), as far as the polynomial's steps go; applied to a
+// noised sum it is post-processing, so it costs no privacy.  A matrix with more rows than columns is transposed on the way in
+// and out, so that X is m x n with m <= n and A, B are m x m.
+//
+// Every product runs on the tensor cores in three bf16-rate products of fp16 operands: X, A and B are kept as two planes
+// of fp16, high and low terms (22 bits), scaled by powers of two that the host derives from bounds of the polynomials (|X| <= s
+// in the spectral norm gives |A| <= s^2 and so on), so that nothing overflows and small entries keep their low terms: one
+// bf16 product per product is off by 1e-2 after five steps, two bf16 terms by 2e-5, these by what the sums round.
+// lo hi' and hi lo' of all of K come before hi hi': an MMA rounds its sum towards zero, by as much as the sum is large.
+// A and A A are symmetric: tiles on and below the diagonal are computed, the others written as their transposes.
+//
+// One kernel for all three products and all matrices of a call: persistent, work items are output tiles.  kPair: CTA pairs
+// (cta_group::2) with 256 x 256 tiles; else single CTAs with 128 x 128 tiles, for calls with few tiles.  Roles: two producer
+// warps (TMA, 64-wide K steps of the left and the right operand), the MMA issuer, a relay (pairs: tells rank 0's issuer
+// that rank 1's half of a stage has landed), 16 epilogue warps; two accumulators, so an epilogue overlaps the next tile.
+#include <cuda.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <vector>
+
+#include "dp_common.cuh"
+#include "ptx_sm100.cuh"
+#include "tma_host.cuh"
+
+namespace dpg {
+
+namespace {
+
+constexpr int kBK = 64;
+constexpr int kBoxBytes = 64 * 128;                   // 64 rows x 64 fp16
+constexpr int kPartBytes = 2 * kBoxBytes;             // 128 rows (or columns) of an operand
+constexpr int kStageBytes = 2 * kPartBytes;
+constexpr int kStages = 7;
+constexpr size_t kSmemBytes = size_t(kStages) * kStageBytes + 1024 + 512;
+constexpr int kRelayWarp = 2, kProducerQWarp = 3, kEpiWarp0 = 4, kEpiWarps = 16;
+constexpr int kThreads = (kEpiWarp0 + kEpiWarps) * 32;
+constexpr int kNsMaxMats = 96;                        // matrices per launch (parameter-block limit)
+constexpr int kNormParts = 32;                        // partial sums of a matrix's squares
+
+enum Product { kGram, kPoly, kApply };                // A = X X^T, B = b A + c A A, X' = a X + B X
+
+struct NsMat {
+  const __half* add;         // planes that the epilogue adds (A or X), rows of `ld_add`
+  __half* dst;               // planes written, or nullptr: `out`
+  void* out;
+  long long plane_add, plane_dst, ldo;
+  int ld_add, ld_dst;
+  int M, N, ksteps;
+  int item_begin;
+  int transposed;            // out is X'^T
+  float out_scale;
+};
+
+struct __align__(64) NsParams {
+  CUtensorMap tmP[kNsMaxMats];
+  CUtensorMap tmQ[kNsMaxMats];
+  NsMat mat[kNsMaxMats];
+  int n_mats, total_items;
+  int out_dt;
+  float f_acc, f_add;        // written value = f_acc * product + f_add * (high + low term of `add`)
+  int* dev_status;
+  long long wait_limit;
+};
+static_assert(sizeof(NsParams) <= 32764, "kernel parameter block too large");
+
+struct Item { int mat, tm, tn; };
+
+template <Product kProduct, int kTile>
+__device__ __forceinline__ Item decode_item(const NsParams& P, int item, int& l) {
+  while (l + 1 < P.n_mats && item >= P.mat[l + 1].item_begin) ++l;
+  const NsMat& L = P.mat[l];
+  int local = item - L.item_begin;
+  Item it;
+  it.mat = l;
+  if (kProduct == kApply) {
+    const int tiles_n = (L.N + kTile - 1) / kTile;
+    it.tm = local / tiles_n;
+    it.tn = local - it.tm * tiles_n;
+  } else {                                            // rows of the lower triangle, the diagonal in them
+    it.tm = 0;
+    while (local > it.tm) { local -= it.tm + 1; ++it.tm; }
+    it.tn = local;
+  }
+  return it;
+}
+
+// K steps of a tile: lo hi' of all of K, hi lo', then hi hi'
+struct Walk {
+  int k = 0, term = 0;
+  __device__ __forceinline__ int plane(bool right) const { return term == (right ? 1 : 0) ? 1 : 0; }
+  __device__ __forceinline__ void next(int ksteps) { if (++k == ksteps) { k = 0; ++term; } }
+};
+
+__device__ __forceinline__ void split_fp16(float v, __half& hi, __half& lo) {
+  hi = __float2half_rn(v);
+  lo = __float2half_rn(v - __half2float(hi));
+}
+
+__device__ __forceinline__ void unpack_add(const __half* p, long long plane, float (&v)[8]) {
+  const uint4 h = *reinterpret_cast<const uint4*>(p), l = *reinterpret_cast<const uint4*>(p + plane);
+  const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&hw[e]));
+    const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&lw[e]));
+    v[2 * e] = a.x + b.x;
+    v[2 * e + 1] = a.y + b.y;
+  }
+}
+
+template <Product kProduct, bool kPair>
+__global__ void __launch_bounds__(kThreads, 1)
+ns_product_kernel(const __grid_constant__ NsParams P) {
+  constexpr int kTile = kPair ? 256 : 128;             // output tile; also columns of an accumulator
+  constexpr bool kRightMn = kProduct == kApply;        // the right operand is contiguous along N
+  const uint32_t rank = kPair ? ptx::cluster_ctarank() : 0u;
+  const int first_item = kPair ? int(blockIdx.x >> 1) : int(blockIdx.x);
+  const int item_stride = kPair ? int(gridDim.x >> 1) : int(gridDim.x);
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(tiles + size_t(kStages) * kStageBytes);
+  uint64_t* full = bars;                      // both producers' TMA loads landed
+  uint64_t* ready = bars + kStages;           // pair: in both CTAs (rank 0's copy)
+  uint64_t* empty = bars + 2 * kStages;       // MMAs retired
+  uint64_t* acc_full = bars + 3 * kStages;    // [2]
+  uint64_t* acc_empty = acc_full + 2;         // [2]
+  uint64_t* mma_done = acc_empty + 2;         // only used when the MMA issuer gives up
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(mma_done + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  uint32_t* sink = tmem_slot + 2;             // [kStages] written by st.async, never read
+
+  const int warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
+  const uint32_t tiles_a = ptx::smem_u32(tiles);
+  const uint32_t full_a = ptx::smem_u32(full), ready_a = ptx::smem_u32(ready), empty_a = ptx::smem_u32(empty);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      ptx::mbar_init(&full[s], 2);
+      ptx::mbar_init(&ready[s], 1);           // rank 0's relay arrives and announces 4 bytes, rank 1's sends them
+      ptx::mbar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      ptx::mbar_init(&acc_full[b], 1);
+      ptx::mbar_init(&acc_empty[b], kEpiWarps);    // pair: + 4 bytes from each of rank 1's
+    }
+    ptx::mbar_init(mma_done, 1);
+    *abort_flag = 0;
+    ptx::fence_mbar_init();
+  }
+  if (warp == 1) {
+    if (kPair) { ptx::tmem_alloc_pair(tmem_slot, 2 * kTile); ptx::tmem_relinquish_pair(); }
+    else { ptx::tmem_alloc(tmem_slot, 2 * kTile); ptx::tmem_relinquish(); }
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (kPair) ptx::cluster_sync_all();         // the partner's barriers exist before anyone arrives on them
+  ptx::tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+
+  if (warp == 0 || warp == kProducerQWarp) {
+    // ------------------------------------------------------------- TMA producers
+    // producers, issuer and relay: the whole warp runs the loop, an elected lane issues (see ptx::warp_ok)
+    const bool right = warp != 0;
+    uint32_t stage = 0, phase = 0, issued = 0;
+    int lay = 0;
+    bool ok = true;
+    for (int item = first_item; item < P.total_items && ok; item += item_stride) {
+      const Item it = decode_item<kProduct, kTile>(P, item, lay);
+      const uint64_t tm = reinterpret_cast<uint64_t>(right ? &P.tmQ[it.mat] : &P.tmP[it.mat]);
+      const int ksteps = P.mat[it.mat].ksteps;
+      // first of this CTA's 128 rows (columns) of the operand
+      const int r0 = (right ? it.tn : it.tm) * kTile + int(rank) * 128;
+      Walk at;
+      for (int j = 0; j < 3 * ksteps; ++j) {
+        ok = ptx::warp_ok(ptx::mbar_wait_a(empty_a + 8 * stage, phase ^ 1, abort_flag, P.wait_limit));
+        if (!ok) break;
+        const uint32_t bar = full_a + 8 * stage;
+        const uint32_t dst = tiles_a + stage * kStageBytes + (right ? kPartBytes : 0);
+        if (ptx::elect_one()) {
+          ptx::mbar_arrive_expect_tx_a(bar, uint32_t(kPartBytes));
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            if (kRightMn && right) ptx::tma_load_3d_a(dst + b * kBoxBytes, tm, bar, r0 + b * 64, at.k * kBK, at.plane(right));
+            else ptx::tma_load_3d_a(dst + b * kBoxBytes, tm, bar, at.k * kBK, r0 + b * 64, at.plane(right));
+          }
+        }
+        __syncwarp();
+        ++issued;
+        at.next(ksteps);
+        if (++stage == kStages) { stage = 0; phase ^= 1; }
+      }
+    }
+    if (!ok && ptx::elect_one()) {
+      *abort_flag = 1;
+      if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
+      ptx::drain_issued_copies(full, kStages, issued);
+    }
+  } else if (warp == 1) {
+    // --------------------------------------------------------------- MMA issuer
+    if (rank == 0) {
+      // fp16 operands: format 0 in place of bf16's 1 in bits 7 and 10
+      constexpr uint32_t idesc = ptx::idesc_bf16_f32(kTile, kTile, 0, kRightMn ? 1 : 0) & ~((1u << 7) | (1u << 10));
+      // K-major: groups of 8 rows 1 KiB apart, 16 columns further 32 bytes; MN-major: 64-column boxes apart, 16 rows 2 KiB
+      constexpr uint64_t dk = ptx::smem_desc_base(16, 1024, ptx::SWIZZLE_128B);
+      constexpr uint64_t dmn = ptx::smem_desc_base(kBoxBytes, 1024, ptx::SWIZZLE_128B);
+      constexpr uint32_t desc_hi = uint32_t(dk >> 32);
+      static_assert(desc_hi == uint32_t(dmn >> 32), "descriptors differ in the low word only");
+      const uint32_t base = (tiles_a >> 4) & 0x3FFF;
+      const uint32_t lo_p0 = uint32_t(dk) | base;
+      const uint32_t lo_q0 = (kRightMn ? uint32_t(dmn) : uint32_t(dk)) | (base + (kPartBytes >> 4));
+      const uint32_t go_a = kPair ? ready_a : full_a;
+      uint32_t stage = 0, phase = 0, n_item = 0;
+      int lay = 0;
+      bool ok = true;
+      for (int item = first_item; item < P.total_items && ok; item += item_stride, ++n_item) {
+        const Item it = decode_item<kProduct, kTile>(P, item, lay);
+        const uint32_t buf = n_item & 1, acc_phase = (n_item >> 1) & 1;
+        ok = ptx::warp_ok(kPair ? ptx::mbar_wait_cluster(&acc_empty[buf], acc_phase ^ 1, abort_flag, P.wait_limit)
+                                : ptx::mbar_wait(&acc_empty[buf], acc_phase ^ 1, abort_flag, P.wait_limit));
+        if (!ok) break;
+        ptx::tc_fence_after();
+        const uint32_t d_tmem = tmem_base + buf * kTile;
+        const int steps = 3 * P.mat[it.mat].ksteps;
+        for (int j = 0; j < steps; ++j) {
+          ok = ptx::warp_ok(kPair ? ptx::mbar_wait_cluster_a(go_a + 8 * stage, phase, abort_flag, P.wait_limit)
+                                  : ptx::mbar_wait_a(go_a + 8 * stage, phase, abort_flag, P.wait_limit));
+          if (!ok) break;
+          ptx::tc_fence_after();
+          const uint32_t lo_p = lo_p0 + stage * (kStageBytes >> 4), lo_q = lo_q0 + stage * (kStageBytes >> 4);
+          if (ptx::elect_one()) {
+#pragma unroll
+            for (int kk = 0; kk < kBK / 16; ++kk) {
+              const uint32_t p = lo_p + kk * 2, q = lo_q + kk * (kRightMn ? 128 : 2), more = (j > 0 || kk > 0) ? 1u : 0u;
+              if (kPair) ptx::mma_bf16_ss_pair_lh(d_tmem, p, q, desc_hi, idesc, more);
+              else ptx::mma_bf16_ss_lh(d_tmem, p, q, desc_hi, idesc, more);
+            }
+            if (kPair) ptx::mma_commit_pair_a(empty_a + 8 * stage, 3);     // stage reusable once these MMAs retire
+            else ptx::mma_commit_a(empty_a + 8 * stage);
+            if (j + 1 == steps) {
+              if (kPair) ptx::mma_commit_pair(&acc_full[buf], 3);
+              else ptx::mma_commit(&acc_full[buf]);
+            }
+          }
+          __syncwarp();
+          if (++stage == kStages) { stage = 0; phase ^= 1; }
+        }
+      }
+      if (!ok && ptx::elect_one()) {
+        *abort_flag = 1;
+        if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
+        ptx::drain_issued_mmas(mma_done, kPair);
+      }
+    }
+  } else if (warp == kRelayWarp) {
+    // -------------------------------------------------------------------- relay
+    // Rank 0's relay arrives on its own `ready` barrier and announces 4 more bytes; rank 1's, which has acquired its `full`
+    // barrier, delivers them with an asynchronous store whose completion is a release at cluster scope.
+    if (kPair) {
+      const uint32_t ready_remote = ptx::mapa_u32(ready_a, 0), sink_remote = ptx::mapa_u32(ptx::smem_u32(sink), 0);
+      uint32_t stage = 0, phase = 0;
+      int lay = 0;
+      bool ok = true;
+      for (int item = first_item; item < P.total_items && ok; item += item_stride) {
+        const Item it = decode_item<kProduct, kTile>(P, item, lay);
+        for (int j = 3 * P.mat[it.mat].ksteps; j > 0; --j) {
+          ok = ptx::warp_ok(ptx::mbar_wait_a(full_a + 8 * stage, phase, abort_flag, P.wait_limit));
+          if (!ok) break;
+          if (ptx::elect_one()) {
+            if (rank == 0) ptx::mbar_arrive_expect_tx_a(ready_a + 8 * stage, 4);
+            else ptx::st_async_signal_a(ready_remote + 8 * stage, sink_remote + 4 * stage);
+          }
+          __syncwarp();
+          if (++stage == kStages) { stage = 0; phase ^= 1; }
+        }
+      }
+      if (!ok && ptx::elect_one()) {
+        *abort_flag = 1;
+        if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
+      }
+    }
+  } else {
+    // ----------------------------------------------------------------- epilogue
+    const int q = warp & 3;                          // TMEM lane quarter this warp may read
+    const int ew = warp - kEpiWarp0;
+    constexpr int kCols = kTile / (kEpiWarps / 4);   // columns of a warp
+    const uint32_t acc_empty_a = ptx::smem_u32(acc_empty);
+    const uint32_t acc_empty_remote = kPair ? ptx::mapa_u32(acc_empty_a, 0) : 0u;
+    const uint32_t sink_remote = kPair ? ptx::mapa_u32(ptx::smem_u32(sink), 0) : 0u;
+    auto free_acc = [&](uint32_t buf) {              // see gemm_gta_tc.cu
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (!kPair) ptx::mbar_arrive(&acc_empty[buf]);
+        else if (rank == 0) ptx::mbar_arrive_expect_tx_a(acc_empty_a + 8 * buf, 4);
+        else ptx::st_async_signal_a(acc_empty_remote + 8 * buf, sink_remote);
+      }
+    };
+    uint32_t n_item = 0;
+    int lay = 0;
+    bool ok = true;
+    for (int item = first_item; item < P.total_items && ok; item += item_stride, ++n_item) {
+      const Item it = decode_item<kProduct, kTile>(P, item, lay);
+      const NsMat& L = P.mat[it.mat];
+      const uint32_t buf = n_item & 1, acc_phase = (n_item >> 1) & 1;
+      if (!ptx::mbar_wait_relaxed(&acc_full[buf], acc_phase, abort_flag, P.wait_limit)) { ok = false; break; }
+      ptx::tc_fence_after();
+      const uint32_t t0 = tmem_base + (uint32_t(q * 32) << 16) + buf * kTile + (ew >> 2) * kCols;
+      const int row = it.tm * kTile + int(rank) * 128 + q * 32 + lane;
+      const bool mirror = kProduct != kApply && it.tm != it.tn;
+      const float f_acc = P.f_acc * L.out_scale, f_add = P.f_add * L.out_scale;
+#pragma unroll 1
+      for (int c = 0; c < kCols; c += 32) {
+        uint32_t r[32];
+        ptx::tmem_ld_32x32b_x32(t0 + c, r);
+        ptx::tmem_ld_wait();
+        if (c + 32 == kCols) free_acc(buf);
+        const int col0 = it.tn * kTile + (ew >> 2) * kCols + c;
+        if (row < L.M) {
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int col = col0 + 8 * g, left = L.N - col;
+            if (left <= 0) break;
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = f_acc * __uint_as_float(r[8 * g + e]);
+            if (kProduct != kGram) {
+              float a[8];
+              unpack_add(L.add + size_t(row) * L.ld_add + col, L.plane_add, a);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[e] = fmaf(f_add, a[e], v[e]);
+            }
+            if (kProduct != kApply || L.dst) {
+              // rows are padded to whole chunks of eight, which nobody reads
+              __half hi[8], lo[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) split_fp16(v[e], hi[e], lo[e]);
+              __half* d = L.dst + size_t(row) * L.ld_dst + col;
+              uint4 w;
+              memcpy(&w, hi, 16);
+              *reinterpret_cast<uint4*>(d) = w;
+              memcpy(&w, lo, 16);
+              *reinterpret_cast<uint4*>(d + L.plane_dst) = w;
+              if (mirror) {
+                __half* t = L.dst + size_t(col) * L.ld_dst + row;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                  if (e < left) { t[size_t(e) * L.ld_dst] = hi[e]; t[size_t(e) * L.ld_dst + L.plane_dst] = lo[e]; }
+              }
+            } else if (P.out_dt == DP_F32) {
+              float* o = static_cast<float*>(L.out);
+              if (L.transposed) {
+                o += size_t(col) * L.ldo + row;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) if (e < left) o[e * L.ldo] = v[e];
+              } else {
+                o += size_t(row) * L.ldo + col;
+                if (left >= 8 && (reinterpret_cast<uintptr_t>(o) & 31) == 0) ptx::st_global_v8(o, v);
+                else {
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) if (e < left) o[e] = v[e];
+                }
+              }
+            } else {
+              __nv_bfloat16* o = static_cast<__nv_bfloat16*>(L.out);
+              if (L.transposed) {
+                o += size_t(col) * L.ldo + row;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) if (e < left) o[e * L.ldo] = __float2bfloat16_rn(v[e]);
+              } else {
+                o += size_t(row) * L.ldo + col;
+                if (left >= 8 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+                  __nv_bfloat162 h[4];
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) h[e] = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+                  uint4 w;
+                  memcpy(&w, h, 16);
+                  *reinterpret_cast<uint4*>(o) = w;
+                } else {
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) if (e < left) o[e] = __float2bfloat16_rn(v[e]);
+                }
+              }
+            }
+          }
+        }
+        __syncwarp();                                        // the TMEM load is a warp operation
+      }
+    }
+    if (!ok && lane == 0) {
+      *abort_flag = 1;
+      if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
+    }
+  }
+
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (kPair) ptx::cluster_sync_all();         // neither CTA leaves while the partner may still use its memory
+  if (warp == 1) {
+    ptx::tc_fence_after();
+    if (kPair) ptx::tmem_dealloc_pair(tmem_base, 2 * kTile);
+    else ptx::tmem_dealloc(tmem_base, 2 * kTile);
+  }
+}
+
+// ---- the way in: norms, scaled and split matrices ------------------------------------------------
+
+struct NsIn {
+  const void* M;
+  long long ldm, plane;
+  __half* X;                 // planes of the m x n matrix
+  int p, d, ldx;
+  int transposed;
+  int block_begin;
+};
+struct NsInParams {
+  NsIn mat[kNsMaxMats];
+  int n_mats, dt;
+  double* partials;          // [matrix][kNormParts]
+  double eps;
+  float scale;
+};
+
+__device__ __forceinline__ float ns_load(const NsIn& L, int dt, int r, int c) {
+  const size_t at = size_t(r) * size_t(L.ldm) + c;
+  return dt == DP_F32 ? static_cast<const float*>(L.M)[at] : __bfloat162float(static_cast<const __nv_bfloat16*>(L.M)[at]);
+}
+
+// squares of a matrix, kNormParts blocks each; in 64 bits, whose range holds the square of every fp32 number
+__global__ void __launch_bounds__(256)
+ns_norm_kernel(const __grid_constant__ NsInParams P) {
+  __shared__ double red[8];
+  const int l = blockIdx.x / kNormParts, part = blockIdx.x % kNormParts;
+  const NsIn& L = P.mat[l];
+  double s = 0.0;
+  for (int r = part; r < L.p; r += kNormParts)
+    for (int c = threadIdx.x; c < L.d; c += 256) {
+      const double v = double(ns_load(L, P.dt, r, c));
+      s = fma(v, v, s);
+    }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double all = 0.0;
+    for (int w = 0; w < 8; ++w) all += red[w];
+    P.partials[l * kNormParts + part] = all;
+  }
+}
+
+// 64 x 64 blocks of M / (|M| + eps), scaled and split, transposed where M has more rows than columns
+__global__ void __launch_bounds__(256)
+ns_split_kernel(const __grid_constant__ NsInParams P) {
+  __shared__ float tile[64][65];
+  __shared__ double factor;
+  int lo = 0, hi = P.n_mats - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (int(blockIdx.x) >= P.mat[mid].block_begin) lo = mid; else hi = mid - 1;
+  }
+  const NsIn& L = P.mat[lo];
+  if (threadIdx.x < 32) {
+    double s = P.partials[lo * kNormParts + threadIdx.x];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (threadIdx.x == 0) factor = double(P.scale) / (sqrt(s) + P.eps);
+  }
+  const int local = blockIdx.x - L.block_begin, tiles_c = (L.d + 63) / 64;
+  const int r0 = local / tiles_c * 64, c0 = local % tiles_c * 64;
+  const int x = threadIdx.x & 63, y0 = threadIdx.x >> 6;
+#pragma unroll 4
+  for (int y = y0; y < 64; y += 4)
+    tile[y][x] = r0 + y < L.p && c0 + x < L.d ? ns_load(L, P.dt, r0 + y, c0 + x) : 0.f;
+  __syncthreads();
+#pragma unroll 4
+  for (int y = y0; y < 64; y += 4) {
+    const int r = (L.transposed ? c0 : r0) + y, c = (L.transposed ? r0 : c0) + x;
+    if (r < (L.transposed ? L.d : L.p) && c < (L.transposed ? L.p : L.d)) {
+      __half h, l;
+      split_fp16(float(double(L.transposed ? tile[x][y] : tile[y][x]) * factor), h, l);
+      __half* to = L.X + size_t(r) * L.ldx + c;
+      to[0] = h;
+      to[L.plane] = l;
+    }
+  }
+}
+
+// ---- host ----------------------------------------------------------------------------------------
+
+struct NsShape {
+  int m, n, ldx, lda;
+  bool transposed;
+  size_t x_bytes, a_bytes;             // of both planes
+  explicit NsShape(const dp_matrix_desc& D) {
+    transposed = D.p > D.d;
+    m = std::min(D.p, D.d);
+    n = std::max(D.p, D.d);
+    ldx = (n + 7) / 8 * 8;
+    lda = (m + 7) / 8 * 8;
+    x_bytes = align_up(2 * size_t(m) * ldx * sizeof(__half), 256);
+    a_bytes = align_up(2 * size_t(m) * lda * sizeof(__half), 256);
+  }
+  size_t bytes() const { return 2 * x_bytes + 2 * a_bytes; }
+};
+
+// The power of two that brings values of at most `bound` below half of fp16's largest.
+float scale_for(double bound) {
+  int e = 0;
+  frexp(std::max(bound, 1e-6), &e);                  // bound < 2^e
+  return float(ldexp(1.0, 15 - e));
+}
+
+// Bounds of a step on a matrix whose singular values are at most s: of |b l + c l^2| for l <= s^2, of |a x + b x^3 + c x^5|.
+void step_bounds(double a, double b, double c, double s, double* poly, double* next) {
+  auto f = [&](double l) { return std::fabs(b * l + c * l * l); };
+  auto g = [&](double x) { return std::fabs(x * (a + x * x * (b + x * x * c))); };
+  *poly = f(s * s);
+  *next = g(s);
+  if (c != 0.0) {
+    const double l = -b / (2 * c);
+    if (l > 0 && l < s * s) *poly = std::max(*poly, f(l));
+    const double disc = 9 * b * b - 20 * a * c;      // a + 3 b y + 5 c y^2 = 0, y = x^2
+    if (disc >= 0)
+      for (int sign = -1; sign <= 1; sign += 2) {
+        const double y = (-3 * b + sign * std::sqrt(disc)) / (10 * c);
+        if (y > 0 && y < s * s) *next = std::max(*next, g(std::sqrt(y)));
+      }
+  } else if (b != 0.0) {
+    const double y = -a / (3 * b);
+    if (y > 0 && y < s * s) *next = std::max(*next, g(std::sqrt(y)));
+  }
+}
+
+struct NsStep { float a, b, c, x, A, B, next; };     // coefficients; scales of X, A, B and the new X
+
+constexpr double kMargin = 1.01;                     // on a bound, for what the products round
+constexpr double kMaxBound = 1e6;
+
+bool plan_steps(const float* coefs, int steps, std::vector<NsStep>& plan) {
+  double s = 1.0;
+  for (int k = 0; k < steps; ++k) {
+    const double a = coefs[3 * k], b = coefs[3 * k + 1], c = coefs[3 * k + 2];
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+    double poly = 0, next = 0;
+    step_bounds(a, b, c, s, &poly, &next);
+    if (!(poly <= kMaxBound) || !(next <= kMaxBound)) return false;
+    NsStep st{float(a), float(b), float(c), scale_for(s * kMargin), scale_for(s * s * kMargin), scale_for(poly * kMargin), 0.f};
+    s = next * kMargin;
+    st.next = scale_for(s);
+    plan.push_back(st);
+  }
+  return true;
+}
+
+template <Product kProduct, bool kPair>
+dp_status ns_launch(const NsParams& P, cudaStream_t st) {
+  auto* kernel = ns_product_kernel<kProduct, kPair>;
+  if (first_use_on_this_device((const void*)kernel)) DP_CUDA_OK(allow_shared(kernel, kSmemBytes));
+  const int units = kPair ? sm_count() / 2 : sm_count();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((kPair ? 2 : 1) * std::min(P.total_items, units));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmemBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim = {kPair ? 2u : 1u, 1u, 1u};
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  DP_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, P));
+  ++g_kernel_launches;
+  return DP_OK;
+}
+
+int tiles_of(Product product, int m, int n, int tile) {
+  const int tm = ceil_div(m, tile);
+  return product == kApply ? tm * ceil_div(n, tile) : tm * (tm + 1) / 2;
+}
+
+// One product of all matrices of a group.
+dp_status ns_product(Product product, NsParams& P, bool pair, cudaStream_t st) {
+  if (pair) {
+    return product == kGram ? ns_launch<kGram, true>(P, st) : product == kPoly ? ns_launch<kPoly, true>(P, st)
+                                                                                : ns_launch<kApply, true>(P, st);
+  }
+  return product == kGram ? ns_launch<kGram, false>(P, st) : product == kPoly ? ns_launch<kPoly, false>(P, st)
+                                                                               : ns_launch<kApply, false>(P, st);
+}
+
+dp_status ns_group(const dp_matrix_desc* mats, int n, dp_dtype dt, dp_dtype out_dt, const std::vector<NsStep>& plan, float eps,
+                   double* partials, char* base, int* dev_status, cudaStream_t st) {
+  struct Place { NsShape s; __half *x[2], *A, *B; };
+  std::vector<Place> at;
+  at.reserve(n);
+  NsInParams In;
+  memset(&In, 0, sizeof(In));
+  int blocks = 0;
+  for (int k = 0; k < n; ++k) {
+    Place p{NsShape(mats[k]), {nullptr, nullptr}, nullptr, nullptr};
+    p.x[0] = reinterpret_cast<__half*>(base); base += p.s.x_bytes;
+    p.x[1] = reinterpret_cast<__half*>(base); base += p.s.x_bytes;
+    p.A = reinterpret_cast<__half*>(base); base += p.s.a_bytes;
+    p.B = reinterpret_cast<__half*>(base); base += p.s.a_bytes;
+    at.push_back(p);
+    In.mat[k] = {mats[k].M, mats[k].ldm, (long long)p.s.m * p.s.ldx, p.x[0], mats[k].p, mats[k].d, p.s.ldx, p.s.transposed, blocks};
+    blocks += ceil_div(mats[k].p, 64) * ceil_div(mats[k].d, 64);
+  }
+  In.n_mats = n; In.dt = dt; In.partials = partials; In.eps = eps; In.scale = plan[0].x;
+  ns_norm_kernel<<<n * kNormParts, 256, 0, st>>>(In);
+  DP_LAUNCH_OK();
+  ns_split_kernel<<<blocks, 256, 0, st>>>(In);
+  DP_LAUNCH_OK();
+
+  const int steps = int(plan.size());
+  for (int k = 0; k < steps; ++k) {
+    const NsStep& S = plan[k];
+    const bool last = k + 1 == steps;
+    for (int q = 0; q < 3; ++q) {
+      const Product product = Product(q);
+      int big = 0;
+      for (int i = 0; i < n; ++i) big += tiles_of(product, at[i].s.m, at[i].s.n, 256);
+      const bool pair = big >= sm_count() / 2;         // a tile for every CTA pair
+      NsParams P;
+      memset(&P, 0, sizeof(P));
+      int items = 0;
+      for (int i = 0; i < n; ++i) {
+        const Place& p = at[i];
+        const int m = p.s.m, nn = p.s.n;
+        const long long px = (long long)m * p.s.ldx, pa = (long long)m * p.s.lda;
+        NsMat& L = P.mat[i];
+        dp_status r;
+        L.M = m;
+        L.out_scale = 1.f;
+        L.item_begin = items;
+        items += tiles_of(product, m, nn, pair ? 256 : 128);
+        if (product == kGram) {
+          L.N = m; L.ksteps = ceil_div(nn, kBK);
+          L.dst = p.A; L.plane_dst = pa; L.ld_dst = p.s.lda;
+          r = make_tmap_bf16_3d(&P.tmP[i], p.x[k & 1], p.s.ldx, nn, m, 2, 64, 64);
+          if (r == DP_OK) P.tmQ[i] = P.tmP[i];
+        } else if (product == kPoly) {
+          L.N = m; L.ksteps = ceil_div(m, kBK);
+          L.add = p.A; L.plane_add = pa; L.ld_add = p.s.lda;
+          L.dst = p.B; L.plane_dst = pa; L.ld_dst = p.s.lda;
+          r = make_tmap_bf16_3d(&P.tmP[i], p.A, p.s.lda, m, m, 2, 64, 64);
+          if (r == DP_OK) P.tmQ[i] = P.tmP[i];
+        } else {
+          L.N = nn; L.ksteps = ceil_div(m, kBK);
+          L.add = p.x[k & 1]; L.plane_add = px; L.ld_add = p.s.ldx;
+          if (last) { L.out = mats[i].out; L.ldo = mats[i].ldo; L.transposed = p.s.transposed; L.out_scale = mats[i].scale; }
+          else { L.dst = p.x[(k + 1) & 1]; L.plane_dst = px; L.ld_dst = p.s.ldx; }
+          r = make_tmap_bf16_3d(&P.tmP[i], p.B, p.s.lda, m, m, 2, 64, 64);
+          if (r == DP_OK) r = make_tmap_bf16_3d(&P.tmQ[i], p.x[k & 1], p.s.ldx, nn, m, 2, 64, 64);
+        }
+        if (r != DP_OK) return r;
+      }
+      P.n_mats = n; P.total_items = items; P.out_dt = out_dt; P.dev_status = dev_status; P.wait_limit = g_wait_limit;
+      if (product == kGram) { P.f_acc = S.A / (S.x * S.x); P.f_add = 0.f; }
+      else if (product == kPoly) { P.f_acc = S.c * S.B / (S.A * S.A); P.f_add = S.b * S.B / S.A; }
+      else {
+        const float to = last ? 1.f : S.next;
+        P.f_acc = to / (S.B * S.x);
+        P.f_add = S.a * to / S.x;
+      }
+      const dp_status r = ns_product(product, P, pair, st);
+      if (r != DP_OK) return r;
+    }
+  }
+  return DP_OK;
+}
+
+size_t ns_partial_bytes(int n) { return size_t(std::min(n, kNsMaxMats)) * kNormParts * sizeof(double); }
+
+dp_status check_matrix(const dp_matrix_desc& D, bool pointers) {
+  if (D.p <= 0 || D.d <= 0) return DP_ERR_INVALID_ARG;
+  if (D.p > (1 << 20) || D.d > (1 << 20)) return DP_ERR_UNSUPPORTED;
+  if (pointers && (!D.M || !D.out || D.ldm < D.d || D.ldo < D.d || !std::isfinite(D.scale))) return DP_ERR_INVALID_ARG;
+  return DP_OK;
+}
+
+}  // namespace
+
+}  // namespace dpg
+
+using namespace dpg;
+
+extern "C" {
+
+size_t dp_orthogonalize_ws_bytes(const dp_matrix_desc* mats, int32_t n) {
+  if (!mats || n <= 0) return 0;
+  size_t most = 0;
+  for (int g = 0; g < n; g += kNsMaxMats) {          // groups run one after the other in the same memory
+    size_t need = 0;
+    for (int k = g; k < std::min(n, g + kNsMaxMats); ++k) {
+      if (check_matrix(mats[k], false) != DP_OK) return 0;
+      need += NsShape(mats[k]).bytes();
+    }
+    most = std::max(most, need);
+  }
+  return ns_partial_bytes(n) + most;
+}
+
+dp_status dp_orthogonalize(const dp_matrix_desc* mats, int32_t n, dp_dtype dt, dp_dtype out_dt, const float* coefs, int32_t steps,
+                           float eps, void* ws, size_t ws_bytes, int32_t* dev_status, void* stream) {
+  if (!mats || n <= 0 || !coefs || steps <= 0 || !std::isfinite(eps) || eps < 0.f) return DP_ERR_INVALID_ARG;
+  if ((dt != DP_F32 && dt != DP_BF16) || (out_dt != DP_F32 && out_dt != DP_BF16)) return DP_ERR_INVALID_ARG;
+  for (int k = 0; k < n; ++k) {
+    const dp_status r = check_matrix(mats[k], true);
+    if (r != DP_OK) return r;
+    if (!on_boundary(dt == DP_F32 ? 4 : 2, mats[k].M) || !on_boundary(out_dt == DP_F32 ? 4 : 2, mats[k].out)) return DP_ERR_ALIGNMENT;
+  }
+  std::vector<NsStep> plan;
+  if (!plan_steps(coefs, steps, plan)) return DP_ERR_INVALID_ARG;
+  if (!ws || ws_bytes < dp_orthogonalize_ws_bytes(mats, n)) return DP_ERR_WORKSPACE;
+  if (!aligned16(ws)) return DP_ERR_ALIGNMENT;
+  char* base = static_cast<char*>(ws) + ns_partial_bytes(n);
+  for (int g = 0; g < n; g += kNsMaxMats) {
+    const dp_status r = ns_group(mats + g, std::min(n - g, kNsMaxMats), dt, out_dt, plan, eps, static_cast<double*>(ws), base, dev_status,
+                                 (cudaStream_t)stream);
+    if (r != DP_OK) return r;
+  }
+  return DP_OK;
+}
+
+}  // extern "C"
