@@ -10,13 +10,18 @@
 // of fp16, high and low terms (22 bits), scaled by powers of two that the host derives from bounds of the polynomials (|X| <= s
 // in the spectral norm gives |A| <= s^2 and so on), so that nothing overflows and small entries keep their low terms: one
 // bf16 product per product is off by 1e-2 after five steps, two bf16 terms by 2e-5, these by what the sums round.
-// lo hi' and hi lo' of all of K come before hi hi': an MMA rounds its sum towards zero, by as much as the sum is large.
-// A and A A are symmetric: tiles on and below the diagonal are computed, the others written as their transposes.
+// An MMA rounds its sum towards zero, by as much as the sum is large.  So lo hi' and hi lo' of all of K come before hi hi', and
+// hi hi' is summed in chunks of 256 of K, each in an accumulator of its own, that the epilogue adds up in registers to nearest:
+// error of DistilGPT2's updates against 64 bits 2.2e-5 with one accumulator per tile (the diagonal of A, a sum of squares,
+// came out 6e-6 too small at K = 3072).
+// A and A A are symmetric: tiles on and below the diagonal are computed and stored, and a product that needs one above it reads the
+// stored one with rows and columns exchanged (the tensor core takes either order).
 //
 // One kernel for all three products and all matrices of a call: persistent, work items are output tiles.  kPair: CTA pairs
 // (cta_group::2) with 256 x 256 tiles; else single CTAs with 128 x 128 tiles, for calls with few tiles.  Roles: two producer
 // warps (TMA, 64-wide K steps of the left and the right operand), the MMA issuer, a relay (pairs: tells rank 0's issuer
-// that rank 1's half of a stage has landed), 16 epilogue warps; two accumulators, so an epilogue overlaps the next tile.
+// that rank 1's half of a stage has landed), 16 epilogue warps; two accumulators, so adding up a chunk and the epilogue of a
+// tile overlap the next ones.
 #include <cuda.h>
 #include <cuda_fp16.h>
 
@@ -41,6 +46,7 @@ constexpr int kStages = 7;
 constexpr size_t kSmemBytes = size_t(kStages) * kStageBytes + 1024 + 512;
 constexpr int kRelayWarp = 2, kProducerQWarp = 3, kEpiWarp0 = 4, kEpiWarps = 16;
 constexpr int kThreads = (kEpiWarp0 + kEpiWarps) * 32;
+constexpr int kChunk = 4;                             // K steps of hi hi' per accumulator
 constexpr int kNsMaxMats = 96;                        // matrices per launch (parameter-block limit)
 constexpr int kNormParts = 32;                        // partial sums of a matrix's squares
 
@@ -79,10 +85,10 @@ __device__ __forceinline__ Item decode_item(const NsParams& P, int item, int& l)
   int local = item - L.item_begin;
   Item it;
   it.mat = l;
-  if (kProduct == kApply) {
-    const int tiles_n = (L.N + kTile - 1) / kTile;
-    it.tm = local / tiles_n;
-    it.tn = local - it.tm * tiles_n;
+  if (kProduct == kApply) {                           // tiles of the same columns of X, which B's rows all meet, together
+    const int tiles_m = (L.M + kTile - 1) / kTile;
+    it.tn = local / tiles_m;
+    it.tm = local - it.tn * tiles_m;
   } else {                                            // rows of the lower triangle, the diagonal in them
     it.tm = 0;
     while (local > it.tm) { local -= it.tm + 1; ++it.tm; }
@@ -97,6 +103,17 @@ struct Walk {
   __device__ __forceinline__ int plane(bool right) const { return term == (right ? 1 : 0) ? 1 : 0; }
   __device__ __forceinline__ void next(int ksteps) { if (++k == ksteps) { k = 0; ++term; } }
 };
+
+// Whether a K step of a symmetric operand's row tile `t` lies above the diagonal's tiles: there the stored tile is the transpose,
+// contiguous along the rows that are wanted.
+template <Product kProduct, int kTile>
+__device__ __forceinline__ bool exchanged(bool right, int t, int k) {
+  if (kProduct == kApply && right) return true;       // X: K rows, contiguous along N
+  return kProduct != kGram && k * kBK / kTile > t;
+}
+
+// accumulators that a tile's sum is spread over
+__device__ __forceinline__ int chunks_of(int ksteps) { return (ksteps + kChunk - 1) / kChunk; }
 
 __device__ __forceinline__ void split_fp16(float v, __half& hi, __half& lo) {
   hi = __float2half_rn(v);
@@ -115,11 +132,49 @@ __device__ __forceinline__ void unpack_add(const __half* p, long long plane, flo
   }
 }
 
+// eight columns of the result, `left` of which exist
+__device__ __forceinline__ void store_out(const NsMat& L, int dt, int row, int col, int left, const float (&v)[8]) {
+  if (dt == DP_F32) {
+    float* o = static_cast<float*>(L.out);
+    if (L.transposed) {
+      o += size_t(col) * L.ldo + row;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) if (e < left) o[e * L.ldo] = v[e];
+    } else {
+      o += size_t(row) * L.ldo + col;
+      if (left >= 8 && (reinterpret_cast<uintptr_t>(o) & 31) == 0) ptx::st_global_v8(o, v);
+      else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) if (e < left) o[e] = v[e];
+      }
+    }
+  } else {
+    __nv_bfloat16* o = static_cast<__nv_bfloat16*>(L.out);
+    if (L.transposed) {
+      o += size_t(col) * L.ldo + row;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) if (e < left) o[e * L.ldo] = __float2bfloat16_rn(v[e]);
+    } else {
+      o += size_t(row) * L.ldo + col;
+      if (left >= 8 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+        __nv_bfloat162 h[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+        uint4 w;
+        memcpy(&w, h, 16);
+        *reinterpret_cast<uint4*>(o) = w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) if (e < left) o[e] = __float2bfloat16_rn(v[e]);
+      }
+    }
+  }
+}
+
 template <Product kProduct, bool kPair>
 __global__ void __launch_bounds__(kThreads, 1)
 ns_product_kernel(const __grid_constant__ NsParams P) {
   constexpr int kTile = kPair ? 256 : 128;             // output tile; also columns of an accumulator
-  constexpr bool kRightMn = kProduct == kApply;        // the right operand is contiguous along N
   const uint32_t rank = kPair ? ptx::cluster_ctarank() : 0u;
   const int first_item = kPair ? int(blockIdx.x >> 1) : int(blockIdx.x);
   const int item_stride = kPair ? int(gridDim.x >> 1) : int(gridDim.x);
@@ -188,7 +243,8 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
           ptx::mbar_arrive_expect_tx_a(bar, uint32_t(kPartBytes));
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
-            if (kRightMn && right) ptx::tma_load_3d_a(dst + b * kBoxBytes, tm, bar, r0 + b * 64, at.k * kBK, at.plane(right));
+            if (exchanged<kProduct, kTile>(right, right ? it.tn : it.tm, at.k))
+              ptx::tma_load_3d_a(dst + b * kBoxBytes, tm, bar, r0 + b * 64, at.k * kBK, at.plane(right));
             else ptx::tma_load_3d_a(dst + b * kBoxBytes, tm, bar, at.k * kBK, r0 + b * 64, at.plane(right));
           }
         }
@@ -206,50 +262,62 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
   } else if (warp == 1) {
     // --------------------------------------------------------------- MMA issuer
     if (rank == 0) {
-      // fp16 operands: format 0 in place of bf16's 1 in bits 7 and 10
-      constexpr uint32_t idesc = ptx::idesc_bf16_f32(kTile, kTile, 0, kRightMn ? 1 : 0) & ~((1u << 7) | (1u << 10));
+      // fp16 operands: format 0 in place of bf16's 1 in bits 7 and 10; bits 15, 16: left, right operand contiguous along M, N
+      constexpr uint32_t idesc0 = ptx::idesc_bf16_f32(kTile, kTile, 0, 0) & ~((1u << 7) | (1u << 10));
       // K-major: groups of 8 rows 1 KiB apart, 16 columns further 32 bytes; MN-major: 64-column boxes apart, 16 rows 2 KiB
       constexpr uint64_t dk = ptx::smem_desc_base(16, 1024, ptx::SWIZZLE_128B);
       constexpr uint64_t dmn = ptx::smem_desc_base(kBoxBytes, 1024, ptx::SWIZZLE_128B);
       constexpr uint32_t desc_hi = uint32_t(dk >> 32);
       static_assert(desc_hi == uint32_t(dmn >> 32), "descriptors differ in the low word only");
       const uint32_t base = (tiles_a >> 4) & 0x3FFF;
-      const uint32_t lo_p0 = uint32_t(dk) | base;
-      const uint32_t lo_q0 = (kRightMn ? uint32_t(dmn) : uint32_t(dk)) | (base + (kPartBytes >> 4));
       const uint32_t go_a = kPair ? ready_a : full_a;
-      uint32_t stage = 0, phase = 0, n_item = 0;
+      uint32_t stage = 0, phase = 0, n_chunk = 0;
       int lay = 0;
       bool ok = true;
-      for (int item = first_item; item < P.total_items && ok; item += item_stride, ++n_item) {
+      for (int item = first_item; item < P.total_items && ok; item += item_stride) {
         const Item it = decode_item<kProduct, kTile>(P, item, lay);
-        const uint32_t buf = n_item & 1, acc_phase = (n_item >> 1) & 1;
-        ok = ptx::warp_ok(kPair ? ptx::mbar_wait_cluster(&acc_empty[buf], acc_phase ^ 1, abort_flag, P.wait_limit)
-                                : ptx::mbar_wait(&acc_empty[buf], acc_phase ^ 1, abort_flag, P.wait_limit));
-        if (!ok) break;
-        ptx::tc_fence_after();
-        const uint32_t d_tmem = tmem_base + buf * kTile;
-        const int steps = 3 * P.mat[it.mat].ksteps;
+        const int ksteps = P.mat[it.mat].ksteps, steps = 3 * ksteps;
+        Walk at;
+        uint32_t d_tmem = 0, more = 0;
+        int left = 0;                                  // steps left in this accumulator
         for (int j = 0; j < steps; ++j) {
+          const uint32_t buf = n_chunk & 1;
+          if (left == 0) {
+            ok = ptx::warp_ok(kPair ? ptx::mbar_wait_cluster(&acc_empty[buf], ((n_chunk >> 1) & 1) ^ 1, abort_flag, P.wait_limit)
+                                    : ptx::mbar_wait(&acc_empty[buf], ((n_chunk >> 1) & 1) ^ 1, abort_flag, P.wait_limit));
+            if (!ok) break;
+            d_tmem = tmem_base + buf * kTile;
+            left = min((j == 0 ? 2 * ksteps : 0) + kChunk, steps - j);
+            more = 0;
+          }
           ok = ptx::warp_ok(kPair ? ptx::mbar_wait_cluster_a(go_a + 8 * stage, phase, abort_flag, P.wait_limit)
                                   : ptx::mbar_wait_a(go_a + 8 * stage, phase, abort_flag, P.wait_limit));
           if (!ok) break;
           ptx::tc_fence_after();
-          const uint32_t lo_p = lo_p0 + stage * (kStageBytes >> 4), lo_q = lo_q0 + stage * (kStageBytes >> 4);
+          const bool xp = exchanged<kProduct, kTile>(false, it.tm, at.k), xq = exchanged<kProduct, kTile>(true, it.tn, at.k);
+          const uint32_t idesc = idesc0 | (xp ? 1u << 15 : 0u) | (xq ? 1u << 16 : 0u);
+          const uint32_t lo_p = (xp ? uint32_t(dmn) : uint32_t(dk)) | (base + stage * (kStageBytes >> 4));
+          const uint32_t lo_q = (xq ? uint32_t(dmn) : uint32_t(dk)) | (base + stage * (kStageBytes >> 4) + (kPartBytes >> 4));
+          const uint32_t dp = xp ? 128 : 2, dq = xq ? 128 : 2;
+          --left;
           if (ptx::elect_one()) {
 #pragma unroll
             for (int kk = 0; kk < kBK / 16; ++kk) {
-              const uint32_t p = lo_p + kk * 2, q = lo_q + kk * (kRightMn ? 128 : 2), more = (j > 0 || kk > 0) ? 1u : 0u;
-              if (kPair) ptx::mma_bf16_ss_pair_lh(d_tmem, p, q, desc_hi, idesc, more);
-              else ptx::mma_bf16_ss_lh(d_tmem, p, q, desc_hi, idesc, more);
+              const uint32_t p = lo_p + kk * dp, q = lo_q + kk * dq;
+              if (kPair) ptx::mma_bf16_ss_pair_lh(d_tmem, p, q, desc_hi, idesc, kk ? 1u : more);
+              else ptx::mma_bf16_ss_lh(d_tmem, p, q, desc_hi, idesc, kk ? 1u : more);
             }
             if (kPair) ptx::mma_commit_pair_a(empty_a + 8 * stage, 3);     // stage reusable once these MMAs retire
             else ptx::mma_commit_a(empty_a + 8 * stage);
-            if (j + 1 == steps) {
+            if (left == 0) {
               if (kPair) ptx::mma_commit_pair(&acc_full[buf], 3);
               else ptx::mma_commit(&acc_full[buf]);
             }
           }
           __syncwarp();
+          more = 1;
+          if (left == 0) ++n_chunk;
+          at.next(ksteps);
           if (++stage == kStages) { stage = 0; phase ^= 1; }
         }
       }
@@ -303,34 +371,42 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
         else ptx::st_async_signal_a(acc_empty_remote + 8 * buf, sink_remote);
       }
     };
-    uint32_t n_item = 0;
+    uint32_t n_chunk = 0;
     int lay = 0;
     bool ok = true;
-    for (int item = first_item; item < P.total_items && ok; item += item_stride, ++n_item) {
+    for (int item = first_item; item < P.total_items && ok; item += item_stride) {
       const Item it = decode_item<kProduct, kTile>(P, item, lay);
       const NsMat& L = P.mat[it.mat];
-      const uint32_t buf = n_item & 1, acc_phase = (n_item >> 1) & 1;
-      if (!ptx::mbar_wait_relaxed(&acc_full[buf], acc_phase, abort_flag, P.wait_limit)) { ok = false; break; }
-      ptx::tc_fence_after();
-      const uint32_t t0 = tmem_base + (uint32_t(q * 32) << 16) + buf * kTile + (ew >> 2) * kCols;
-      const int row = it.tm * kTile + int(rank) * 128 + q * 32 + lane;
-      const bool mirror = kProduct != kApply && it.tm != it.tn;
-      const float f_acc = P.f_acc * L.out_scale, f_add = P.f_add * L.out_scale;
-#pragma unroll 1
-      for (int c = 0; c < kCols; c += 32) {
-        uint32_t r[32];
-        ptx::tmem_ld_32x32b_x32(t0 + c, r);
-        ptx::tmem_ld_wait();
-        if (c + 32 == kCols) free_acc(buf);
-        const int col0 = it.tn * kTile + (ew >> 2) * kCols + c;
-        if (row < L.M) {
+      float sum[kCols];
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const int col = col0 + 8 * g, left = L.N - col;
-            if (left <= 0) break;
+      for (int e = 0; e < kCols; ++e) sum[e] = 0.f;
+      for (int left = chunks_of(L.ksteps); left > 0; --left, ++n_chunk) {
+        const uint32_t buf = n_chunk & 1;
+        if (!ptx::mbar_wait_relaxed(&acc_full[buf], (n_chunk >> 1) & 1, abort_flag, P.wait_limit)) { ok = false; break; }
+        ptx::tc_fence_after();
+        const uint32_t t0 = tmem_base + (uint32_t(q * 32) << 16) + buf * kTile + (ew >> 2) * kCols;
+#pragma unroll
+        for (int c = 0; c < kCols; c += 16) {
+          uint32_t r[16];
+          ptx::tmem_ld_32x32b_x16(t0 + c, r);
+          ptx::tmem_ld_wait();
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sum[c + e] += __uint_as_float(r[e]);
+        }
+        free_acc(buf);
+      }
+      if (!ok) break;
+      const int row = it.tm * kTile + int(rank) * 128 + q * 32 + lane;
+      const int col0 = it.tn * kTile + (ew >> 2) * kCols;
+      const float f_acc = P.f_acc * L.out_scale, f_add = P.f_add * L.out_scale;
+      if (row < L.M) {
+#pragma unroll
+        for (int g = 0; g < kCols / 8; ++g) {
+          const int col = col0 + 8 * g, left = L.N - col;
+          if (left > 0) {
             float v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = f_acc * __uint_as_float(r[8 * g + e]);
+            for (int e = 0; e < 8; ++e) v[e] = f_acc * sum[8 * g + e];
             if (kProduct != kGram) {
               float a[8];
               unpack_add(L.add + size_t(row) * L.ld_add + col, L.plane_add, a);
@@ -348,51 +424,13 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
               *reinterpret_cast<uint4*>(d) = w;
               memcpy(&w, lo, 16);
               *reinterpret_cast<uint4*>(d + L.plane_dst) = w;
-              if (mirror) {
-                __half* t = L.dst + size_t(col) * L.ld_dst + row;
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                  if (e < left) { t[size_t(e) * L.ld_dst] = hi[e]; t[size_t(e) * L.ld_dst + L.plane_dst] = lo[e]; }
-              }
-            } else if (P.out_dt == DP_F32) {
-              float* o = static_cast<float*>(L.out);
-              if (L.transposed) {
-                o += size_t(col) * L.ldo + row;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) if (e < left) o[e * L.ldo] = v[e];
-              } else {
-                o += size_t(row) * L.ldo + col;
-                if (left >= 8 && (reinterpret_cast<uintptr_t>(o) & 31) == 0) ptx::st_global_v8(o, v);
-                else {
-#pragma unroll
-                  for (int e = 0; e < 8; ++e) if (e < left) o[e] = v[e];
-                }
-              }
             } else {
-              __nv_bfloat16* o = static_cast<__nv_bfloat16*>(L.out);
-              if (L.transposed) {
-                o += size_t(col) * L.ldo + row;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) if (e < left) o[e * L.ldo] = __float2bfloat16_rn(v[e]);
-              } else {
-                o += size_t(row) * L.ldo + col;
-                if (left >= 8 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
-                  __nv_bfloat162 h[4];
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) h[e] = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
-                  uint4 w;
-                  memcpy(&w, h, 16);
-                  *reinterpret_cast<uint4*>(o) = w;
-                } else {
-#pragma unroll
-                  for (int e = 0; e < 8; ++e) if (e < left) o[e] = __float2bfloat16_rn(v[e]);
-                }
-              }
+              store_out(L, P.out_dt, row, col, left, v);
             }
           }
         }
-        __syncwarp();                                        // the TMEM load is a warp operation
       }
+      __syncwarp();
     }
     if (!ok && lane == 0) {
       *abort_flag = 1;
@@ -585,6 +623,25 @@ int tiles_of(Product product, int m, int n, int tile) {
   return product == kApply ? tm * ceil_div(n, tile) : tm * (tm + 1) / 2;
 }
 
+// CTA pairs or single CTAs, the same for all products of a call, since symmetric matrices are stored by the tile: whichever
+// takes less time in whole waves, a pair's tile twice as long as a quarter of it on one CTA.
+bool take_pairs(const std::vector<NsShape>& shapes) {
+  double pair = 0, single = 0;
+  for (int q = 0; q < 3; ++q) {
+    long long big = 0, small = 0, ksteps = 0;
+    for (const NsShape& s : shapes) {
+      big += tiles_of(Product(q), s.m, s.n, 256);
+      small += tiles_of(Product(q), s.m, s.n, 128);
+      ksteps += (long long)tiles_of(Product(q), s.m, s.n, 256) * ceil_div(q == kGram ? s.n : s.m, kBK);
+    }
+    const int units = sm_count();
+    const double k = double(ksteps) / double(big);
+    pair += 2 * k * double((big + units / 2 - 1) / (units / 2));
+    single += k * double((small + units - 1) / units);
+  }
+  return pair <= single;
+}
+
 // One product of all matrices of a group.
 dp_status ns_product(Product product, NsParams& P, bool pair, cudaStream_t st) {
   if (pair) {
@@ -619,15 +676,15 @@ dp_status ns_group(const dp_matrix_desc* mats, int n, dp_dtype dt, dp_dtype out_
   ns_split_kernel<<<blocks, 256, 0, st>>>(In);
   DP_LAUNCH_OK();
 
+  std::vector<NsShape> shapes;
+  for (const Place& p : at) shapes.push_back(p.s);
+  const bool pair = take_pairs(shapes);
   const int steps = int(plan.size());
   for (int k = 0; k < steps; ++k) {
     const NsStep& S = plan[k];
     const bool last = k + 1 == steps;
     for (int q = 0; q < 3; ++q) {
       const Product product = Product(q);
-      int big = 0;
-      for (int i = 0; i < n; ++i) big += tiles_of(product, at[i].s.m, at[i].s.n, 256);
-      const bool pair = big >= sm_count() / 2;         // a tile for every CTA pair
       NsParams P;
       memset(&P, 0, sizeof(P));
       int items = 0;
