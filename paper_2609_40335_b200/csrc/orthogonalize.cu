@@ -10,10 +10,10 @@
 // of fp16, high and low terms (22 bits), scaled by powers of two that the host derives from bounds of the polynomials (|X| <= s
 // in the spectral norm gives |A| <= s^2 and so on), so that nothing overflows and small entries keep their low terms: one
 // bf16 product per product is off by 1e-2 after five steps, two bf16 terms by 2e-5, these by what the sums round.
-// An MMA rounds its sum towards zero, by as much as the sum is large.  So lo hi' and hi lo' of all of K come before hi hi', and
-// hi hi' is summed in chunks of 256 of K, each in an accumulator of its own, that the epilogue adds up in registers to nearest:
-// error of DistilGPT2's updates against 64 bits 2.2e-5 with one accumulator per tile (the diagonal of A, a sum of squares,
-// came out 6e-6 too small at K = 3072).
+// An MMA rounds its sum towards zero, by as much as the sum is large.  So sums are taken in chunks of 128 of K, each in an
+// accumulator of its own, that the epilogue adds up in registers to nearest: error of DistilGPT2's updates against 64 bits 2.2e-5
+// with one accumulator per tile (the diagonal of A, a sum of squares, came out 6e-6 too small at K = 3072).  a goes onto the
+// diagonal of B, so that a X + B X is one product with nothing to add.
 // A and A A are symmetric: tiles on and below the diagonal are computed and stored, and a product that needs one above it reads the
 // stored one with rows and columns exchanged (the tensor core takes either order).
 //
@@ -41,19 +41,19 @@ namespace {
 constexpr int kBK = 64;
 constexpr int kBoxBytes = 64 * 128;                   // 64 rows x 64 fp16
 constexpr int kPartBytes = 2 * kBoxBytes;             // 128 rows (or columns) of an operand
-constexpr int kStageBytes = 2 * kPartBytes;
-constexpr int kStages = 7;
+constexpr int kStageBytes = 4 * kPartBytes;           // high and low terms of the left and of the right operand
+constexpr int kStages = 3;
 constexpr size_t kSmemBytes = size_t(kStages) * kStageBytes + 1024 + 512;
 constexpr int kRelayWarp = 2, kProducerQWarp = 3, kEpiWarp0 = 4, kEpiWarps = 16;
 constexpr int kThreads = (kEpiWarp0 + kEpiWarps) * 32;
-constexpr int kChunk = 4;                             // K steps of hi hi' per accumulator
+constexpr int kChunk = 2;                             // K steps per accumulator
 constexpr int kNsMaxMats = 96;                        // matrices per launch (parameter-block limit)
 constexpr int kNormParts = 32;                        // partial sums of a matrix's squares
 
 enum Product { kGram, kPoly, kApply };                // A = X X^T, B = b A + c A A, X' = a X + B X
 
 struct NsMat {
-  const __half* add;         // planes that the epilogue adds (A or X), rows of `ld_add`
+  const __half* add;         // A's planes, which kPoly adds, rows of `ld_add`
   __half* dst;               // planes written, or nullptr: `out`
   void* out;
   long long plane_add, plane_dst, ldo;
@@ -70,7 +70,8 @@ struct __align__(64) NsParams {
   NsMat mat[kNsMaxMats];
   int n_mats, total_items;
   int out_dt;
-  float f_acc, f_add;        // written value = f_acc * product + f_add * (high + low term of `add`)
+  float f_acc;               // written value = f_acc * product
+  float f_add, diagonal;     //   + f_add * (high + low term of `add`), + diagonal where row = column (kPoly)
   int* dev_status;
   long long wait_limit;
 };
@@ -97,13 +98,6 @@ __device__ __forceinline__ Item decode_item(const NsParams& P, int item, int& l)
   return it;
 }
 
-// K steps of a tile: lo hi' of all of K, hi lo', then hi hi'
-struct Walk {
-  int k = 0, term = 0;
-  __device__ __forceinline__ int plane(bool right) const { return term == (right ? 1 : 0) ? 1 : 0; }
-  __device__ __forceinline__ void next(int ksteps) { if (++k == ksteps) { k = 0; ++term; } }
-};
-
 // Whether a K step of a symmetric operand's row tile `t` lies above the diagonal's tiles: there the stored tile is the transpose,
 // contiguous along the rows that are wanted.
 template <Product kProduct, int kTile>
@@ -120,53 +114,75 @@ __device__ __forceinline__ void split_fp16(float v, __half& hi, __half& lo) {
   lo = __float2half_rn(v - __half2float(hi));
 }
 
-__device__ __forceinline__ void unpack_add(const __half* p, long long plane, float (&v)[8]) {
-  const uint4 h = *reinterpret_cast<const uint4*>(p), l = *reinterpret_cast<const uint4*>(p + plane);
-  const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
+// 16 consecutive values of two planes, on a 32-byte boundary
+__device__ __forceinline__ void load_planes(const __half* p, long long plane, float (&v)[16]) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&hw[e]));
-    const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&lw[e]));
-    v[2 * e] = a.x + b.x;
-    v[2 * e + 1] = a.y + b.y;
+  for (int h = 0; h < 2; ++h) {
+    const uint4 a = reinterpret_cast<const uint4*>(p)[h], b = reinterpret_cast<const uint4*>(p + plane)[h];
+    const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&aw[e]));
+      const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&bw[e]));
+      v[8 * h + 2 * e] = x.x + y.x;
+      v[8 * h + 2 * e + 1] = x.y + y.y;
+    }
   }
 }
+__device__ __forceinline__ void store_planes(__half* p, long long plane, const float (&v)[16]) {
+  float hi[8], lo[8];                                  // pairs of fp16
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    __half2 h, l;
+    split_fp16(v[2 * e], h.x, l.x);
+    split_fp16(v[2 * e + 1], h.y, l.y);
+    memcpy(&hi[e], &h, 4);
+    memcpy(&lo[e], &l, 4);
+  }
+  ptx::st_global_v8_keep(reinterpret_cast<float*>(p), hi);
+  ptx::st_global_v8_keep(reinterpret_cast<float*>(p + plane), lo);
+}
 
-// eight columns of the result, `left` of which exist
-__device__ __forceinline__ void store_out(const NsMat& L, int dt, int row, int col, int left, const float (&v)[8]) {
+// 16 columns of the result, `left` of which exist
+__device__ __forceinline__ void store_out(const NsMat& L, int dt, int row, int col, int left, const float (&v)[16]) {
+  if (L.transposed) {                                  // a warp's lanes lie side by side
+    const size_t at = size_t(col) * L.ldo + row;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      if (e >= left) continue;
+      if (dt == DP_F32) static_cast<float*>(L.out)[at + e * L.ldo] = v[e];
+      else static_cast<__nv_bfloat16*>(L.out)[at + e * L.ldo] = __float2bfloat16_rn(v[e]);
+    }
+    return;
+  }
+  const size_t at = size_t(row) * L.ldo + col;
   if (dt == DP_F32) {
-    float* o = static_cast<float*>(L.out);
-    if (L.transposed) {
-      o += size_t(col) * L.ldo + row;
+    float* o = static_cast<float*>(L.out) + at;
+    if (left >= 16 && (reinterpret_cast<uintptr_t>(o) & 31) == 0) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) if (e < left) o[e * L.ldo] = v[e];
-    } else {
-      o += size_t(row) * L.ldo + col;
-      if (left >= 8 && (reinterpret_cast<uintptr_t>(o) & 31) == 0) ptx::st_global_v8(o, v);
-      else {
+      for (int h = 0; h < 2; ++h) {
+        float w[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) if (e < left) o[e] = v[e];
+        for (int e = 0; e < 8; ++e) w[e] = v[8 * h + e];
+        ptx::st_global_v8(o + 8 * h, w);
       }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) if (e < left) o[e] = v[e];
     }
   } else {
-    __nv_bfloat16* o = static_cast<__nv_bfloat16*>(L.out);
-    if (L.transposed) {
-      o += size_t(col) * L.ldo + row;
+    __nv_bfloat16* o = static_cast<__nv_bfloat16*>(L.out) + at;
+    if (left >= 16 && (reinterpret_cast<uintptr_t>(o) & 31) == 0) {
+      float w[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) if (e < left) o[e * L.ldo] = __float2bfloat16_rn(v[e]);
-    } else {
-      o += size_t(row) * L.ldo + col;
-      if (left >= 8 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
-        __nv_bfloat162 h[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
-        uint4 w;
-        memcpy(&w, h, 16);
-        *reinterpret_cast<uint4*>(o) = w;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) if (e < left) o[e] = __float2bfloat16_rn(v[e]);
+      for (int e = 0; e < 8; ++e) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+        memcpy(&w[e], &h, 4);
       }
+      ptx::st_global_v8(reinterpret_cast<float*>(o), w);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) if (e < left) o[e] = __float2bfloat16_rn(v[e]);
     }
   }
 }
@@ -233,24 +249,22 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
       const int ksteps = P.mat[it.mat].ksteps;
       // first of this CTA's 128 rows (columns) of the operand
       const int r0 = (right ? it.tn : it.tm) * kTile + int(rank) * 128;
-      Walk at;
-      for (int j = 0; j < 3 * ksteps; ++j) {
+      for (int k = 0; k < ksteps; ++k) {
         ok = ptx::warp_ok(ptx::mbar_wait_a(empty_a + 8 * stage, phase ^ 1, abort_flag, P.wait_limit));
         if (!ok) break;
         const uint32_t bar = full_a + 8 * stage;
-        const uint32_t dst = tiles_a + stage * kStageBytes + (right ? kPartBytes : 0);
+        const uint32_t dst = tiles_a + stage * kStageBytes + (right ? 2 * kPartBytes : 0);
+        const bool x = exchanged<kProduct, kTile>(right, right ? it.tn : it.tm, k);
         if (ptx::elect_one()) {
-          ptx::mbar_arrive_expect_tx_a(bar, uint32_t(kPartBytes));
+          ptx::mbar_arrive_expect_tx_a(bar, uint32_t(2 * kPartBytes));
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            if (exchanged<kProduct, kTile>(right, right ? it.tn : it.tm, at.k))
-              ptx::tma_load_3d_a(dst + b * kBoxBytes, tm, bar, r0 + b * 64, at.k * kBK, at.plane(right));
-            else ptx::tma_load_3d_a(dst + b * kBoxBytes, tm, bar, at.k * kBK, r0 + b * 64, at.plane(right));
+          for (int b = 0; b < 4; ++b) {                // two boxes of high terms, two of low ones
+            const int r = r0 + (b & 1) * 64;
+            ptx::tma_load_3d_a(dst + b * kBoxBytes, tm, bar, x ? r : k * kBK, x ? k * kBK : r, b >> 1);
           }
         }
         __syncwarp();
         ++issued;
-        at.next(ksteps);
         if (++stage == kStages) { stage = 0; phase ^= 1; }
       }
     }
@@ -276,48 +290,47 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
       bool ok = true;
       for (int item = first_item; item < P.total_items && ok; item += item_stride) {
         const Item it = decode_item<kProduct, kTile>(P, item, lay);
-        const int ksteps = P.mat[it.mat].ksteps, steps = 3 * ksteps;
-        Walk at;
-        uint32_t d_tmem = 0, more = 0;
-        int left = 0;                                  // steps left in this accumulator
-        for (int j = 0; j < steps; ++j) {
+        const int ksteps = P.mat[it.mat].ksteps;
+        uint32_t d_tmem = 0;
+        for (int k = 0; k < ksteps; ++k) {
           const uint32_t buf = n_chunk & 1;
-          if (left == 0) {
+          const bool first = k % kChunk == 0, last = k % kChunk == kChunk - 1 || k + 1 == ksteps;
+          if (first) {
             ok = ptx::warp_ok(kPair ? ptx::mbar_wait_cluster(&acc_empty[buf], ((n_chunk >> 1) & 1) ^ 1, abort_flag, P.wait_limit)
                                     : ptx::mbar_wait(&acc_empty[buf], ((n_chunk >> 1) & 1) ^ 1, abort_flag, P.wait_limit));
             if (!ok) break;
             d_tmem = tmem_base + buf * kTile;
-            left = min((j == 0 ? 2 * ksteps : 0) + kChunk, steps - j);
-            more = 0;
           }
           ok = ptx::warp_ok(kPair ? ptx::mbar_wait_cluster_a(go_a + 8 * stage, phase, abort_flag, P.wait_limit)
                                   : ptx::mbar_wait_a(go_a + 8 * stage, phase, abort_flag, P.wait_limit));
           if (!ok) break;
           ptx::tc_fence_after();
-          const bool xp = exchanged<kProduct, kTile>(false, it.tm, at.k), xq = exchanged<kProduct, kTile>(true, it.tn, at.k);
+          const bool xp = exchanged<kProduct, kTile>(false, it.tm, k), xq = exchanged<kProduct, kTile>(true, it.tn, k);
           const uint32_t idesc = idesc0 | (xp ? 1u << 15 : 0u) | (xq ? 1u << 16 : 0u);
           const uint32_t lo_p = (xp ? uint32_t(dmn) : uint32_t(dk)) | (base + stage * (kStageBytes >> 4));
-          const uint32_t lo_q = (xq ? uint32_t(dmn) : uint32_t(dk)) | (base + stage * (kStageBytes >> 4) + (kPartBytes >> 4));
+          const uint32_t lo_q = (xq ? uint32_t(dmn) : uint32_t(dk)) | (base + stage * (kStageBytes >> 4) + (2 * kPartBytes >> 4));
           const uint32_t dp = xp ? 128 : 2, dq = xq ? 128 : 2;
-          --left;
           if (ptx::elect_one()) {
 #pragma unroll
-            for (int kk = 0; kk < kBK / 16; ++kk) {
-              const uint32_t p = lo_p + kk * dp, q = lo_q + kk * dq;
-              if (kPair) ptx::mma_bf16_ss_pair_lh(d_tmem, p, q, desc_hi, idesc, kk ? 1u : more);
-              else ptx::mma_bf16_ss_lh(d_tmem, p, q, desc_hi, idesc, kk ? 1u : more);
+            for (int t = 0; t < 3; ++t) {              // lo hi', hi lo', hi hi': the small products while the sum is small
+              constexpr uint32_t low = kPartBytes >> 4;
+#pragma unroll
+              for (int kk = 0; kk < kBK / 16; ++kk) {
+                const uint32_t p = lo_p + (t == 0 ? low : 0u) + kk * dp, q = lo_q + (t == 1 ? low : 0u) + kk * dq;
+                const uint32_t more = t || kk || !first ? 1u : 0u;
+                if (kPair) ptx::mma_bf16_ss_pair_lh(d_tmem, p, q, desc_hi, idesc, more);
+                else ptx::mma_bf16_ss_lh(d_tmem, p, q, desc_hi, idesc, more);
+              }
             }
             if (kPair) ptx::mma_commit_pair_a(empty_a + 8 * stage, 3);     // stage reusable once these MMAs retire
             else ptx::mma_commit_a(empty_a + 8 * stage);
-            if (left == 0) {
+            if (last) {
               if (kPair) ptx::mma_commit_pair(&acc_full[buf], 3);
               else ptx::mma_commit(&acc_full[buf]);
             }
           }
           __syncwarp();
-          more = 1;
-          if (left == 0) ++n_chunk;
-          at.next(ksteps);
+          if (last) ++n_chunk;
           if (++stage == kStages) { stage = 0; phase ^= 1; }
         }
       }
@@ -338,7 +351,7 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
       bool ok = true;
       for (int item = first_item; item < P.total_items && ok; item += item_stride) {
         const Item it = decode_item<kProduct, kTile>(P, item, lay);
-        for (int j = 3 * P.mat[it.mat].ksteps; j > 0; --j) {
+        for (int k = P.mat[it.mat].ksteps; k > 0; --k) {
           ok = ptx::warp_ok(ptx::mbar_wait_a(full_a + 8 * stage, phase, abort_flag, P.wait_limit));
           if (!ok) break;
           if (ptx::elect_one()) {
@@ -398,35 +411,25 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
       if (!ok) break;
       const int row = it.tm * kTile + int(rank) * 128 + q * 32 + lane;
       const int col0 = it.tn * kTile + (ew >> 2) * kCols;
-      const float f_acc = P.f_acc * L.out_scale, f_add = P.f_add * L.out_scale;
+      const float f_acc = P.f_acc * L.out_scale;
       if (row < L.M) {
+        // 16 columns at a time: 32 bytes of a plane, a whole sector, per lane and store
 #pragma unroll
-        for (int g = 0; g < kCols / 8; ++g) {
-          const int col = col0 + 8 * g, left = L.N - col;
+        for (int g = 0; g < kCols / 16; ++g) {
+          const int col = col0 + 16 * g, left = L.N - col;
           if (left > 0) {
-            float v[8];
+            float v[16];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = f_acc * sum[8 * g + e];
-            if (kProduct != kGram) {
-              float a[8];
-              unpack_add(L.add + size_t(row) * L.ld_add + col, L.plane_add, a);
+            for (int e = 0; e < 16; ++e) v[e] = f_acc * sum[16 * g + e];
+            if (kProduct == kPoly) {
+              float a[16];
+              load_planes(L.add + size_t(row) * L.ld_add + col, L.plane_add, a);
 #pragma unroll
-              for (int e = 0; e < 8; ++e) v[e] = fmaf(f_add, a[e], v[e]);
+              for (int e = 0; e < 16; ++e) v[e] = fmaf(P.f_add, a[e], v[e]) + (col + e == row ? P.diagonal : 0.f);
             }
-            if (kProduct != kApply || L.dst) {
-              // rows are padded to whole chunks of eight, which nobody reads
-              __half hi[8], lo[8];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) split_fp16(v[e], hi[e], lo[e]);
-              __half* d = L.dst + size_t(row) * L.ld_dst + col;
-              uint4 w;
-              memcpy(&w, hi, 16);
-              *reinterpret_cast<uint4*>(d) = w;
-              memcpy(&w, lo, 16);
-              *reinterpret_cast<uint4*>(d + L.plane_dst) = w;
-            } else {
-              store_out(L, P.out_dt, row, col, left, v);
-            }
+            // rows are padded to whole chunks of 16, which nobody reads
+            if (kProduct != kApply || L.dst) store_planes(L.dst + size_t(row) * L.ld_dst + col, L.plane_dst, v);
+            else store_out(L, P.out_dt, row, col, left, v);
           }
         }
       }
@@ -455,7 +458,7 @@ struct NsIn {
   long long ldm, plane;
   __half* X;                 // planes of the m x n matrix
   int p, d, ldx;
-  int transposed;
+  int transposed, vec;       // vec: rows on 16-byte boundaries
   int block_begin;
 };
 struct NsInParams {
@@ -466,9 +469,11 @@ struct NsInParams {
   float scale;
 };
 
-__device__ __forceinline__ float ns_load(const NsIn& L, int dt, int r, int c) {
+// eight columns of a row, zeros past its end
+__device__ __forceinline__ void ns_load8(const NsIn& L, int dt, int r, int c, float (&v)[8]) {
   const size_t at = size_t(r) * size_t(L.ldm) + c;
-  return dt == DP_F32 ? static_cast<const float*>(L.M)[at] : __bfloat162float(static_cast<const __nv_bfloat16*>(L.M)[at]);
+  if (dt == DP_F32) load8<float>(static_cast<const float*>(L.M) + at, L.d - c, L.vec, v);
+  else load8<__nv_bfloat16>(static_cast<const __nv_bfloat16*>(L.M) + at, L.d - c, L.vec, v);
 }
 
 // squares of a matrix, kNormParts blocks each; in 64 bits, whose range holds the square of every fp32 number
@@ -477,12 +482,29 @@ ns_norm_kernel(const __grid_constant__ NsInParams P) {
   __shared__ double red[8];
   const int l = blockIdx.x / kNormParts, part = blockIdx.x % kNormParts;
   const NsIn& L = P.mat[l];
+  const int chunks = (L.d + 7) / 8;                   // of eight columns; a thread's lie 256 * kNormParts apart
+  const long long total = (long long)chunks * L.p, stride = 256LL * kNormParts;
+  const int step_r = int(stride / chunks), step_c = int(stride % chunks);
+  long long k = part * 256LL + threadIdx.x;
+  int r = int(k / chunks), c = int(k % chunks);
   double s = 0.0;
-  for (int r = part; r < L.p; r += kNormParts)
-    for (int c = threadIdx.x; c < L.d; c += 256) {
-      const double v = double(ns_load(L, P.dt, r, c));
-      s = fma(v, v, s);
+  while (k < total) {
+    float v[4][8];
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (k < total) { ns_load8(L, P.dt, r, 8 * c, v[u]); ++n; }
+      k += stride;
+      r += step_r;
+      c += step_c;
+      if (c >= chunks) { c -= chunks; ++r; }
     }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (u < n)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = fma(double(v[u][e]), double(v[u][e]), s);
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
@@ -498,7 +520,7 @@ ns_norm_kernel(const __grid_constant__ NsInParams P) {
 __global__ void __launch_bounds__(256)
 ns_split_kernel(const __grid_constant__ NsInParams P) {
   __shared__ float tile[64][65];
-  __shared__ double factor;
+  __shared__ float factor[3];
   int lo = 0, hi = P.n_mats - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -509,24 +531,54 @@ ns_split_kernel(const __grid_constant__ NsInParams P) {
     double s = P.partials[lo * kNormParts + threadIdx.x];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (threadIdx.x == 0) factor = double(P.scale) / (sqrt(s) + P.eps);
+    if (threadIdx.x == 0) {
+      // as a number in [1, 2) and two powers of two, since fp32 may hold neither the factor nor its inverse
+      const double f = double(P.scale) / (sqrt(s) + P.eps);
+      int e = 0;
+      if (f > 0 && f <= 1.7e308) e = ilogb(f);
+      factor[0] = float(scalbn(f, -e));
+      factor[1] = float(scalbn(1.0, e / 2));
+      factor[2] = float(scalbn(1.0, e - e / 2));
+    }
   }
   const int local = blockIdx.x - L.block_begin, tiles_c = (L.d + 63) / 64;
   const int r0 = local / tiles_c * 64, c0 = local % tiles_c * 64;
-  const int x = threadIdx.x & 63, y0 = threadIdx.x >> 6;
-#pragma unroll 4
-  for (int y = y0; y < 64; y += 4)
-    tile[y][x] = r0 + y < L.p && c0 + x < L.d ? ns_load(L, P.dt, r0 + y, c0 + x) : 0.f;
+  const int x = (threadIdx.x & 7) * 8, y0 = threadIdx.x >> 3;        // eight columns of rows y0 and y0 + 32
+  float v[2][8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = r0 + y0 + 32 * h;
+    if (r < L.p && c0 + x < L.d) ns_load8(L, P.dt, r, c0 + x, v[h]);
+    else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[h][e] = 0.f;
+    }
+  }
+  if (L.transposed) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) tile[y0 + 32 * h][x + e] = v[h][e];
+  }
   __syncthreads();
-#pragma unroll 4
-  for (int y = y0; y < 64; y += 4) {
-    const int r = (L.transposed ? c0 : r0) + y, c = (L.transposed ? r0 : c0) + x;
-    if (r < (L.transposed ? L.d : L.p) && c < (L.transposed ? L.p : L.d)) {
-      __half h, l;
-      split_fp16(float(double(L.transposed ? tile[x][y] : tile[y][x]) * factor), h, l);
+  const float f0 = factor[0], f1 = factor[1], f2 = factor[2];
+  const int rows = L.transposed ? L.d : L.p, cols = L.transposed ? L.p : L.d;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = (L.transposed ? c0 : r0) + y0 + 32 * h, c = (L.transposed ? r0 : c0) + x;
+    if (r < rows && c < cols) {                        // whole chunks of eight: rows of X are padded to 16
+      __half a[8], b[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float w = L.transposed ? tile[x + e][y0 + 32 * h] : v[h][e];
+        split_fp16(w * f1 * f2 * f0, a[e], b[e]);
+      }
       __half* to = L.X + size_t(r) * L.ldx + c;
-      to[0] = h;
-      to[L.plane] = l;
+      uint4 q;
+      memcpy(&q, a, 16);
+      *reinterpret_cast<uint4*>(to) = q;
+      memcpy(&q, b, 16);
+      *reinterpret_cast<uint4*>(to + L.plane) = q;
     }
   }
 }
@@ -541,8 +593,8 @@ struct NsShape {
     transposed = D.p > D.d;
     m = std::min(D.p, D.d);
     n = std::max(D.p, D.d);
-    ldx = (n + 7) / 8 * 8;
-    lda = (m + 7) / 8 * 8;
+    ldx = (n + 15) / 16 * 16;
+    lda = (m + 15) / 16 * 16;
     x_bytes = align_up(2 * size_t(m) * ldx * sizeof(__half), 256);
     a_bytes = align_up(2 * size_t(m) * lda * sizeof(__half), 256);
   }
@@ -556,11 +608,11 @@ float scale_for(double bound) {
   return float(ldexp(1.0, 15 - e));
 }
 
-// Bounds of a step on a matrix whose singular values are at most s: of |b l + c l^2| for l <= s^2, of |a x + b x^3 + c x^5|.
+// Bounds of a step on a matrix whose singular values are at most s: of |a + b l + c l^2| for l <= s^2, of |a x + b x^3 + c x^5|.
 void step_bounds(double a, double b, double c, double s, double* poly, double* next) {
-  auto f = [&](double l) { return std::fabs(b * l + c * l * l); };
+  auto f = [&](double l) { return std::fabs(a + b * l + c * l * l); };
   auto g = [&](double x) { return std::fabs(x * (a + x * x * (b + x * x * c))); };
-  *poly = f(s * s);
+  *poly = std::max(std::fabs(a), f(s * s));
   *next = g(s);
   if (c != 0.0) {
     const double l = -b / (2 * c);
@@ -667,7 +719,8 @@ dp_status ns_group(const dp_matrix_desc* mats, int n, dp_dtype dt, dp_dtype out_
     p.A = reinterpret_cast<__half*>(base); base += p.s.a_bytes;
     p.B = reinterpret_cast<__half*>(base); base += p.s.a_bytes;
     at.push_back(p);
-    In.mat[k] = {mats[k].M, mats[k].ldm, (long long)p.s.m * p.s.ldx, p.x[0], mats[k].p, mats[k].d, p.s.ldx, p.s.transposed, blocks};
+    In.mat[k] = {mats[k].M, mats[k].ldm, (long long)p.s.m * p.s.ldx, p.x[0], mats[k].p, mats[k].d, p.s.ldx, p.s.transposed,
+                 aligned16(mats[k].M) && mats[k].ldm * (dt == DP_F32 ? 4 : 2) % 16 == 0, blocks};
     blocks += ceil_div(mats[k].p, 64) * ceil_div(mats[k].d, 64);
   }
   In.n_mats = n; In.dt = dt; In.partials = partials; In.eps = eps; In.scale = plan[0].x;
@@ -711,7 +764,6 @@ dp_status ns_group(const dp_matrix_desc* mats, int n, dp_dtype dt, dp_dtype out_
           if (r == DP_OK) P.tmQ[i] = P.tmP[i];
         } else {
           L.N = nn; L.ksteps = ceil_div(m, kBK);
-          L.add = p.x[k & 1]; L.plane_add = px; L.ld_add = p.s.ldx;
           if (last) { L.out = mats[i].out; L.ldo = mats[i].ldo; L.transposed = p.s.transposed; L.out_scale = mats[i].scale; }
           else { L.dst = p.x[(k + 1) & 1]; L.plane_dst = px; L.ld_dst = p.s.ldx; }
           r = make_tmap_bf16_3d(&P.tmP[i], p.B, p.s.lda, m, m, 2, 64, 64);
@@ -720,13 +772,9 @@ dp_status ns_group(const dp_matrix_desc* mats, int n, dp_dtype dt, dp_dtype out_
         if (r != DP_OK) return r;
       }
       P.n_mats = n; P.total_items = items; P.out_dt = out_dt; P.dev_status = dev_status; P.wait_limit = g_wait_limit;
-      if (product == kGram) { P.f_acc = S.A / (S.x * S.x); P.f_add = 0.f; }
-      else if (product == kPoly) { P.f_acc = S.c * S.B / (S.A * S.A); P.f_add = S.b * S.B / S.A; }
-      else {
-        const float to = last ? 1.f : S.next;
-        P.f_acc = to / (S.B * S.x);
-        P.f_add = S.a * to / S.x;
-      }
+      if (product == kGram) P.f_acc = S.A / (S.x * S.x);
+      else if (product == kPoly) { P.f_acc = S.c * S.B / (S.A * S.A); P.f_add = S.b * S.B / S.A; P.diagonal = S.a * S.B; }
+      else P.f_acc = (last ? 1.f : S.next) / (S.B * S.x);
       const dp_status r = ns_product(product, P, pair, st);
       if (r != DP_OK) return r;
     }
