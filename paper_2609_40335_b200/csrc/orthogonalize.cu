@@ -46,7 +46,7 @@ constexpr int kStages = 3;
 constexpr size_t kSmemBytes = size_t(kStages) * kStageBytes + 1024 + 512;
 constexpr int kRelayWarp = 2, kProducerQWarp = 3, kEpiWarp0 = 4, kEpiWarps = 16;
 constexpr int kThreads = (kEpiWarp0 + kEpiWarps) * 32;
-constexpr int kChunk = 2;                             // K steps per accumulator
+constexpr int kChunk = 1;                             // K steps per accumulator
 constexpr int kNsMaxMats = 96;                        // matrices per launch (parameter-block limit)
 constexpr int kNormParts = 32;                        // partial sums of a matrix's squares
 
