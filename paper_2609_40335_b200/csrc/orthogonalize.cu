@@ -10,10 +10,14 @@
 // of fp16, high and low terms (22 bits), scaled by powers of two that the host derives from bounds of the polynomials (|X| <= s
 // in the spectral norm gives |A| <= s^2 and so on), so that nothing overflows and small entries keep their low terms: one
 // bf16 product per product is off by 1e-2 after five steps, two bf16 terms by 2e-5, these by what the sums round.
-// An MMA rounds its sum towards zero, by as much as the sum is large.  So sums are taken in chunks of 128 of K, each in an
+// An MMA rounds its sum towards zero, by as much as the sum is large.  So sums are taken in K steps of 64, each in an
 // accumulator of its own, that the epilogue adds up in registers to nearest: error of DistilGPT2's updates against 64 bits 2.2e-5
-// with one accumulator per tile (the diagonal of A, a sum of squares, came out 6e-6 too small at K = 3072).  a goes onto the
-// diagonal of B, so that a X + B X is one product with nothing to add.
+// with one accumulator per tile (the diagonal of A, a sum of squares, came out 6e-6 too small at K = 3072).
+//
+// Nothing is added to a product but on the diagonal, so no epilogue reads matrices: with A' = A + q I, q = b / 2c, the square
+// completed, a I + b A + c A A = c A' A' + (a - c q^2) I is B' and X' = B' X.  (A polynomial without c needs no second product; one whose
+// c is so small that q would drown A adds b A instead.)
+//
 // A and A A are symmetric: tiles on and below the diagonal are computed and stored, and a product that needs one above it reads the
 // stored one with rows and columns exchanged (the tensor core takes either order).
 //
@@ -43,21 +47,20 @@ constexpr int kBoxBytes = 64 * 128;                   // 64 rows x 64 fp16
 constexpr int kPartBytes = 2 * kBoxBytes;             // 128 rows (or columns) of an operand
 constexpr int kStageBytes = 4 * kPartBytes;           // high and low terms of the left and of the right operand
 constexpr int kStages = 3;
-constexpr size_t kSmemBytes = size_t(kStages) * kStageBytes + 1024 + 512;
+constexpr int kStagingBytes = 32 * 64;                // a warp's 32 rows x 32 fp16 on their way out
 constexpr int kRelayWarp = 2, kProducerQWarp = 3, kEpiWarp0 = 4, kEpiWarps = 16;
 constexpr int kThreads = (kEpiWarp0 + kEpiWarps) * 32;
-constexpr int kChunk = 1;                             // K steps per accumulator
-constexpr int kNsMaxMats = 96;                        // matrices per launch (parameter-block limit)
+constexpr size_t kSmemBytes = size_t(kStages) * kStageBytes + kEpiWarps * kStagingBytes + 1024 + 512;
+constexpr int kNsMaxMats = 64;                        // matrices per launch (parameter-block limit)
 constexpr int kNormParts = 32;                        // partial sums of a matrix's squares
 
-enum Product { kGram, kPoly, kApply };                // A = X X^T, B = b A + c A A, X' = a X + B X
+enum Product { kGram, kPoly, kApply };                // A' = X X^T + q I, B' = c A' A' + (a - c q^2) I, X' = B' X
 
 struct NsMat {
-  const __half* add;         // A's planes, which kPoly adds, rows of `ld_add`
-  __half* dst;               // planes written, or nullptr: `out`
-  void* out;
-  long long plane_add, plane_dst, ldo;
-  int ld_add, ld_dst;
+  const __half* add;         // kPoly: A's planes where they are added, or nullptr
+  void* out;                 // the call's output, or nullptr: planes, through tmD
+  long long plane_add, ldo;
+  int ld_add;
   int M, N, ksteps;
   int item_begin;
   int transposed;            // out is X'^T
@@ -67,11 +70,12 @@ struct NsMat {
 struct __align__(64) NsParams {
   CUtensorMap tmP[kNsMaxMats];
   CUtensorMap tmQ[kNsMaxMats];
+  CUtensorMap tmD[kNsMaxMats];
   NsMat mat[kNsMaxMats];
   int n_mats, total_items;
   int out_dt;
   float f_acc;               // written value = f_acc * product
-  float f_add, diagonal;     //   + f_add * (high + low term of `add`), + diagonal where row = column (kPoly)
+  float f_add, diagonal;     //   + f_add * (high + low term of `add`), + diagonal where row = column
   int* dev_status;
   long long wait_limit;
 };
@@ -106,16 +110,21 @@ __device__ __forceinline__ bool exchanged(bool right, int t, int k) {
   return kProduct != kGram && k * kBK / kTile > t;
 }
 
-// accumulators that a tile's sum is spread over
-__device__ __forceinline__ int chunks_of(int ksteps) { return (ksteps + kChunk - 1) / kChunk; }
-
 __device__ __forceinline__ void split_fp16(float v, __half& hi, __half& lo) {
   hi = __float2half_rn(v);
   lo = __float2half_rn(v - __half2float(hi));
 }
 
-// 16 consecutive values of two planes, on a 32-byte boundary
-__device__ __forceinline__ void load_planes(const __half* p, long long plane, float (&v)[16]) {
+__device__ __forceinline__ void split_pair(float a, float b, uint32_t& hi, uint32_t& lo) {
+  __half2 h, l;
+  split_fp16(a, h.x, l.x);
+  split_fp16(b, h.y, l.y);
+  memcpy(&hi, &h, 4);
+  memcpy(&lo, &l, 4);
+}
+
+// v += f * (16 consecutive values of two planes)
+__device__ __forceinline__ void add_planes(const __half* p, long long plane, float f, float* v) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const uint4 a = reinterpret_cast<const uint4*>(p)[h], b = reinterpret_cast<const uint4*>(p + plane)[h];
@@ -124,27 +133,14 @@ __device__ __forceinline__ void load_planes(const __half* p, long long plane, fl
     for (int e = 0; e < 4; ++e) {
       const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&aw[e]));
       const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&bw[e]));
-      v[8 * h + 2 * e] = x.x + y.x;
-      v[8 * h + 2 * e + 1] = x.y + y.y;
+      v[8 * h + 2 * e] = fmaf(f, x.x + y.x, v[8 * h + 2 * e]);
+      v[8 * h + 2 * e + 1] = fmaf(f, x.y + y.y, v[8 * h + 2 * e + 1]);
     }
   }
 }
-__device__ __forceinline__ void store_planes(__half* p, long long plane, const float (&v)[16]) {
-  float hi[8], lo[8];                                  // pairs of fp16
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    __half2 h, l;
-    split_fp16(v[2 * e], h.x, l.x);
-    split_fp16(v[2 * e + 1], h.y, l.y);
-    memcpy(&hi[e], &h, 4);
-    memcpy(&lo[e], &l, 4);
-  }
-  ptx::st_global_v8_keep(reinterpret_cast<float*>(p), hi);
-  ptx::st_global_v8_keep(reinterpret_cast<float*>(p + plane), lo);
-}
 
 // 16 columns of the result, `left` of which exist
-__device__ __forceinline__ void store_out(const NsMat& L, int dt, int row, int col, int left, const float (&v)[16]) {
+__device__ __forceinline__ void store_out(const NsMat& L, int dt, int row, int col, int left, const float* v) {
   if (L.transposed) {                                  // a warp's lanes lie side by side
     const size_t at = size_t(col) * L.ldo + row;
 #pragma unroll
@@ -196,7 +192,8 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
   const int item_stride = kPair ? int(gridDim.x >> 1) : int(gridDim.x);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint64_t* bars = reinterpret_cast<uint64_t*>(tiles + size_t(kStages) * kStageBytes);
+  uint8_t* staging = tiles + size_t(kStages) * kStageBytes;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(staging + kEpiWarps * kStagingBytes);
   uint64_t* full = bars;                      // both producers' TMA loads landed
   uint64_t* ready = bars + kStages;           // pair: in both CTAs (rank 0's copy)
   uint64_t* empty = bars + 2 * kStages;       // MMAs retired
@@ -285,22 +282,17 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
       static_assert(desc_hi == uint32_t(dmn >> 32), "descriptors differ in the low word only");
       const uint32_t base = (tiles_a >> 4) & 0x3FFF;
       const uint32_t go_a = kPair ? ready_a : full_a;
-      uint32_t stage = 0, phase = 0, n_chunk = 0;
+      uint32_t stage = 0, phase = 0, n_acc = 0;
       int lay = 0;
       bool ok = true;
       for (int item = first_item; item < P.total_items && ok; item += item_stride) {
         const Item it = decode_item<kProduct, kTile>(P, item, lay);
         const int ksteps = P.mat[it.mat].ksteps;
-        uint32_t d_tmem = 0;
-        for (int k = 0; k < ksteps; ++k) {
-          const uint32_t buf = n_chunk & 1;
-          const bool first = k % kChunk == 0, last = k % kChunk == kChunk - 1 || k + 1 == ksteps;
-          if (first) {
-            ok = ptx::warp_ok(kPair ? ptx::mbar_wait_cluster(&acc_empty[buf], ((n_chunk >> 1) & 1) ^ 1, abort_flag, P.wait_limit)
-                                    : ptx::mbar_wait(&acc_empty[buf], ((n_chunk >> 1) & 1) ^ 1, abort_flag, P.wait_limit));
-            if (!ok) break;
-            d_tmem = tmem_base + buf * kTile;
-          }
+        for (int k = 0; k < ksteps; ++k, ++n_acc) {
+          const uint32_t buf = n_acc & 1, d_tmem = tmem_base + buf * kTile;
+          ok = ptx::warp_ok(kPair ? ptx::mbar_wait_cluster(&acc_empty[buf], ((n_acc >> 1) & 1) ^ 1, abort_flag, P.wait_limit)
+                                  : ptx::mbar_wait(&acc_empty[buf], ((n_acc >> 1) & 1) ^ 1, abort_flag, P.wait_limit));
+          if (!ok) break;
           ok = ptx::warp_ok(kPair ? ptx::mbar_wait_cluster_a(go_a + 8 * stage, phase, abort_flag, P.wait_limit)
                                   : ptx::mbar_wait_a(go_a + 8 * stage, phase, abort_flag, P.wait_limit));
           if (!ok) break;
@@ -317,20 +309,17 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
 #pragma unroll
               for (int kk = 0; kk < kBK / 16; ++kk) {
                 const uint32_t p = lo_p + (t == 0 ? low : 0u) + kk * dp, q = lo_q + (t == 1 ? low : 0u) + kk * dq;
-                const uint32_t more = t || kk || !first ? 1u : 0u;
+                const uint32_t more = t || kk ? 1u : 0u;
                 if (kPair) ptx::mma_bf16_ss_pair_lh(d_tmem, p, q, desc_hi, idesc, more);
                 else ptx::mma_bf16_ss_lh(d_tmem, p, q, desc_hi, idesc, more);
               }
             }
             if (kPair) ptx::mma_commit_pair_a(empty_a + 8 * stage, 3);     // stage reusable once these MMAs retire
             else ptx::mma_commit_a(empty_a + 8 * stage);
-            if (last) {
-              if (kPair) ptx::mma_commit_pair(&acc_full[buf], 3);
-              else ptx::mma_commit(&acc_full[buf]);
-            }
+            if (kPair) ptx::mma_commit_pair(&acc_full[buf], 3);
+            else ptx::mma_commit(&acc_full[buf]);
           }
           __syncwarp();
-          if (last) ++n_chunk;
           if (++stage == kStages) { stage = 0; phase ^= 1; }
         }
       }
@@ -384,7 +373,9 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
         else ptx::st_async_signal_a(acc_empty_remote + 8 * buf, sink_remote);
       }
     };
-    uint32_t n_chunk = 0;
+    uint32_t n_acc = 0;
+    uint8_t* my_staging = staging + ew * kStagingBytes;
+    const uint32_t my_staging_a = ptx::smem_u32(my_staging);
     int lay = 0;
     bool ok = true;
     for (int item = first_item; item < P.total_items && ok; item += item_stride) {
@@ -393,9 +384,11 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
       float sum[kCols];
 #pragma unroll
       for (int e = 0; e < kCols; ++e) sum[e] = 0.f;
-      for (int left = chunks_of(L.ksteps); left > 0; --left, ++n_chunk) {
-        const uint32_t buf = n_chunk & 1;
-        if (!ptx::mbar_wait_relaxed(&acc_full[buf], (n_chunk >> 1) & 1, abort_flag, P.wait_limit)) { ok = false; break; }
+      for (int left = L.ksteps; left > 0; --left, ++n_acc) {
+        const uint32_t buf = n_acc & 1;
+        // no sleep between polls: the accumulator is wanted again in a K step's time
+        ok = ptx::warp_ok(ptx::mbar_wait(&acc_full[buf], (n_acc >> 1) & 1, abort_flag, P.wait_limit));
+        if (!ok) break;
         ptx::tc_fence_after();
         const uint32_t t0 = tmem_base + (uint32_t(q * 32) << 16) + buf * kTile + (ew >> 2) * kCols;
 #pragma unroll
@@ -409,32 +402,56 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
         free_acc(buf);
       }
       if (!ok) break;
-      const int row = it.tm * kTile + int(rank) * 128 + q * 32 + lane;
+      const int row0 = it.tm * kTile + int(rank) * 128 + q * 32, row = row0 + lane;
       const int col0 = it.tn * kTile + (ew >> 2) * kCols;
       const float f_acc = P.f_acc * L.out_scale;
-      if (row < L.M) {
-        // 16 columns at a time: 32 bytes of a plane, a whole sector, per lane and store
+      if (row0 >= L.M) continue;
 #pragma unroll
-        for (int g = 0; g < kCols / 16; ++g) {
-          const int col = col0 + 16 * g, left = L.N - col;
-          if (left > 0) {
-            float v[16];
+      for (int g = 0; g < kCols / 32; ++g) {
+        const int col = col0 + 32 * g;
+        if (col >= L.N) continue;
+        float* v = sum + 32 * g;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] = f_acc * sum[16 * g + e];
-            if (kProduct == kPoly) {
-              float a[16];
-              load_planes(L.add + size_t(row) * L.ld_add + col, L.plane_add, a);
+        for (int e = 0; e < 32; ++e) v[e] *= f_acc;
+        if (kProduct != kApply) {
+          if (kProduct == kPoly && L.add && row < L.M) {
 #pragma unroll
-              for (int e = 0; e < 16; ++e) v[e] = fmaf(P.f_add, a[e], v[e]) + (col + e == row ? P.diagonal : 0.f);
-            }
-            // rows are padded to whole chunks of 16, which nobody reads
-            if (kProduct != kApply || L.dst) store_planes(L.dst + size_t(row) * L.ld_dst + col, L.plane_dst, v);
-            else store_out(L, P.out_dt, row, col, left, v);
+            for (int h = 0; h < 2; ++h)
+              if (col + 16 * h < L.N) add_planes(L.add + size_t(row) * L.ld_add + col + 16 * h, L.plane_add, P.f_add, v + 16 * h);
+          }
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] += col + e == row ? P.diagonal : 0.f;
+        }
+        if (kProduct == kApply && L.out) {
+          if (row < L.M) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              if (col + 16 * h < L.N) store_out(L, P.out_dt, row, col + 16 * h, L.N - col - 16 * h, v + 16 * h);
+          }
+        } else {
+          // 32 x 32 of each plane through shared memory to a TMA store, which leaves out what lies outside the matrix
+          uint32_t hi[16], lo[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) split_pair(v[2 * e], v[2 * e + 1], hi[e], lo[e]);
+          const uint64_t tm = reinterpret_cast<uint64_t>(&P.tmD[it.mat]);
+#pragma unroll
+          for (int plane = 0; plane < 2; ++plane) {
+            const uint32_t* w = plane ? lo : hi;
+            if (lane == 0) ptx::tma_store_wait_read();
+            __syncwarp();
+#pragma unroll
+            for (int c = 0; c < 4; ++c)                // 64-byte swizzle: no two of a quarter-warp's stores share a bank
+              *reinterpret_cast<uint4*>(my_staging + lane * 64 + ((c ^ (lane >> 1 & 3)) << 4)) =
+                  make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) ptx::tma_store_3d_a(tm, my_staging_a, col, row0, plane);
           }
         }
       }
       __syncwarp();
     }
+    if (lane == 0) ptx::tma_store_wait();
     if (!ok && lane == 0) {
       *abort_flag = 1;
       if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
@@ -629,7 +646,9 @@ void step_bounds(double a, double b, double c, double s, double* poly, double* n
   }
 }
 
-struct NsStep { float a, b, c, x, A, B, next; };     // coefficients; scales of X, A, B and the new X
+// A step: scales of X, A', B' and the new X; B' = c A' A' + b A' + d I of A' = A + q I (unscaled).  products 1: B' = b A + d I comes
+// out of X X^T.
+struct NsStep { double b, c, d, q; float x, A, B, next; int products; };
 
 constexpr double kMargin = 1.01;                     // on a bound, for what the products round
 constexpr double kMaxBound = 1e6;
@@ -642,7 +661,21 @@ bool plan_steps(const float* coefs, int steps, std::vector<NsStep>& plan) {
     double poly = 0, next = 0;
     step_bounds(a, b, c, s, &poly, &next);
     if (!(poly <= kMaxBound) || !(next <= kMaxBound)) return false;
-    NsStep st{float(a), float(b), float(c), scale_for(s * kMargin), scale_for(s * s * kMargin), scale_for(poly * kMargin), 0.f};
+    NsStep st{};
+    double largest = s * s;                            // of A'
+    if (c == 0.0) {
+      st = {b, 0.0, a, 0.0, 0.f, 0.f, 0.f, 0.f, 1};
+    } else if (std::fabs(b) <= 8.0 * s * s * std::fabs(c)) {
+      // the square completed: A' is at most four times as large as A, two bits of its terms
+      const double q = b / (2 * c);
+      st = {0.0, c, a - c * q * q, q, 0.f, 0.f, 0.f, 0.f, 2};
+      largest += std::fabs(q);
+    } else {
+      st = {b, c, a, 0.0, 0.f, 0.f, 0.f, 0.f, 2};
+    }
+    st.x = scale_for(s * kMargin);
+    st.A = scale_for(largest * kMargin);
+    st.B = scale_for(poly * kMargin);
     s = next * kMargin;
     st.next = scale_for(s);
     plan.push_back(st);
@@ -706,20 +739,27 @@ dp_status ns_product(Product product, NsParams& P, bool pair, cudaStream_t st) {
 
 dp_status ns_group(const dp_matrix_desc* mats, int n, dp_dtype dt, dp_dtype out_dt, const std::vector<NsStep>& plan, float eps,
                    double* partials, char* base, int* dev_status, cudaStream_t st) {
-  struct Place { NsShape s; __half *x[2], *A, *B; };
-  std::vector<Place> at;
-  at.reserve(n);
+  // operand and store maps of X (both buffers), A and B of every matrix
+  enum { kX0, kX1, kA, kB };
+  struct Place { NsShape s; __half* at[4]; CUtensorMap load[4], store[4]; };
+  std::vector<Place> places(n, Place{NsShape(mats[0]), {}, {}, {}});
+  std::vector<NsShape> shapes;
   NsInParams In;
-  memset(&In, 0, sizeof(In));
   int blocks = 0;
   for (int k = 0; k < n; ++k) {
-    Place p{NsShape(mats[k]), {nullptr, nullptr}, nullptr, nullptr};
-    p.x[0] = reinterpret_cast<__half*>(base); base += p.s.x_bytes;
-    p.x[1] = reinterpret_cast<__half*>(base); base += p.s.x_bytes;
-    p.A = reinterpret_cast<__half*>(base); base += p.s.a_bytes;
-    p.B = reinterpret_cast<__half*>(base); base += p.s.a_bytes;
-    at.push_back(p);
-    In.mat[k] = {mats[k].M, mats[k].ldm, (long long)p.s.m * p.s.ldx, p.x[0], mats[k].p, mats[k].d, p.s.ldx, p.s.transposed,
+    Place& p = places[k];
+    p.s = NsShape(mats[k]);
+    shapes.push_back(p.s);
+    for (int j = 0; j < 4; ++j) {
+      const bool x = j == kX0 || j == kX1;
+      p.at[j] = reinterpret_cast<__half*>(base);
+      base += x ? p.s.x_bytes : p.s.a_bytes;
+      const int ld = x ? p.s.ldx : p.s.lda, cols = x ? p.s.n : p.s.m;
+      dp_status r = make_tmap_bf16_3d(&p.load[j], p.at[j], ld, cols, p.s.m, 2, 64, 64);
+      if (r == DP_OK) r = make_tmap_store16_3d(&p.store[j], p.at[j], ld, cols, p.s.m, 2);
+      if (r != DP_OK) return r;
+    }
+    In.mat[k] = {mats[k].M, mats[k].ldm, (long long)p.s.m * p.s.ldx, p.at[kX0], mats[k].p, mats[k].d, p.s.ldx, p.s.transposed,
                  aligned16(mats[k].M) && mats[k].ldm * (dt == DP_F32 ? 4 : 2) % 16 == 0, blocks};
     blocks += ceil_div(mats[k].p, 64) * ceil_div(mats[k].d, 64);
   }
@@ -729,52 +769,44 @@ dp_status ns_group(const dp_matrix_desc* mats, int n, dp_dtype dt, dp_dtype out_
   ns_split_kernel<<<blocks, 256, 0, st>>>(In);
   DP_LAUNCH_OK();
 
-  std::vector<NsShape> shapes;
-  for (const Place& p : at) shapes.push_back(p.s);
   const bool pair = take_pairs(shapes);
+  NsParams P;
+  P.n_mats = n; P.out_dt = out_dt; P.dev_status = dev_status; P.wait_limit = g_wait_limit;
   const int steps = int(plan.size());
   for (int k = 0; k < steps; ++k) {
     const NsStep& S = plan[k];
     const bool last = k + 1 == steps;
-    for (int q = 0; q < 3; ++q) {
-      const Product product = Product(q);
-      NsParams P;
-      memset(&P, 0, sizeof(P));
-      int items = 0;
+    const int x = k & 1 ? kX1 : kX0, next = k & 1 ? kX0 : kX1;
+    for (const Product product : {kGram, kPoly, kApply}) {
+      if (product == kPoly && S.products == 1) continue;
+      P.total_items = 0;
       for (int i = 0; i < n; ++i) {
-        const Place& p = at[i];
-        const int m = p.s.m, nn = p.s.n;
-        const long long px = (long long)m * p.s.ldx, pa = (long long)m * p.s.lda;
+        const Place& p = places[i];
         NsMat& L = P.mat[i];
-        dp_status r;
-        L.M = m;
+        L = {};
+        L.M = p.s.m;
+        L.N = product == kApply ? p.s.n : p.s.m;
+        L.ksteps = ceil_div(product == kGram ? p.s.n : p.s.m, kBK);
         L.out_scale = 1.f;
-        L.item_begin = items;
-        items += tiles_of(product, m, nn, pair ? 256 : 128);
-        if (product == kGram) {
-          L.N = m; L.ksteps = ceil_div(nn, kBK);
-          L.dst = p.A; L.plane_dst = pa; L.ld_dst = p.s.lda;
-          r = make_tmap_bf16_3d(&P.tmP[i], p.x[k & 1], p.s.ldx, nn, m, 2, 64, 64);
-          if (r == DP_OK) P.tmQ[i] = P.tmP[i];
-        } else if (product == kPoly) {
-          L.N = m; L.ksteps = ceil_div(m, kBK);
-          L.add = p.A; L.plane_add = pa; L.ld_add = p.s.lda;
-          L.dst = p.B; L.plane_dst = pa; L.ld_dst = p.s.lda;
-          r = make_tmap_bf16_3d(&P.tmP[i], p.A, p.s.lda, m, m, 2, 64, 64);
-          if (r == DP_OK) P.tmQ[i] = P.tmP[i];
-        } else {
-          L.N = nn; L.ksteps = ceil_div(m, kBK);
-          if (last) { L.out = mats[i].out; L.ldo = mats[i].ldo; L.transposed = p.s.transposed; L.out_scale = mats[i].scale; }
-          else { L.dst = p.x[(k + 1) & 1]; L.plane_dst = px; L.ld_dst = p.s.ldx; }
-          r = make_tmap_bf16_3d(&P.tmP[i], p.B, p.s.lda, m, m, 2, 64, 64);
-          if (r == DP_OK) r = make_tmap_bf16_3d(&P.tmQ[i], p.x[k & 1], p.s.ldx, nn, m, 2, 64, 64);
+        L.item_begin = P.total_items;
+        P.total_items += tiles_of(product, p.s.m, p.s.n, pair ? 256 : 128);
+        P.tmP[i] = p.load[product == kGram ? x : product == kPoly ? kA : kB];
+        P.tmQ[i] = p.load[product == kPoly ? kA : x];
+        P.tmD[i] = p.store[product == kGram ? (S.products == 1 ? kB : kA) : product == kPoly ? kB : next];
+        if (product == kPoly && S.b != 0.0) { L.add = p.at[kA]; L.plane_add = (long long)p.s.m * p.s.lda; L.ld_add = p.s.lda; }
+        if (product == kApply && last) {
+          L.out = mats[i].out; L.ldo = mats[i].ldo; L.transposed = p.s.transposed; L.out_scale = mats[i].scale;
         }
-        if (r != DP_OK) return r;
       }
-      P.n_mats = n; P.total_items = items; P.out_dt = out_dt; P.dev_status = dev_status; P.wait_limit = g_wait_limit;
-      if (product == kGram) P.f_acc = S.A / (S.x * S.x);
-      else if (product == kPoly) { P.f_acc = S.c * S.B / (S.A * S.A); P.f_add = S.b * S.B / S.A; P.diagonal = S.a * S.B; }
-      else P.f_acc = (last ? 1.f : S.next) / (S.B * S.x);
+      const double sx = S.x, sA = S.A, sB = S.B;
+      P.f_add = P.diagonal = 0.f;
+      if (product == kGram && S.products == 1) { P.f_acc = float(S.b * sB / (sx * sx)); P.diagonal = float(S.d * sB); }
+      else if (product == kGram) { P.f_acc = float(sA / (sx * sx)); P.diagonal = float(S.q * sA); }
+      else if (product == kPoly) {
+        P.f_acc = float(S.c * sB / (sA * sA));
+        P.f_add = float(S.b * sB / sA);
+        P.diagonal = float(S.d * sB);
+      } else P.f_acc = float((last ? 1.0 : S.next) / (sB * sx));
       const dp_status r = ns_product(product, P, pair, st);
       if (r != DP_OK) return r;
     }

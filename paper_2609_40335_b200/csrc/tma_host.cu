@@ -28,11 +28,12 @@ EncodeTiledFn encode_fn() {
 // Encoded maps are kept: a tensor map is a pure function of (address, pitch, extents, box), so
 // a step that is issued call by call every iteration (no CUDA graph) pays the driver's encode
 // once per tensor instead of once per call.  Bounded: the table is cleared when it is full.
+enum MapKind { kTiles16, kPlain32, kStores16 };
 struct TmapKey {
-  const void* base; int64_t ld; int cols, rows, batch, box_cols, box_rows, f32;
+  const void* base; int64_t ld; int cols, rows, batch, box_cols, box_rows, kind;
   bool operator==(const TmapKey& o) const {
     return base == o.base && ld == o.ld && cols == o.cols && rows == o.rows && batch == o.batch &&
-           box_cols == o.box_cols && box_rows == o.box_rows && f32 == o.f32;
+           box_cols == o.box_cols && box_rows == o.box_rows && kind == o.kind;
   }
 };
 struct TmapKeyHash {
@@ -40,7 +41,7 @@ struct TmapKeyHash {
     uint64_t h = reinterpret_cast<uint64_t>(k.base) * 0x9E3779B97F4A7C15ull;
     auto mix = [&](uint64_t v) { h ^= v + 0x9E3779B97F4A7C15ull + (h << 6) + (h >> 2); };
     mix(uint64_t(k.ld)); mix(uint64_t(k.cols) << 32 | uint32_t(k.rows));
-    mix(uint64_t(k.batch) << 32 | uint32_t(k.box_cols) << 16 | uint32_t(k.box_rows) << 1 | uint32_t(k.f32));
+    mix(uint64_t(k.batch) << 32 | uint32_t(k.box_cols) << 16 | uint32_t(k.box_rows) << 2 | uint32_t(k.kind));
     return size_t(h);
   }
 };
@@ -53,8 +54,9 @@ long long g_tmap_encodes = 0;
 long long tmap_encode_count() { return g_tmap_encodes; }
 
 static dp_status make_tmap_3d(CUtensorMap* out, const void* base, int64_t ld, int cols, int rows, int batch, int box_cols,
-                              int box_rows, bool f32) {
-  const TmapKey key{base, ld, cols, rows, batch, box_cols, box_rows, f32 ? 1 : 0};
+                              int box_rows, MapKind kind) {
+  const bool f32 = kind == kPlain32;
+  const TmapKey key{base, ld, cols, rows, batch, box_cols, box_rows, kind};
   {
     std::lock_guard<std::mutex> lock(g_tmap_mutex);
     auto it = g_tmap_cache.find(key);
@@ -70,7 +72,7 @@ static dp_status make_tmap_3d(CUtensorMap* out, const void* base, int64_t ld, in
   const cuuint32_t estr[3] = {1, 1, 1};
   const CUresult r = fn(out, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims,
                         strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                        f32 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        f32 ? CU_TENSOR_MAP_SWIZZLE_NONE : kind == kStores16 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) { g_last_cuda_error = (int)r; return DP_ERR_CUDA; }
   std::lock_guard<std::mutex> lock(g_tmap_mutex);
@@ -82,12 +84,16 @@ static dp_status make_tmap_3d(CUtensorMap* out, const void* base, int64_t ld, in
 
 dp_status make_tmap_bf16_3d(CUtensorMap* out, const void* base, int64_t ld, int cols, int rows,
                             int batch, int box_cols, int box_rows) {
-  return make_tmap_3d(out, base, ld, cols, rows, batch, box_cols, box_rows, false);
+  return make_tmap_3d(out, base, ld, cols, rows, batch, box_cols, box_rows, kTiles16);
 }
 
 dp_status make_tmap_f32_3d(CUtensorMap* out, const void* base, int64_t ld, int cols, int rows,
                            int batch, int box_cols, int box_rows) {
-  return make_tmap_3d(out, base, ld, cols, rows, batch, box_cols, box_rows, true);
+  return make_tmap_3d(out, base, ld, cols, rows, batch, box_cols, box_rows, kPlain32);
+}
+
+dp_status make_tmap_store16_3d(CUtensorMap* out, const void* base, int64_t ld, int cols, int rows, int batch) {
+  return make_tmap_3d(out, base, ld, cols, rows, batch, 32, 32, kStores16);
 }
 
 }  // namespace dpg

@@ -23,4 +23,7 @@ long long tmap_encode_count();
 dp_status make_tmap_f32_3d(CUtensorMap* out, const void* base, int64_t ld, int cols, int rows,
                            int batch, int box_cols, int box_rows);
 
+// 16-bit tensors that a kernel stores to in tiles of 32 x 32, 64-byte swizzle; what lies outside is not written
+dp_status make_tmap_store16_3d(CUtensorMap* out, const void* base, int64_t ld, int cols, int rows, int batch);
+
 }  // namespace dpg

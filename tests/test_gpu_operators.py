@@ -390,7 +390,7 @@ def test_orthogonalize_many_matrices_take_pairs_and_several_launches():
 
 
 @pytest.mark.parametrize("coefs", [((1.5, -0.5, 0.0),) * 8, ((1.875, -1.25, 0.375),) * 6, ((4.0, -6.0, 3.0), (2.0, -1.5, 0.5), (1.5, -0.5, 0.0)),
-                                   ((2.0, 0.0, 0.0),), ((0.0, 0.0, 0.0),)])
+                                   ((2.0, 0.0, 0.0),), ((0.0, 0.0, 0.0),), ((1.9, -1.0, 0.02),) * 2, ((1.5, 0.0, -0.4),)])
 def test_orthogonalize_other_polynomials(coefs):
     m = tensor((96, 160), torch.float32, 4)
     o = torch.empty_like(m)
