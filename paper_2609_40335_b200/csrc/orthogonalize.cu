@@ -15,8 +15,14 @@
 // with one accumulator per tile (the diagonal of A, a sum of squares, came out 6e-6 too small at K = 3072).
 //
 // Nothing is added to a product but on the diagonal, so no epilogue reads matrices: with A' = A + q I, q = b / 2c, the square
-// completed, a I + b A + c A A = c A' A' + (a - c q^2) I is B' and X' = B' X.  (A polynomial without c needs no second product; one whose
-// c is so small that q would drown A adds b A instead.)
+// completed, B = a I + b A + c A A = c A' A' + (a - c q^2) I, and X' = B X.  A and A' differ on the diagonal: A' is a copy of the
+// diagonal's tiles.  (A polynomial whose c is so small that q would drown A adds b A instead.)
+//
+// Up to three steps go by A alone: A_1 = B_0 A_0 B_0 and so on, all of them symmetric products of m x m, and X meets B_2 B_1 B_0 once
+// at the end.  Where X is longer than high that takes fewer products with it: 36 % less work for a GPT-2 block in five steps as 3 + 2.
+// A's error grows by max |B|^2 a step (11.8 for the usual quintic) relative to its small eigenvalues, but B = a I + ... sees it next to a:
+// in 64-bit emulation with these products' errors 3 + 2 is as close as one by one for noise, for noise on a low-rank signal and for
+// singular values over four decades; five at once are not (1e-5 against 9e-7).
 //
 // A and A A are symmetric: tiles on and below the diagonal are computed and stored, and a product that needs one above it reads the
 // stored one with rows and columns exchanged (the tensor core takes either order).
@@ -51,13 +57,14 @@ constexpr int kStagingBytes = 32 * 64;                // a warp's 32 rows x 32 f
 constexpr int kRelayWarp = 2, kProducerQWarp = 3, kEpiWarp0 = 4, kEpiWarps = 16;
 constexpr int kThreads = (kEpiWarp0 + kEpiWarps) * 32;
 constexpr size_t kSmemBytes = size_t(kStages) * kStageBytes + kEpiWarps * kStagingBytes + 1024 + 512;
-constexpr int kNsMaxMats = 64;                        // matrices per launch (parameter-block limit)
+constexpr int kNsMaxMats = 48;                        // matrices per launch (parameter-block limit)
+constexpr int kMaxFused = 3;                          // steps that go by A alone
 constexpr int kNormParts = 32;                        // partial sums of a matrix's squares
 
-enum Product { kGram, kPoly, kApply };                // A' = X X^T + q I, B' = c A' A' + (a - c q^2) I, X' = B' X
+enum Product { kGram, kSym, kApply };                 // X X^T; symmetric times symmetric, commuting; symmetric times X
 
 struct NsMat {
-  const __half* add;         // kPoly: A's planes where they are added, or nullptr
+  const __half* add;         // kSym: planes that are added, or nullptr
   void* out;                 // the call's output, or nullptr: planes, through tmD
   long long plane_add, ldo;
   int ld_add;
@@ -71,9 +78,12 @@ struct __align__(64) NsParams {
   CUtensorMap tmP[kNsMaxMats];
   CUtensorMap tmQ[kNsMaxMats];
   CUtensorMap tmD[kNsMaxMats];
+  CUtensorMap tmE[kNsMaxMats];       // the copy of the diagonal's tiles: written beside tmD, or read by a square
   NsMat mat[kNsMaxMats];
   int n_mats, total_items;
   int out_dt;
+  int square;                // kSym: both operands are tmP, tmE on the diagonal's tiles
+  int copy;                  // the diagonal's tiles go to tmE too, with `diagonal` there and not in tmD
   float f_acc;               // written value = f_acc * product
   float f_add, diagonal;     //   + f_add * (high + low term of `add`), + diagonal where row = column
   int* dev_status;
@@ -115,12 +125,15 @@ __device__ __forceinline__ void split_fp16(float v, __half& hi, __half& lo) {
   lo = __float2half_rn(v - __half2float(hi));
 }
 
-__device__ __forceinline__ void split_pair(float a, float b, uint32_t& hi, uint32_t& lo) {
-  __half2 h, l;
-  split_fp16(a, h.x, l.x);
-  split_fp16(b, h.y, l.y);
-  memcpy(&hi, &h, 4);
-  memcpy(&lo, &l, 4);
+__device__ __forceinline__ uint32_t high_pair(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  uint32_t w;
+  memcpy(&w, &h, 4);
+  return w;
+}
+__device__ __forceinline__ uint32_t low_pair(float a, float b) {
+  const float2 h = __half22float2(__floats2half2_rn(a, b));
+  return high_pair(a - h.x, b - h.y);
 }
 
 // v += f * (16 consecutive values of two planes)
@@ -252,12 +265,14 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
         const uint32_t bar = full_a + 8 * stage;
         const uint32_t dst = tiles_a + stage * kStageBytes + (right ? 2 * kPartBytes : 0);
         const bool x = exchanged<kProduct, kTile>(right, right ? it.tn : it.tm, k);
+        const bool diagonal = kProduct == kSym && P.square && k * kBK / kTile == (right ? it.tn : it.tm);
+        const uint64_t from = diagonal ? reinterpret_cast<uint64_t>(&P.tmE[it.mat]) : tm;
         if (ptx::elect_one()) {
           ptx::mbar_arrive_expect_tx_a(bar, uint32_t(2 * kPartBytes));
 #pragma unroll
           for (int b = 0; b < 4; ++b) {                // two boxes of high terms, two of low ones
             const int r = r0 + (b & 1) * 64;
-            ptx::tma_load_3d_a(dst + b * kBoxBytes, tm, bar, x ? r : k * kBK, x ? k * kBK : r, b >> 1);
+            ptx::tma_load_3d_a(dst + b * kBoxBytes, from, bar, x ? r : k * kBK, x ? k * kBK : r, b >> 1);
           }
         }
         __syncwarp();
@@ -413,14 +428,10 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
         float* v = sum + 32 * g;
 #pragma unroll
         for (int e = 0; e < 32; ++e) v[e] *= f_acc;
-        if (kProduct != kApply) {
-          if (kProduct == kPoly && L.add && row < L.M) {
+        if (kProduct == kSym && L.add && row < L.M) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-              if (col + 16 * h < L.N) add_planes(L.add + size_t(row) * L.ld_add + col + 16 * h, L.plane_add, P.f_add, v + 16 * h);
-          }
-#pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] += col + e == row ? P.diagonal : 0.f;
+          for (int h = 0; h < 2; ++h)
+            if (col + 16 * h < L.N) add_planes(L.add + size_t(row) * L.ld_add + col + 16 * h, L.plane_add, P.f_add, v + 16 * h);
         }
         if (kProduct == kApply && L.out) {
           if (row < L.M) {
@@ -428,15 +439,23 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
             for (int h = 0; h < 2; ++h)
               if (col + 16 * h < L.N) store_out(L, P.out_dt, row, col + 16 * h, L.N - col - 16 * h, v + 16 * h);
           }
-        } else {
-          // 32 x 32 of each plane through shared memory to a TMA store, which leaves out what lies outside the matrix
-          uint32_t hi[16], lo[16];
+          continue;
+        }
+        // 32 x 32 of each plane through shared memory to a TMA store, which leaves out what lies outside the matrix
+        const bool on_diagonal = kProduct != kApply && it.tm == it.tn;
+        const int copies = on_diagonal && P.copy ? 2 : 1;
+#pragma unroll 1
+        for (int t = 0; t < copies; ++t) {
+          const uint64_t tm = reinterpret_cast<uint64_t>(t ? &P.tmE[it.mat] : &P.tmD[it.mat]);
+          if (on_diagonal && t == P.copy) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) split_pair(v[2 * e], v[2 * e + 1], hi[e], lo[e]);
-          const uint64_t tm = reinterpret_cast<uint64_t>(&P.tmD[it.mat]);
+            for (int e = 0; e < 32; ++e) v[e] += col + e == row ? P.diagonal : 0.f;
+          }
 #pragma unroll
           for (int plane = 0; plane < 2; ++plane) {
-            const uint32_t* w = plane ? lo : hi;
+            uint32_t w[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e] = plane ? low_pair(v[2 * e], v[2 * e + 1]) : high_pair(v[2 * e], v[2 * e + 1]);
             if (lane == 0) ptx::tma_store_wait_read();
             __syncwarp();
 #pragma unroll
@@ -606,6 +625,7 @@ struct NsShape {
   int m, n, ldx, lda;
   bool transposed;
   size_t x_bytes, a_bytes;             // of both planes
+  NsShape() = default;
   explicit NsShape(const dp_matrix_desc& D) {
     transposed = D.p > D.d;
     m = std::min(D.p, D.d);
@@ -615,7 +635,7 @@ struct NsShape {
     x_bytes = align_up(2 * size_t(m) * ldx * sizeof(__half), 256);
     a_bytes = align_up(2 * size_t(m) * lda * sizeof(__half), 256);
   }
-  size_t bytes() const { return 2 * x_bytes + 2 * a_bytes; }
+  size_t bytes() const { return 2 * x_bytes + 7 * a_bytes; }
 };
 
 // The power of two that brings values of at most `bound` below half of fp16's largest.
@@ -646,9 +666,8 @@ void step_bounds(double a, double b, double c, double s, double* poly, double* n
   }
 }
 
-// A step: scales of X, A', B' and the new X; B' = c A' A' + b A' + d I of A' = A + q I (unscaled).  products 1: B' = b A + d I comes
-// out of X X^T.
-struct NsStep { double b, c, d, q; float x, A, B, next; int products; };
+// A step: B = c A' A' + d I of A' = A + q I, or (added) c A A + b A + d I; bounds of singular values before and after, and of |B|.
+struct NsStep { double b, c, d, q, before, after, poly; bool added; };
 
 constexpr double kMargin = 1.01;                     // on a bound, for what the products round
 constexpr double kMaxBound = 1e6;
@@ -658,29 +677,34 @@ bool plan_steps(const float* coefs, int steps, std::vector<NsStep>& plan) {
   for (int k = 0; k < steps; ++k) {
     const double a = coefs[3 * k], b = coefs[3 * k + 1], c = coefs[3 * k + 2];
     if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
-    double poly = 0, next = 0;
-    step_bounds(a, b, c, s, &poly, &next);
-    if (!(poly <= kMaxBound) || !(next <= kMaxBound)) return false;
-    NsStep st{};
-    double largest = s * s;                            // of A'
-    if (c == 0.0) {
-      st = {b, 0.0, a, 0.0, 0.f, 0.f, 0.f, 0.f, 1};
-    } else if (std::fabs(b) <= 8.0 * s * s * std::fabs(c)) {
-      // the square completed: A' is at most four times as large as A, two bits of its terms
-      const double q = b / (2 * c);
-      st = {0.0, c, a - c * q * q, q, 0.f, 0.f, 0.f, 0.f, 2};
-      largest += std::fabs(q);
-    } else {
-      st = {b, c, a, 0.0, 0.f, 0.f, 0.f, 0.f, 2};
-    }
-    st.x = scale_for(s * kMargin);
-    st.A = scale_for(largest * kMargin);
-    st.B = scale_for(poly * kMargin);
-    s = next * kMargin;
-    st.next = scale_for(s);
-    plan.push_back(st);
+    NsStep S{};
+    S.before = s * kMargin;
+    step_bounds(a, b, c, s, &S.poly, &S.after);
+    if (!(S.poly <= kMaxBound) || !(S.after <= kMaxBound)) return false;
+    S.c = c;
+    // the square completed where A' stays within a few times A, two bits of its terms
+    S.added = std::fabs(b) > 8.0 * s * s * std::fabs(c);
+    if (S.added) { S.b = b; S.d = a; }
+    else if (c != 0.0) { S.q = b / (2 * c); S.d = a - c * S.q * S.q; }
+    else S.d = a;                                      // b = c = 0
+    S.poly *= kMargin;
+    S.after *= kMargin;
+    s = S.after;
+    plan.push_back(S);
   }
   return true;
+}
+
+// Steps from k on that go by A alone: while A's error has not grown too far (see the top of the file).
+int fused_steps(const std::vector<NsStep>& plan, size_t k) {
+  double growth = 1.0;
+  int n = 1;
+  while (n < kMaxFused && k + n < plan.size()) {
+    growth *= plan[k + n - 1].poly * plan[k + n - 1].poly;
+    if (growth > 150.0) break;
+    ++n;
+  }
+  return n;
 }
 
 template <Product kProduct, bool kPair>
@@ -708,49 +732,69 @@ int tiles_of(Product product, int m, int n, int tile) {
   return product == kApply ? tm * ceil_div(n, tile) : tm * (tm + 1) / 2;
 }
 
-// CTA pairs or single CTAs, the same for all products of a call, since symmetric matrices are stored by the tile: whichever
-// takes less time in whole waves, a pair's tile twice as long as a quarter of it on one CTA.
-bool take_pairs(const std::vector<NsShape>& shapes) {
-  double pair = 0, single = 0;
-  for (int q = 0; q < 3; ++q) {
-    long long big = 0, small = 0, ksteps = 0;
-    for (const NsShape& s : shapes) {
-      big += tiles_of(Product(q), s.m, s.n, 256);
-      small += tiles_of(Product(q), s.m, s.n, 128);
-      ksteps += (long long)tiles_of(Product(q), s.m, s.n, 256) * ceil_div(q == kGram ? s.n : s.m, kBK);
+// How a group of matrices runs: on CTA pairs or single CTAs, the same for all products, since symmetric matrices are stored by
+// the tile; and whether steps are fused.  Whichever takes less time in whole waves of K steps (a pair's is twice as long), a launch
+// counting three more.
+struct NsForm { bool pair, fused; };
+NsForm choose_form(const std::vector<NsShape>& shapes, const std::vector<NsStep>& plan) {
+  NsForm best{};
+  double least = INFINITY;
+  for (int form = 0; form < 4; ++form) {
+    const NsForm f{(form & 1) != 0, (form & 2) != 0};
+    const int tile = f.pair ? 256 : 128, units = f.pair ? sm_count() / 2 : sm_count();
+    double cost[3];
+    for (const Product q : {kGram, kSym, kApply}) {
+      long long tiles = 0, work = 0, longest = 0;
+      for (const NsShape& s : shapes) {
+        const long long t = tiles_of(q, s.m, s.n, tile), k = ceil_div(q == kGram ? s.n : s.m, kBK);
+        tiles += t;
+        work += t * k;
+        longest = std::max(longest, k);
+      }
+      const double waves = double((tiles + units - 1) / units);
+      cost[q] = 3.0 + (f.pair ? 2.0 : 1.0) * std::max(double(longest), waves * double(work) / double(tiles));
     }
-    const int units = sm_count();
-    const double k = double(ksteps) / double(big);
-    pair += 2 * k * double((big + units / 2 - 1) / (units / 2));
-    single += k * double((small + units - 1) / units);
+    double all = 0;
+    for (size_t k = 0; k < plan.size();) {
+      const int n = f.fused ? fused_steps(plan, k) : 1;
+      all += cost[kGram] + (1 + 4 * (n - 1)) * cost[kSym] + cost[kApply];
+      k += n;
+    }
+    if (all < least) { least = all; best = f; }
   }
-  return pair <= single;
+  return best;
 }
 
 // One product of all matrices of a group.
 dp_status ns_product(Product product, NsParams& P, bool pair, cudaStream_t st) {
   if (pair) {
-    return product == kGram ? ns_launch<kGram, true>(P, st) : product == kPoly ? ns_launch<kPoly, true>(P, st)
-                                                                                : ns_launch<kApply, true>(P, st);
+    return product == kGram ? ns_launch<kGram, true>(P, st) : product == kSym ? ns_launch<kSym, true>(P, st)
+                                                                              : ns_launch<kApply, true>(P, st);
   }
-  return product == kGram ? ns_launch<kGram, false>(P, st) : product == kPoly ? ns_launch<kPoly, false>(P, st)
-                                                                               : ns_launch<kApply, false>(P, st);
+  return product == kGram ? ns_launch<kGram, false>(P, st) : product == kSym ? ns_launch<kSym, false>(P, st)
+                                                                             : ns_launch<kApply, false>(P, st);
 }
+
+enum { kX0, kX1, kA, kDiagonal, kT, kB0, kB, kB1, kB2, kPlaces };
+struct NsPlace {
+  NsShape s;
+  __half* at[kPlaces];
+  CUtensorMap load[kPlaces], store[kPlaces];
+};
 
 dp_status ns_group(const dp_matrix_desc* mats, int n, dp_dtype dt, dp_dtype out_dt, const std::vector<NsStep>& plan, float eps,
                    double* partials, char* base, int* dev_status, cudaStream_t st) {
-  // operand and store maps of X (both buffers), A and B of every matrix
-  enum { kX0, kX1, kA, kB };
-  struct Place { NsShape s; __half* at[4]; CUtensorMap load[4], store[4]; };
-  std::vector<Place> places(n, Place{NsShape(mats[0]), {}, {}, {}});
+  // The matrices kept of each: X and the next one; A and the copy of its diagonal's tiles; B; a product on the way from one A to the
+  // next; the product of the Bs of fused steps and the next one.  The last four are as large as A.
+  std::vector<NsPlace> places(n);
   std::vector<NsShape> shapes;
   NsInParams In;
   int blocks = 0;
   for (int k = 0; k < n; ++k) {
-    Place& p = places[k];
+    NsPlace& p = places[k];
     p.s = NsShape(mats[k]);
     shapes.push_back(p.s);
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < kPlaces; ++j) {
       const bool x = j == kX0 || j == kX1;
       p.at[j] = reinterpret_cast<__half*>(base);
       base += x ? p.s.x_bytes : p.s.a_bytes;
@@ -763,53 +807,87 @@ dp_status ns_group(const dp_matrix_desc* mats, int n, dp_dtype dt, dp_dtype out_
                  aligned16(mats[k].M) && mats[k].ldm * (dt == DP_F32 ? 4 : 2) % 16 == 0, blocks};
     blocks += ceil_div(mats[k].p, 64) * ceil_div(mats[k].d, 64);
   }
-  In.n_mats = n; In.dt = dt; In.partials = partials; In.eps = eps; In.scale = plan[0].x;
+  double sx = scale_for(plan[0].before);
+  In.n_mats = n; In.dt = dt; In.partials = partials; In.eps = eps; In.scale = float(sx);
   ns_norm_kernel<<<n * kNormParts, 256, 0, st>>>(In);
   DP_LAUNCH_OK();
   ns_split_kernel<<<blocks, 256, 0, st>>>(In);
   DP_LAUNCH_OK();
 
-  const bool pair = take_pairs(shapes);
+  const NsForm form = choose_form(shapes, plan);
   NsParams P;
   P.n_mats = n; P.out_dt = out_dt; P.dev_status = dev_status; P.wait_limit = g_wait_limit;
-  const int steps = int(plan.size());
-  for (int k = 0; k < steps; ++k) {
-    const NsStep& S = plan[k];
-    const bool last = k + 1 == steps;
-    const int x = k & 1 ? kX1 : kX0, next = k & 1 ? kX0 : kX1;
-    for (const Product product : {kGram, kPoly, kApply}) {
-      if (product == kPoly && S.products == 1) continue;
-      P.total_items = 0;
-      for (int i = 0; i < n; ++i) {
-        const Place& p = places[i];
-        NsMat& L = P.mat[i];
-        L = {};
-        L.M = p.s.m;
-        L.N = product == kApply ? p.s.n : p.s.m;
-        L.ksteps = ceil_div(product == kGram ? p.s.n : p.s.m, kBK);
-        L.out_scale = 1.f;
-        L.item_begin = P.total_items;
-        P.total_items += tiles_of(product, p.s.m, p.s.n, pair ? 256 : 128);
-        P.tmP[i] = p.load[product == kGram ? x : product == kPoly ? kA : kB];
-        P.tmQ[i] = p.load[product == kPoly ? kA : x];
-        P.tmD[i] = p.store[product == kGram ? (S.products == 1 ? kB : kA) : product == kPoly ? kB : next];
-        if (product == kPoly && S.b != 0.0) { L.add = p.at[kA]; L.plane_add = (long long)p.s.m * p.s.lda; L.ld_add = p.s.lda; }
-        if (product == kApply && last) {
-          L.out = mats[i].out; L.ldo = mats[i].ldo; L.transposed = p.s.transposed; L.out_scale = mats[i].scale;
-        }
-      }
-      const double sx = S.x, sA = S.A, sB = S.B;
-      P.f_add = P.diagonal = 0.f;
-      if (product == kGram && S.products == 1) { P.f_acc = float(S.b * sB / (sx * sx)); P.diagonal = float(S.d * sB); }
-      else if (product == kGram) { P.f_acc = float(sA / (sx * sx)); P.diagonal = float(S.q * sA); }
-      else if (product == kPoly) {
-        P.f_acc = float(S.c * sB / (sA * sA));
-        P.f_add = float(S.b * sB / sA);
-        P.diagonal = float(S.d * sB);
-      } else P.f_acc = float((last ? 1.0 : S.next) / (sB * sx));
-      const dp_status r = ns_product(product, P, pair, st);
-      if (r != DP_OK) return r;
+  // D = f_acc * P Q + f_add * add [+ diagonal I: in D, or in the copy of the diagonal's tiles]
+  auto product = [&](Product kind, int left, int right, int to, double f_acc, double f_add, double diagonal, bool copy, bool last) {
+    P.total_items = 0;
+    P.f_acc = float(f_acc); P.f_add = float(f_add); P.diagonal = float(diagonal);
+    P.copy = copy;
+    P.square = kind == kSym && left == kA && right == kA && f_add == 0.0;
+    for (int i = 0; i < n; ++i) {
+      const NsPlace& p = places[i];
+      NsMat& L = P.mat[i];
+      L = {};
+      L.M = p.s.m;
+      L.N = kind == kApply ? p.s.n : p.s.m;
+      L.ksteps = ceil_div(kind == kGram ? p.s.n : p.s.m, kBK);
+      L.out_scale = 1.f;
+      L.item_begin = P.total_items;
+      P.total_items += tiles_of(kind, p.s.m, p.s.n, form.pair ? 256 : 128);
+      P.tmP[i] = p.load[left];
+      P.tmQ[i] = p.load[right];
+      P.tmD[i] = p.store[to];
+      P.tmE[i] = copy ? p.store[kDiagonal] : p.load[kDiagonal];
+      if (f_add != 0.0) { L.add = p.at[kA]; L.plane_add = (long long)p.s.m * p.s.lda; L.ld_add = p.s.lda; }
+      if (last) { L.out = mats[i].out; L.ldo = mats[i].ldo; L.transposed = p.s.transposed; L.out_scale = mats[i].scale; }
     }
+    return ns_product(kind, P, form.pair, st);
+  };
+  int x = kX0;
+  for (size_t k = 0; k < plan.size();) {
+    const int fused = form.fused ? fused_steps(plan, k) : 1;
+    int acc = kB0;                                     // the product of the group's Bs so far
+    double s_acc = 0, sA = 0, acc_bound = 1;
+    for (int f = 0; f < fused; ++f) {
+      const NsStep& S = plan[k + f];
+      const double old_sA = sA, a_bound = S.before * S.before;
+      sA = scale_for(a_bound + std::fabs(S.q));
+      const bool copy = !S.added;
+      dp_status r;
+      if (f == 0) {
+        r = product(kGram, x, x, kA, sA / (sx * sx), 0.0, S.q * sA, copy, false);
+      } else {
+        // A <- B A B; B of the step before is in kB0 (the group's first) or kB
+        const NsStep& before = plan[k + f - 1];
+        const int B = f == 1 ? kB0 : kB;
+        const double sB = scale_for(before.poly), sT = scale_for(before.before * before.after);
+        r = product(kSym, B, kA, kT, sT / (sB * old_sA), 0.0, 0.0, false, false);
+        if (r == DP_OK) r = product(kSym, kT, B, kA, sA / (sT * sB), 0.0, S.q * sA, copy, false);
+      }
+      if (r != DP_OK) return r;
+      const double sB = scale_for(S.poly);
+      const int to = f == 0 ? kB0 : kB;
+      r = product(kSym, kA, kA, to, S.c * sB / (sA * sA), S.b * sB / sA, S.d * sB, false, false);
+      if (r != DP_OK) return r;
+      acc_bound *= S.poly;
+      if (f == 0) {
+        s_acc = sB;
+      } else {
+        const int next = acc == kB1 ? kB2 : kB1;
+        const double s_next = scale_for(acc_bound);
+        r = product(kSym, kB, acc, next, s_next / (sB * s_acc), 0.0, 0.0, false, false);
+        if (r != DP_OK) return r;
+        acc = next;
+        s_acc = s_next;
+      }
+    }
+    k += fused;
+    const bool last = k == plan.size();
+    const int next = x == kX0 ? kX1 : kX0;
+    const double to = last ? 1.0 : scale_for(plan[k].before);
+    const dp_status r = product(kApply, acc, x, next, to / (s_acc * sx), 0.0, 0.0, false, last);
+    if (r != DP_OK) return r;
+    x = next;
+    sx = to;
   }
   return DP_OK;
 }
@@ -823,6 +901,20 @@ dp_status check_matrix(const dp_matrix_desc& D, bool pointers) {
   return DP_OK;
 }
 
+// The order in which matrices are taken: long sums first, so that the tiles of a last wave are the short ones.
+std::vector<int> ns_order(const dp_matrix_desc* mats, int n) {
+  std::vector<int> order(n);
+  for (int k = 0; k < n; ++k) order[k] = k;
+  std::stable_sort(order.begin(), order.end(), [&](int a, int b) {
+    return std::max(mats[a].p, mats[a].d) > std::max(mats[b].p, mats[b].d);
+  });
+  return order;
+}
+
+// Launches' groups: of equal size, every so-manieth matrix of the order, so that they are alike.  They run one after the other in the
+// same memory.
+int ns_groups(int n) { return ceil_div(n, kNsMaxMats); }
+
 }  // namespace
 
 }  // namespace dpg
@@ -833,13 +925,14 @@ extern "C" {
 
 size_t dp_orthogonalize_ws_bytes(const dp_matrix_desc* mats, int32_t n) {
   if (!mats || n <= 0) return 0;
+  for (int k = 0; k < n; ++k)
+    if (check_matrix(mats[k], false) != DP_OK) return 0;
+  const std::vector<int> order = ns_order(mats, n);
+  const int groups = ns_groups(n);
   size_t most = 0;
-  for (int g = 0; g < n; g += kNsMaxMats) {          // groups run one after the other in the same memory
+  for (int g = 0; g < groups; ++g) {
     size_t need = 0;
-    for (int k = g; k < std::min(n, g + kNsMaxMats); ++k) {
-      if (check_matrix(mats[k], false) != DP_OK) return 0;
-      need += NsShape(mats[k]).bytes();
-    }
+    for (int k = g; k < n; k += groups) need += NsShape(mats[order[k]]).bytes();
     most = std::max(most, need);
   }
   return ns_partial_bytes(n) + most;
@@ -858,10 +951,13 @@ dp_status dp_orthogonalize(const dp_matrix_desc* mats, int32_t n, dp_dtype dt, d
   if (!plan_steps(coefs, steps, plan)) return DP_ERR_INVALID_ARG;
   if (!ws || ws_bytes < dp_orthogonalize_ws_bytes(mats, n)) return DP_ERR_WORKSPACE;
   if (!aligned16(ws)) return DP_ERR_ALIGNMENT;
-  char* base = static_cast<char*>(ws) + ns_partial_bytes(n);
-  for (int g = 0; g < n; g += kNsMaxMats) {
-    const dp_status r = ns_group(mats + g, std::min(n - g, kNsMaxMats), dt, out_dt, plan, eps, static_cast<double*>(ws), base, dev_status,
-                                 (cudaStream_t)stream);
+  const std::vector<int> order = ns_order(mats, n);
+  const int groups = ns_groups(n);
+  for (int g = 0; g < groups; ++g) {
+    std::vector<dp_matrix_desc> group;
+    for (int k = g; k < n; k += groups) group.push_back(mats[order[k]]);
+    const dp_status r = ns_group(group.data(), int(group.size()), dt, out_dt, plan, eps, static_cast<double*>(ws),
+                                 static_cast<char*>(ws) + ns_partial_bytes(n), dev_status, (cudaStream_t)stream);
     if (r != DP_OK) return r;
   }
   return DP_OK;
