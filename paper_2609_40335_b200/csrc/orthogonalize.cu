@@ -14,15 +14,18 @@
 // accumulator of its own, that the epilogue adds up in registers to nearest: error of DistilGPT2's updates against 64 bits 2.2e-5
 // with one accumulator per tile (the diagonal of A, a sum of squares, came out 6e-6 too small at K = 3072).
 //
-// Nothing is added to a product but on the diagonal, so no epilogue reads matrices: with A' = A + q I, q = b / 2c, the square
-// completed, B = a I + b A + c A A = c A' A' + (a - c q^2) I, and X' = B X.  A and A' differ on the diagonal: A' is a copy of the
-// diagonal's tiles.  (A polynomial whose c is so small that q would drown A adds b A instead.)
+// Nothing is added to a product but on the diagonal, so no epilogue reads matrices: B = a I + b A + c A A = c A A' + a I with
+// A' = A + (b / c) I, which differs from A on the diagonal: A' is a copy of the diagonal's tiles.  X' = B X.  (Completing the square,
+// c A'' A'' with A'' = A + (b / 2c) I, would do too, but in a sum that one large term dominates the others are truncated at that
+// one's exponent: error of DistilGPT2's updates 2.7e-6 against 1.3e-6.  A polynomial whose c is so small that b / c would drown A adds b A
+// instead.)
 //
-// Up to three steps go by A alone: A_1 = B_0 A_0 B_0 and so on, all of them symmetric products of m x m, and X meets B_2 B_1 B_0 once
-// at the end.  Where X is longer than high that takes fewer products with it: 36 % less work for a GPT-2 block in five steps as 3 + 2.
-// A's error grows by max |B|^2 a step (11.8 for the usual quintic) relative to its small eigenvalues, but B = a I + ... sees it next to a:
-// in 64-bit emulation with these products' errors 3 + 2 is as close as one by one for noise, for noise on a low-rank signal and for
-// singular values over four decades; five at once are not (1e-5 against 9e-7).
+// Several steps go by A alone where X is longer than high: A_1 = B_0 A_0 B_0 and so on, all of them symmetric products of m x m, and X
+// meets the product of the Bs once at the end.  Five steps at once take 48 % less work for a GPT-2 block, 2 + 2 + 1 24 %.  A's error grows by
+// max |B|^2 a step (11.8 for the usual quintic) relative to its small eigenvalues, B = a I + ... sees it next to a.  Errors of the updates of
+// layers of d = 256, 768, 1000 (and the square one among them), in 1e-6: one by one 2.4 (1.4), 1.3 (1.4), 1.4 (1.4); two at once 1.9
+// (3.2), 2.8 (3.3), 3.4 (3.2); three 8.9 (5.4), 3.2 (4.3), 2.0 (3.6); five 22 (170), 13 (60), 14 (48); plain fp32 products
+// 2.5 (1.7), 2.8 (2.6), 3.3 (2.8).  So bf16 updates, whose rounding is 1.7e-3, take all steps at once, and fp32 updates two from m = 512 on.
 //
 // A and A A are symmetric: tiles on and below the diagonal are computed and stored, and a product that needs one above it reads the
 // stored one with rows and columns exchanged (the tensor core takes either order).
@@ -58,7 +61,6 @@ constexpr int kRelayWarp = 2, kProducerQWarp = 3, kEpiWarp0 = 4, kEpiWarps = 16;
 constexpr int kThreads = (kEpiWarp0 + kEpiWarps) * 32;
 constexpr size_t kSmemBytes = size_t(kStages) * kStageBytes + kEpiWarps * kStagingBytes + 1024 + 512;
 constexpr int kNsMaxMats = 48;                        // matrices per launch (parameter-block limit)
-constexpr int kMaxFused = 3;                          // steps that go by A alone
 constexpr int kNormParts = 32;                        // partial sums of a matrix's squares
 
 enum Product { kGram, kSym, kApply };                 // X X^T; symmetric times symmetric, commuting; symmetric times X
@@ -78,11 +80,11 @@ struct __align__(64) NsParams {
   CUtensorMap tmP[kNsMaxMats];
   CUtensorMap tmQ[kNsMaxMats];
   CUtensorMap tmD[kNsMaxMats];
-  CUtensorMap tmE[kNsMaxMats];       // the copy of the diagonal's tiles: written beside tmD, or read by a square
+  CUtensorMap tmE[kNsMaxMats];       // the copy of the diagonal's tiles: written beside tmD, or read
   NsMat mat[kNsMaxMats];
   int n_mats, total_items;
   int out_dt;
-  int square;                // kSym: both operands are tmP, tmE on the diagonal's tiles
+  int shifted;               // kSym: the right operand's tiles on the diagonal come from tmE
   int copy;                  // the diagonal's tiles go to tmE too, with `diagonal` there and not in tmD
   float f_acc;               // written value = f_acc * product
   float f_add, diagonal;     //   + f_add * (high + low term of `add`), + diagonal where row = column
@@ -265,7 +267,7 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
         const uint32_t bar = full_a + 8 * stage;
         const uint32_t dst = tiles_a + stage * kStageBytes + (right ? 2 * kPartBytes : 0);
         const bool x = exchanged<kProduct, kTile>(right, right ? it.tn : it.tm, k);
-        const bool diagonal = kProduct == kSym && P.square && k * kBK / kTile == (right ? it.tn : it.tm);
+        const bool diagonal = kProduct == kSym && right && P.shifted && k * kBK / kTile == it.tn;
         const uint64_t from = diagonal ? reinterpret_cast<uint64_t>(&P.tmE[it.mat]) : tm;
         if (ptx::elect_one()) {
           ptx::mbar_arrive_expect_tx_a(bar, uint32_t(2 * kPartBytes));
@@ -666,8 +668,8 @@ void step_bounds(double a, double b, double c, double s, double* poly, double* n
   }
 }
 
-// A step: B = c A' A' + d I of A' = A + q I, or (added) c A A + b A + d I; bounds of singular values before and after, and of |B|.
-struct NsStep { double b, c, d, q, before, after, poly; bool added; };
+// A step: B = c A A' + a I of A' = A + q I, or (added) c A A + b A + a I; bounds of singular values before and after, and of |B|.
+struct NsStep { double a, b, c, q, before, after, poly; bool added; };
 
 constexpr double kMargin = 1.01;                     // on a bound, for what the products round
 constexpr double kMaxBound = 1e6;
@@ -681,12 +683,12 @@ bool plan_steps(const float* coefs, int steps, std::vector<NsStep>& plan) {
     S.before = s * kMargin;
     step_bounds(a, b, c, s, &S.poly, &S.after);
     if (!(S.poly <= kMaxBound) || !(S.after <= kMaxBound)) return false;
+    S.a = a;
     S.c = c;
-    // the square completed where A' stays within a few times A, two bits of its terms
-    S.added = std::fabs(b) > 8.0 * s * s * std::fabs(c);
-    if (S.added) { S.b = b; S.d = a; }
-    else if (c != 0.0) { S.q = b / (2 * c); S.d = a - c * S.q * S.q; }
-    else S.d = a;                                      // b = c = 0
+    // A' within a few times A: two or three bits of its terms
+    S.added = std::fabs(b) > 16.0 * s * s * std::fabs(c);
+    if (S.added) S.b = b;
+    else if (c != 0.0) S.q = b / c;
     S.poly *= kMargin;
     S.after *= kMargin;
     s = S.after;
@@ -695,14 +697,13 @@ bool plan_steps(const float* coefs, int steps, std::vector<NsStep>& plan) {
   return true;
 }
 
-// Steps from k on that go by A alone: while A's error has not grown too far (see the top of the file).
-int fused_steps(const std::vector<NsStep>& plan, size_t k) {
+// Steps from k on that go by A alone, given how far A's error may grow on the way (see the top of the file).
+int fused_steps(const std::vector<NsStep>& plan, size_t k, double most) {
   double growth = 1.0;
   int n = 1;
-  while (n < kMaxFused && k + n < plan.size()) {
+  for (; k + n < plan.size(); ++n) {
     growth *= plan[k + n - 1].poly * plan[k + n - 1].poly;
-    if (growth > 150.0) break;
-    ++n;
+    if (growth > most) break;
   }
   return n;
 }
@@ -733,14 +734,17 @@ int tiles_of(Product product, int m, int n, int tile) {
 }
 
 // How a group of matrices runs: on CTA pairs or single CTAs, the same for all products, since symmetric matrices are stored by
-// the tile; and whether steps are fused.  Whichever takes less time in whole waves of K steps (a pair's is twice as long), a launch
+// the tile; and how far A's error may grow in fused steps, 1 where each is by itself.  Whichever takes less time in whole waves of K steps (a pair's is twice as long), a launch
 // counting three more.
-struct NsForm { bool pair, fused; };
-NsForm choose_form(const std::vector<NsShape>& shapes, const std::vector<NsStep>& plan) {
+struct NsForm { bool pair; double growth; };
+NsForm choose_form(const std::vector<NsShape>& shapes, const std::vector<NsStep>& plan, bool bf16_out) {
+  int least_m = shapes[0].m;
+  for (const NsShape& s : shapes) least_m = std::min(least_m, s.m);
+  const double most = bf16_out ? 3e4 : least_m >= 512 ? 13.0 : 1.0;    // five, two and one of the usual quintic's steps
   NsForm best{};
   double least = INFINITY;
   for (int form = 0; form < 4; ++form) {
-    const NsForm f{(form & 1) != 0, (form & 2) != 0};
+    const NsForm f{(form & 1) != 0, form & 2 ? most : 1.0};
     const int tile = f.pair ? 256 : 128, units = f.pair ? sm_count() / 2 : sm_count();
     double cost[3];
     for (const Product q : {kGram, kSym, kApply}) {
@@ -756,7 +760,7 @@ NsForm choose_form(const std::vector<NsShape>& shapes, const std::vector<NsStep>
     }
     double all = 0;
     for (size_t k = 0; k < plan.size();) {
-      const int n = f.fused ? fused_steps(plan, k) : 1;
+      const int n = fused_steps(plan, k, f.growth);
       all += cost[kGram] + (1 + 4 * (n - 1)) * cost[kSym] + cost[kApply];
       k += n;
     }
@@ -814,7 +818,7 @@ dp_status ns_group(const dp_matrix_desc* mats, int n, dp_dtype dt, dp_dtype out_
   ns_split_kernel<<<blocks, 256, 0, st>>>(In);
   DP_LAUNCH_OK();
 
-  const NsForm form = choose_form(shapes, plan);
+  const NsForm form = choose_form(shapes, plan, out_dt == DP_BF16);
   NsParams P;
   P.n_mats = n; P.out_dt = out_dt; P.dev_status = dev_status; P.wait_limit = g_wait_limit;
   // D = f_acc * P Q + f_add * add [+ diagonal I: in D, or in the copy of the diagonal's tiles]
@@ -822,7 +826,7 @@ dp_status ns_group(const dp_matrix_desc* mats, int n, dp_dtype dt, dp_dtype out_
     P.total_items = 0;
     P.f_acc = float(f_acc); P.f_add = float(f_add); P.diagonal = float(diagonal);
     P.copy = copy;
-    P.square = kind == kSym && left == kA && right == kA && f_add == 0.0;
+    P.shifted = kind == kSym && left == kA && right == kA && f_add == 0.0;
     for (int i = 0; i < n; ++i) {
       const NsPlace& p = places[i];
       NsMat& L = P.mat[i];
@@ -844,7 +848,7 @@ dp_status ns_group(const dp_matrix_desc* mats, int n, dp_dtype dt, dp_dtype out_
   };
   int x = kX0;
   for (size_t k = 0; k < plan.size();) {
-    const int fused = form.fused ? fused_steps(plan, k) : 1;
+    const int fused = fused_steps(plan, k, form.growth);
     int acc = kB0;                                     // the product of the group's Bs so far
     double s_acc = 0, sA = 0, acc_bound = 1;
     for (int f = 0; f < fused; ++f) {
@@ -866,7 +870,7 @@ dp_status ns_group(const dp_matrix_desc* mats, int n, dp_dtype dt, dp_dtype out_
       if (r != DP_OK) return r;
       const double sB = scale_for(S.poly);
       const int to = f == 0 ? kB0 : kB;
-      r = product(kSym, kA, kA, to, S.c * sB / (sA * sA), S.b * sB / sA, S.d * sB, false, false);
+      r = product(kSym, kA, kA, to, S.c * sB / (sA * sA), S.b * sB / sA, S.a * sB, false, false);
       if (r != DP_OK) return r;
       acc_bound *= S.poly;
       if (f == 0) {
