@@ -22,6 +22,7 @@ _LIB_PATH = os.environ.get("DP_GHOST_LIB") or os.path.join(os.path.dirname(os.pa
                                                        "libdp_ghost.so")
 _lib = None
 _native = None
+_address = {}
 
 
 class DpGhostError(RuntimeError):
@@ -163,6 +164,8 @@ def load():
     L.dp_debug_force_fma.restype = i32
     L.dp_set_reserved_sms.argtypes = [i32]
     L.dp_set_reserved_sms.restype = i32
+    for name in ("dp_layernorm", "dp_layernorm_backward", "dp_preference_loss"):     # calls that _marshal.so makes
+        _address[name] = C.cast(getattr(L, name), C.c_void_p).value
     for name in EXPORTS:
         fn = getattr(L, name)
         if fn.restype is C.c_int:          # ctypes default: the dp_status functions
@@ -660,28 +663,34 @@ def _scratch(need: int, ws: Optional[torch.Tensor], device, stream) -> torch.Ten
     return ws
 
 
-def _ln_params(tensors, p: int) -> int:
-    """The dp_dtype of a norm's gain and shift."""
+def _ln_params(tensors, p: int) -> None:
+    """Complains unless gain and shift are dense vectors of p elements of one type."""
     given = [t for t in tensors if t is not None]
     _one_dtype(given, "gain and shift")
     for t in given:
         _dense(t, (p,), t.dtype, "gain and shift")
-    return _dt(given[0]) if given else DP_F32
+
+
+def _raw(stream):
+    return None if stream is None else _stream(stream)
 
 
 def dp_layernorm(X, gain, shift, eps: float, Y=None, X_hat=None, mean=None, rstd=None, p=None, stream=None):
     """Y = X_hat*gain + shift and X_hat = (X - mean)*rstd over the last axis (its first p columns); mean, rstd: floats, one per
     row.  gain, shift: p elements, float32 or bfloat16, or None."""
-    L = load()
-    p = p if p is not None else X.shape[-1]
-    rows = math.prod(X.shape[:-1])
-    _on_one_device((X, gain, shift, Y, X_hat, mean, rstd))
-    pdt = _ln_params((gain, shift), p)
-    ldx, ldy, ldh = (_rows(t, rows, p, X.dtype, n) for t, n in ((X, "X"), (Y, "Y"), (X_hat, "X_hat")))
-    _dense(mean, (rows,), torch.float32, "mean")
-    _dense(rstd, (rows,), torch.float32, "rstd")
-    st = L.dp_layernorm(_ptr(X), ldx, _dt(X), rows, p, _ptr(gain), _ptr(shift), pdt, float(eps), _ptr(Y), ldy, _ptr(X_hat), ldh,
-                        _ptr(mean), _ptr(rstd), _stream(stream))
+    load()
+    st = _marshal().layernorm(_address["dp_layernorm"], X, gain, shift, Y, X_hat, mean, rstd, eps, p, _raw(stream))
+    if st is None:                             # one of these says what is wrong
+        _on_one_device((X, gain, shift, Y, X_hat, mean, rstd))
+        p = p if p is not None else X.shape[-1]
+        rows = math.prod(X.shape[:-1])
+        _ln_params((gain, shift), p)
+        for t, n in ((X, "X"), (Y, "Y"), (X_hat, "X_hat")):
+            _rows(t, rows, p, X.dtype, n)
+        _dense(mean, (rows,), torch.float32, "mean")
+        _dense(rstd, (rows,), torch.float32, "rstd")
+        _dt(X)
+        _complain("dp_layernorm: arguments of the wrong kind")
     _check(st, "dp_layernorm")
 
 
@@ -694,22 +703,28 @@ def dp_layernorm_backward(G, X, gain, mean, rstd, dX=None, gain_sums=None, shift
     """Backward pass of dp_layernorm for G (B,T,>=p): dX, every example's sums for gain and shift (B,p), and
     sq[i] += their squared norms.  The sums' clipped sum: dp_clip_accumulate_vectors on Vector(gain_sums.view(B, 1, p)), T = 1."""
     L = load()
-    if G.dim() != 3:
-        _complain("G: (B, T, p) is wanted")
-    B, T = G.shape[:2]
-    p = p if p is not None else G.shape[-1]
-    _on_one_device((G, X, gain, mean, rstd, dX, gain_sums, shift_sums, sq, ws))
-    pdt = _ln_params((gain,), p)
-    ldg, ldx, ldd = (_rows(t, B * T, p, G.dtype, n) for t, n in ((G, "G"), (X, "X"), (dX, "dX")))
-    for t, n in ((mean, "mean"), (rstd, "rstd")):
-        _dense(t, (B * T,), torch.float32, n)
-    for t, n in ((gain_sums, "gain_sums"), (shift_sums, "shift_sums")):
-        _dense(t, (B, p), torch.float32, n)
-    _dense(sq, (B,), torch.float32, "sq")
-    ws = _scratch(int(L.dp_layernorm_backward_ws_bytes(B, T, p)), ws, G.device, stream)
-    st = L.dp_layernorm_backward(_ptr(G), ldg, _ptr(X), ldx, _dt(G), B, T, p, _ptr(gain), pdt, _ptr(mean), _ptr(rstd), _ptr(dX), ldd,
-                                 _ptr(gain_sums), _ptr(shift_sums), _ptr(sq), _ptr(ws), ws.numel() * ws.element_size(),
-                                 _stream(stream))
+    if ws is None and isinstance(G, torch.Tensor) and G.dim() == 3:
+        need = int(L.dp_layernorm_backward_ws_bytes(G.shape[0], G.shape[1], p if p is not None else G.shape[2]))
+        if need:
+            ws = _scratch(need, None, G.device, stream)
+    st = _marshal().layernorm_backward(_address["dp_layernorm_backward"], G, X, gain, mean, rstd, dX, gain_sums, shift_sums, sq, ws, p,
+                                       _raw(stream))
+    if st is None:                             # one of these says what is wrong
+        _on_one_device((G, X, gain, mean, rstd, dX, gain_sums, shift_sums, sq, ws))
+        if G.dim() != 3:
+            _complain("G: (B, T, p) is wanted")
+        B, T = G.shape[:2]
+        p = p if p is not None else G.shape[-1]
+        _ln_params((gain,), p)
+        for t, n in ((G, "G"), (X, "X"), (dX, "dX")):
+            _rows(t, B * T, p, G.dtype, n)
+        for t, n in ((mean, "mean"), (rstd, "rstd")):
+            _dense(t, (B * T,), torch.float32, n)
+        for t, n in ((gain_sums, "gain_sums"), (shift_sums, "shift_sums")):
+            _dense(t, (B, p), torch.float32, n)
+        _dense(sq, (B,), torch.float32, "sq")
+        _dt(G)
+        _complain("dp_layernorm_backward: arguments of the wrong kind")
     _check(st, "dp_layernorm_backward")
 
 
@@ -722,21 +737,26 @@ def dp_preference_loss(logits, targets, ref_logp, beta: float, loss=None, logp=N
     """Loss of B pairs and the gradient at their logits.  logits, G (B, 2T, >=V): a pair's preferred sequence, then the
     other; targets (B, 2, T) int32, negative: the row does not count; ref_logp (B, 2) or None; loss (B,), logp (B, 2) floats."""
     L = load()
-    if logits.dim() != 3 or targets.dim() != 3 or targets.shape[1] != 2 or logits.shape[:2] != (targets.shape[0], 2 * targets.shape[2]):
-        _complain(f"logits (B, 2T, V) and targets (B, 2, T) are wanted, not {tuple(logits.shape)} and {tuple(targets.shape)}")
-    B, T = targets.shape[0], targets.shape[2]
-    V = V if V is not None else logits.shape[-1]
-    _on_one_device((logits, targets, ref_logp, loss, logp, G, ws, dev_status))
-    ldl, ldg = _rows(logits, 2 * B * T, V, logits.dtype, "logits"), _rows(G, 2 * B * T, V, logits.dtype, "G")
-    _dense(targets, (B, 2, T), torch.int32, "targets")
-    _dense(ref_logp, (B, 2), torch.float32, "ref_logp")
-    _dense(loss, (B,), torch.float32, "loss")
-    _dense(logp, (B, 2), torch.float32, "logp")
-    _dense(dev_status, (1,), torch.int32, "dev_status")
-    ws = _scratch(int(L.dp_preference_loss_ws_bytes(B, T)), ws, logits.device, stream)
-    st = L.dp_preference_loss(_ptr(logits), ldl, _dt(logits), B, T, V, _ptr(targets), _ptr(ref_logp), float(beta), float(smoothing),
-                              float(scale), _ptr(loss), _ptr(logp), _ptr(G), ldg, _ptr(ws), ws.numel() * ws.element_size(),
-                              _ptr(dev_status), _stream(stream))
+    if ws is None and isinstance(targets, torch.Tensor) and targets.dim() == 3:
+        ws = _scratch(int(L.dp_preference_loss_ws_bytes(targets.shape[0], targets.shape[2])), None, targets.device, stream)
+    st = _marshal().preference_loss(_address["dp_preference_loss"], logits, targets, ref_logp, loss, logp, G, ws, dev_status, beta,
+                                    smoothing, scale, V, _raw(stream))
+    if st is None:                             # one of these says what is wrong
+        _on_one_device((logits, targets, ref_logp, loss, logp, G, ws, dev_status))
+        if (logits.dim() != 3 or targets.dim() != 3 or targets.shape[1] != 2
+                or logits.shape[:2] != (targets.shape[0], 2 * targets.shape[2])):
+            _complain(f"logits (B, 2T, V) and targets (B, 2, T) are wanted, not {tuple(logits.shape)} and {tuple(targets.shape)}")
+        B, T = targets.shape[0], targets.shape[2]
+        V = V if V is not None else logits.shape[-1]
+        for t, n in ((logits, "logits"), (G, "G")):
+            _rows(t, 2 * B * T, V, logits.dtype, n)
+        _dense(targets, (B, 2, T), torch.int32, "targets")
+        _dense(ref_logp, (B, 2), torch.float32, "ref_logp")
+        _dense(loss, (B,), torch.float32, "loss")
+        _dense(logp, (B, 2), torch.float32, "logp")
+        _dense(dev_status, (1,), torch.int32, "dev_status")
+        _dt(logits)
+        _complain("dp_preference_loss: arguments of the wrong kind")
     _check(st, "dp_preference_loss")
 
 
@@ -744,20 +764,19 @@ NEWTON_SCHULZ = ((3.4445, -4.7750, 2.0315),) * 5     # the Muon optimiser's quin
 
 
 def _mdescs(mats, outs=None, scales=None):
-    arr = (_MatrixDesc * len(mats))()
-    for k, m in enumerate(mats):
-        if m.dim() != 2 or m.stride(1) != 1 and m.shape[1] > 1:
-            _complain(f"matrix {k}: two axes with consecutive columns are wanted, not {tuple(m.shape)} of strides {m.stride()}")
-        D = arr[k]
-        D.p, D.d = m.shape
-        D.M, D.ldm = m.data_ptr(), m.stride(0) if m.shape[0] > 1 else m.shape[1]
-        if outs is not None:
-            o = outs[k]
-            if o.shape != m.shape or o.stride(1) != 1 and o.shape[1] > 1:
-                _complain(f"output {k}: {tuple(m.shape)} with consecutive columns is wanted, not {tuple(o.shape)} of strides {o.stride()}")
-            D.out, D.ldo = o.data_ptr(), o.stride(0) if m.shape[0] > 1 else m.shape[1]
-            D.scale = 1.0 if scales is None else float(scales[k])
-    return arr
+    buf = _marshal().matrices(mats, outs, scales)
+    if buf is None:                            # one of these says what is wrong
+        _on_one_device((*mats, *(outs or ())))
+        for what, tensors in (("matrices", mats), ("outputs", outs or ())):
+            _one_dtype(tensors, what)
+            for k, m in enumerate(tensors):
+                if m.dim() != 2 or m.stride(1) != 1 and m.shape[1] > 1:
+                    _complain(f"{what}, {k}: two axes with consecutive columns are wanted, not {tuple(m.shape)} of strides {m.stride()}")
+        for k, (m, o) in enumerate(zip(mats, outs or ())):
+            if o.shape != m.shape:
+                _complain(f"output {k}: {tuple(m.shape)} is wanted, not {tuple(o.shape)}")
+        _complain("matrices, outputs and scales: arguments of the wrong kind")
+    return (_MatrixDesc * len(mats)).from_buffer(buf)
 
 
 def dp_orthogonalize_ws_bytes(mats: Sequence[torch.Tensor]) -> int:
@@ -771,15 +790,13 @@ def dp_orthogonalize(mats: Sequence[torch.Tensor], outs: Sequence[torch.Tensor],
     n = len(mats)
     if n == 0 or len(outs) != n or (scales is not None and len(scales) != n):
         _complain("as many outputs and scales as matrices are wanted, one at least")
-    _on_one_device((*mats, *outs, ws, dev_status))
-    _one_dtype(mats, "matrices")
-    _one_dtype(outs, "outputs")
+    _on_one_device((ws, dev_status))
     _dense(dev_status, (1,), torch.int32, "dev_status")
     arr = _mdescs(mats, outs, scales)
     flat = [float(c) for step in coefs for c in step]
     if len(flat) != 3 * len(coefs):
         _complain("coefs: (a, b, c) for each step")
-    ws = _scratch(int(L.dp_orthogonalize_ws_bytes(arr, n)), ws, mats[0].device, stream)
+    ws = _scratch(0 if ws is not None else int(L.dp_orthogonalize_ws_bytes(arr, n)), ws, mats[0].device, stream)
     st = L.dp_orthogonalize(arr, n, _dt(mats[0]), _dt(outs[0]), (C.c_float * len(flat))(*flat), len(coefs), float(eps), _ptr(ws),
                             ws.numel() * ws.element_size(), _ptr(dev_status), _stream(stream))
     _check(st, "dp_orthogonalize")

@@ -3,7 +3,7 @@
 // needs a dozen; with a hundred layers that was most of a step's host time (2.3 us per layer in
 // Python, 0.3 us here).  step() fills the whole record of dp_step_enqueue and makes the call: the step of
 // one small layer, bound by the host, takes 31 us call by call; it took 49 with the record filled in
-// Python.  No device work of its own, nothing is kept between calls.
+// Python.  Calls of one small kernel are made here as well.  No device work of its own, nothing is kept between calls.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -178,6 +178,12 @@ bool word_list(PyObject* arg, Py_ssize_t n, std::vector<uint32_t>& w) {
   });
 }
 
+// the interpreter lock is free while it lives
+struct Unlock {
+  PyThreadState* state = PyEval_SaveThread();
+  ~Unlock() { PyEval_RestoreThread(state); }
+};
+
 // step(address of dp_step_enqueue, layers, outs, ids of outs, vectors, vector outs, their ids,
 //      (17 tensors or None), (stream or None, side stream, 4 events, seed, V, d, tied, noise, step, wte id,
 //      wpe id, phases), C, sigma) -> status, with mode_used set on the layers; None: some argument is not
@@ -253,10 +259,7 @@ PyObject* step(PyObject*, PyObject* const* a, Py_ssize_t na) {
   const int32_t phases = int32_t(v[14]);
   dp_status st;
   {
-    struct Unlocked {
-      PyThreadState* state = PyEval_SaveThread();
-      ~Unlocked() { PyEval_RestoreThread(state); }
-    } unlocked;
+    const Unlock unlock;
     st = enqueue(&S, phases);
   }
   if (st == DP_OK && (phases & DP_STEP_NORMS))
@@ -270,6 +273,217 @@ PyObject* step(PyObject*, PyObject* const* a, Py_ssize_t na) {
   return PyLong_FromLong(long(st));
 }
 
+// ---- single calls: layernorm, layernorm_backward, preference_loss -----------------------------------------------------------
+// Each takes the address of the library's function, the binding's arguments in its order and a stream (None: the current one),
+// checks what the binding's Python checks would, and makes the call: 20 us of Python around a kernel of five otherwise.
+// -> status; None: some argument is not usable and the caller's Python checks say which.
+
+// tensors on the current device, or None
+bool here(PyObject* const* a, Py_ssize_t n, const at::Tensor** t) {
+  for (Py_ssize_t k = 0; k < n; ++k)
+    if (!device_tensor(a[k], &t[k])) return false;
+  const auto device = c10::cuda::current_device();           // (throws without a GPU)
+  for (Py_ssize_t k = 0; k < n; ++k)
+    if (t[k] && t[k]->get_device() != device) return false;
+  return true;
+}
+
+// no tensor, or a contiguous one of n elements of this type
+bool dense(const at::Tensor* t, int64_t n, at::ScalarType type) {
+  return !t || (t->scalar_type() == type && t->is_contiguous() && t->numel() == n);
+}
+
+// no tensor, or `n` rows of at least p consecutive elements of this type at one distance from each other, *ld
+bool spaced(const at::Tensor* t, int64_t n, int64_t p, at::ScalarType type, int64_t* ld) {
+  *ld = 0;
+  if (!t) return true;
+  const auto size = t->sizes(), st = t->strides();
+  const size_t d = size.size();
+  if (t->scalar_type() != type || d < 2 || size[d - 1] < p || st[d - 1] != 1) return false;
+  int64_t rows = 1, at = 1, pitch = -1;
+  for (size_t k = d - 1; k-- > 0;) {
+    rows *= size[k];
+    if (size[k] <= 1) continue;
+    if (pitch < 0) { pitch = st[k]; at = size[k]; continue; }
+    if (st[k] != pitch * at) return false;
+    at *= size[k];
+  }
+  *ld = pitch < 0 ? size[d - 1] : pitch;
+  return rows == n && *ld >= p;
+}
+
+// gain and shift: dense vectors of p elements, both of one type
+bool norm_params(const at::Tensor* const* t, int n, int64_t p, int32_t* kind) {
+  *kind = kNone;
+  for (int k = 0; k < n; ++k)
+    if (t[k] && (!same_dtype(*t[k], kind) || !dense(t[k], p, t[k]->scalar_type()))) return false;
+  if (*kind == kNone) *kind = DP_F32;
+  return true;
+}
+
+bool number(PyObject* o, double* v) {
+  *v = PyFloat_AsDouble(o);
+  if (!PyErr_Occurred()) return true;
+  PyErr_Clear();
+  return false;
+}
+bool whole(PyObject* o, int64_t otherwise, int64_t* v) {
+  *v = o == Py_None ? otherwise : PyLong_AsLongLong(o);
+  if (!PyErr_Occurred()) return true;
+  PyErr_Clear();
+  return false;
+}
+bool stream_of(PyObject* o, void** st) {
+  if (o == Py_None) { *st = c10::cuda::getCurrentCUDAStream().stream(); return true; }
+  *st = reinterpret_cast<void*>(PyLong_AsUnsignedLongLongMask(o));
+  if (!PyErr_Occurred()) return true;
+  PyErr_Clear();
+  return false;
+}
+template <typename F> F function(PyObject* o) {
+  const F f = reinterpret_cast<F>(PyLong_AsVoidPtr(o));
+  if (PyErr_Occurred()) PyErr_Clear();
+  return f;
+}
+
+// (address, X, gain, shift, Y, X_hat, mean, rstd, eps, p, stream)
+PyObject* layernorm(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  if (na != 11) { PyErr_SetString(PyExc_TypeError, "layernorm takes 11 arguments"); return nullptr; }
+  const auto call = function<decltype(&dp_layernorm)>(a[0]);
+  const at::Tensor* t[7];
+  enum { X, GAIN, SHIFT, Y, HAT, MEAN, RSTD };
+  int64_t p, ldx, ldy, ldh;
+  int32_t param;
+  double eps;
+  void* st;
+  if (!call || !here(a + 1, 7, t) || !t[X] || t[X]->dim() < 2 || dtype_of(*t[X]) == kOther) Py_RETURN_NONE;
+  const auto type = t[X]->scalar_type();
+  if (!number(a[8], &eps) || !whole(a[9], t[X]->size(-1), &p) || !stream_of(a[10], &st) || p <= 0 || p > INT32_MAX) Py_RETURN_NONE;
+  const int64_t last = t[X]->size(-1), rows = last ? t[X]->numel() / last : 0;
+  if (!norm_params(t + GAIN, 2, p, &param) || !spaced(t[X], rows, p, type, &ldx) || !spaced(t[Y], rows, p, type, &ldy) ||
+      !spaced(t[HAT], rows, p, type, &ldh) || !dense(t[MEAN], rows, at::kFloat) || !dense(t[RSTD], rows, at::kFloat))
+    Py_RETURN_NONE;
+  const void *x = pointer<const void>(t[X]), *gain = pointer<const void>(t[GAIN]), *shift = pointer<const void>(t[SHIFT]);
+  void *y = pointer<void>(t[Y]), *hat = pointer<void>(t[HAT]);
+  float *mean = pointer<float>(t[MEAN]), *rstd = pointer<float>(t[RSTD]);
+  dp_status r;
+  {
+    const Unlock unlock;
+    r = call(x, ldx, dp_dtype(dtype_of(*t[X])), rows, int32_t(p), gain, shift, dp_dtype(param), float(eps), y, ldy, hat, ldh, mean, rstd, st);
+  }
+  return PyLong_FromLong(long(r));
+}
+
+// (address, G, X, gain, mean, rstd, dX, gain_sums, shift_sums, sq, ws, p, stream)
+PyObject* layernorm_backward(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  if (na != 13) { PyErr_SetString(PyExc_TypeError, "layernorm_backward takes 13 arguments"); return nullptr; }
+  const auto call = function<decltype(&dp_layernorm_backward)>(a[0]);
+  const at::Tensor* t[10];
+  enum { G, X, GAIN, MEAN, RSTD, DX, GS, SS, SQ, WS };
+  int64_t p, ldg, ldx, ldd;
+  int32_t param;
+  void* st;
+  if (!call || !here(a + 1, 10, t) || !t[G] || t[G]->dim() != 3 || dtype_of(*t[G]) == kOther || !t[X] || !t[MEAN] || !t[RSTD]) Py_RETURN_NONE;
+  const auto type = t[G]->scalar_type();
+  const int64_t B = t[G]->size(0), T = t[G]->size(1);
+  if (!whole(a[11], t[G]->size(2), &p) || !stream_of(a[12], &st) || p <= 0 || p > INT32_MAX || B > INT32_MAX || T > INT32_MAX) Py_RETURN_NONE;
+  if (!norm_params(t + GAIN, 1, p, &param) || !spaced(t[G], B * T, p, type, &ldg) || !spaced(t[X], B * T, p, type, &ldx) ||
+      !spaced(t[DX], B * T, p, type, &ldd) || !dense(t[MEAN], B * T, at::kFloat) || !dense(t[RSTD], B * T, at::kFloat) ||
+      !dense(t[GS], B * p, at::kFloat) || !dense(t[SS], B * p, at::kFloat) || !dense(t[SQ], B, at::kFloat) ||
+      (t[WS] && !t[WS]->is_contiguous()))
+    Py_RETURN_NONE;
+  const void *g = pointer<const void>(t[G]), *x = pointer<const void>(t[X]), *gain = pointer<const void>(t[GAIN]);
+  const float *mean = pointer<const float>(t[MEAN]), *rstd = pointer<const float>(t[RSTD]);
+  void *dx = pointer<void>(t[DX]), *ws = pointer<void>(t[WS]);
+  float *gs = pointer<float>(t[GS]), *ss = pointer<float>(t[SS]), *sq = pointer<float>(t[SQ]);
+  const size_t bytes = t[WS] ? t[WS]->nbytes() : 0;
+  dp_status r;
+  {
+    const Unlock unlock;
+    r = call(g, ldg, x, ldx, dp_dtype(dtype_of(*t[G])), int32_t(B), int32_t(T), int32_t(p), gain, dp_dtype(param), mean, rstd, dx, ldd, gs,
+             ss, sq, ws, bytes, st);
+  }
+  return PyLong_FromLong(long(r));
+}
+
+// (address, logits, targets, ref_logp, loss, logp, G, ws, dev_status, beta, smoothing, scale, V, stream)
+PyObject* preference_loss(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  if (na != 14) { PyErr_SetString(PyExc_TypeError, "preference_loss takes 14 arguments"); return nullptr; }
+  const auto call = function<decltype(&dp_preference_loss)>(a[0]);
+  const at::Tensor* t[8];
+  enum { LOGITS, TARGETS, REF, LOSS, LOGP, G, WS, STATUS };
+  double beta, smoothing, scale;
+  int64_t V, ldl, ldg;
+  void* st;
+  if (!call || !here(a + 1, 8, t) || !t[LOGITS] || !t[TARGETS] || !t[WS] || t[LOGITS]->dim() != 3 || t[TARGETS]->dim() != 3 ||
+      dtype_of(*t[LOGITS]) == kOther)
+    Py_RETURN_NONE;
+  const auto type = t[LOGITS]->scalar_type();
+  const int64_t B = t[TARGETS]->size(0), T = t[TARGETS]->size(2);
+  if (t[TARGETS]->size(1) != 2 || t[LOGITS]->size(0) != B || t[LOGITS]->size(1) != 2 * T || B > INT32_MAX || T > INT32_MAX) Py_RETURN_NONE;
+  if (!number(a[9], &beta) || !number(a[10], &smoothing) || !number(a[11], &scale) || !whole(a[12], t[LOGITS]->size(2), &V) ||
+      !stream_of(a[13], &st) || V <= 0 || V > INT32_MAX)
+    Py_RETURN_NONE;
+  if (!spaced(t[LOGITS], 2 * B * T, V, type, &ldl) || !spaced(t[G], 2 * B * T, V, type, &ldg) || !dense(t[TARGETS], 2 * B * T, at::kInt) ||
+      !dense(t[REF], 2 * B, at::kFloat) || !dense(t[LOSS], B, at::kFloat) || !dense(t[LOGP], 2 * B, at::kFloat) ||
+      !dense(t[STATUS], 1, at::kInt) || !t[WS]->is_contiguous())
+    Py_RETURN_NONE;
+  const void* logits = pointer<const void>(t[LOGITS]);
+  const int32_t* targets = pointer<const int32_t>(t[TARGETS]);
+  const float* ref = pointer<const float>(t[REF]);
+  float *loss = pointer<float>(t[LOSS]), *logp = pointer<float>(t[LOGP]);
+  void *g = pointer<void>(t[G]), *ws = pointer<void>(t[WS]);
+  int32_t* status = pointer<int32_t>(t[STATUS]);
+  const size_t bytes = t[WS]->nbytes();
+  dp_status r;
+  {
+    const Unlock unlock;
+    r = call(logits, ldl, dp_dtype(dtype_of(*t[LOGITS])), int32_t(B), int32_t(T), int32_t(V), targets, ref, float(beta), float(smoothing),
+             float(scale), loss, logp, g, ldg, ws, bytes, status, st);
+  }
+  return PyLong_FromLong(long(r));
+}
+
+// matrices(sequence of matrices, sequence of outputs or None, sequence of scales or None) -> dp_matrix_desc[] as a bytearray
+PyObject* matrices(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  if (na != 3) { PyErr_SetString(PyExc_TypeError, "matrices takes 3 arguments"); return nullptr; }
+  const Py_ssize_t n = PyObject_Length(a[0]);
+  if (n < 0) { PyErr_Clear(); Py_RETURN_NONE; }
+  Ref out(PyByteArray_FromStringAndSize(nullptr, n * Py_ssize_t(sizeof(dp_matrix_desc))));
+  if (!out) return nullptr;
+  auto* rec = reinterpret_cast<dp_matrix_desc*>(PyByteArray_AS_STRING(out.get()));
+  memset(static_cast<void*>(rec), 0, size_t(n) * sizeof(dp_matrix_desc));
+  auto matrix = [&](PyObject* o, int32_t* kind, const at::Tensor** t, int64_t* ld) {
+    if (!device_tensor(o, t) || !*t || (*t)->get_device() != c10::cuda::current_device() || (*t)->dim() != 2 || !same_dtype(**t, kind)) return false;
+    const int64_t r = (*t)->size(0), c = (*t)->size(1);
+    if (r > INT32_MAX || c > INT32_MAX || (c > 1 && (*t)->stride(1) != 1)) return false;
+    *ld = r > 1 ? (*t)->stride(0) : c;
+    return true;
+  };
+  int32_t in = kNone, to = kNone;
+  const bool ok = each(a[0], n, [&](Py_ssize_t k, PyObject* o) {
+    const at::Tensor* t;
+    dp_matrix_desc& D = rec[k];
+    if (!matrix(o, &in, &t, &D.ldm)) return false;
+    D.M = pointer<const void>(t);
+    D.p = int32_t(t->size(0)); D.d = int32_t(t->size(1)); D.scale = 1.f;
+    return true;
+  }) && (a[1] == Py_None || each(a[1], n, [&](Py_ssize_t k, PyObject* o) {
+    const at::Tensor* t;
+    dp_matrix_desc& D = rec[k];
+    if (!matrix(o, &to, &t, &D.ldo) || t->size(0) != D.p || t->size(1) != D.d) return false;
+    D.out = pointer<void>(t);
+    return true;
+  })) && (a[2] == Py_None || each(a[2], n, [&](Py_ssize_t k, PyObject* o) {
+    double v;
+    if (!number(o, &v)) return false;
+    rec[k].scale = float(v);
+    return true;
+  }));
+  if (!ok) Py_RETURN_NONE;
+  return out.release();
+}
+
 // What torch throws for tensors without strides or memory of their own (nested ones, those inside vmap) becomes a
 // Python exception: past the C entry it would end the process.
 template <PyObject* (*F)(PyObject*, PyObject*)>
@@ -281,16 +495,24 @@ PyObject* guarded(PyObject* self, PyObject* arg) {
     return nullptr;
   }
 }
-PyObject* guarded_step(PyObject* self, PyObject* const* a, Py_ssize_t na) {
+template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
+PyObject* guarded_call(PyObject* self, PyObject* const* a, Py_ssize_t na) {
   try {
-    return step(self, a, na);
+    return F(self, a, na);
   } catch (const std::exception& e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
     return nullptr;
   }
 }
 
-PyMethodDef methods[] = {{"step", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded_step)), METH_FASTCALL, nullptr},
+template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
+PyCFunction fastcall() { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded_call<F>)); }
+
+PyMethodDef methods[] = {{"step", fastcall<step>(), METH_FASTCALL, nullptr},
+                         {"layernorm", fastcall<layernorm>(), METH_FASTCALL, nullptr},
+                         {"layernorm_backward", fastcall<layernorm_backward>(), METH_FASTCALL, nullptr},
+                         {"preference_loss", fastcall<preference_loss>(), METH_FASTCALL, nullptr},
+                         {"matrices", fastcall<matrices>(), METH_FASTCALL, nullptr},
                          {"linears", guarded<linears>, METH_O, nullptr},
                          {"vectors", guarded<vectors>, METH_O, nullptr},
                          {"outputs", guarded<outputs>, METH_O, nullptr},
