@@ -5,21 +5,26 @@
 //              per example i:  gain_sums_i = sum_t g_t * h_t,  shift_sums_i = sum_t g_t   (the two v_i of
 //              vector_kernels.cu, one pass over g and x together with dx),  sq[i] += |gain_sums_i|^2 + |shift_sums_i|^2
 //
-// Both read every row once and keep it in registers (as stored: a bf16 row is widened where it is used), so the
-// variance is a second pass over registers, not over memory, and is taken about the mean.  A row belongs to a group
-// of W warps with up to four chunks of eight columns per thread; a warp alone (W = 1) does up to 1024 columns.
 // Statistics, sums and everything in between are fp32; y, h and dx are rounded once.
 //
-// Backward: the rows of an example are shared out over a cluster of CTAs.  Every CTA adds up its rows' terms in
-// registers and then in shared memory; at the end each CTA adds a slice of the columns over the cluster through
-// distributed shared memory, and rank 0 adds up the squares: one launch, no workspace, a fixed order.  Where a cluster's
-// CTAs are too few for a long sequence, the partial sums go through the workspace instead (ln_sums_kernel).
+// Forward: a row belongs to a group of W warps with up to four chunks of eight columns per thread, which stay in registers (as stored:
+// a bf16 row is widened where it is used), so the variance is a second pass over registers, not over memory, and is taken about
+// the mean.  A warp alone (W = 1) does up to 1024 columns.
+//
+// Backward: a row's two means run along the row, the parameters' sums across rows.  Rows come to shared memory in tiles (bulk copies, two
+// or more tiles in flight); a warp takes a row's means, then each thread takes the same 16 bytes of columns of every row, writes
+// dx and keeps its columns' sums in registers.  (With a row's columns spread over a warp's registers, sums and all, GPT-2 medium's norm at
+// B = 64, T = 512 took 204 us: 128 registers with spills, too few rows in flight.)
+// The rows of an example are shared out over a cluster of CTAs: at the end each CTA adds a slice of the columns over the cluster through
+// distributed shared memory, and rank 0 adds up the squares: one launch, no workspace, a fixed order.  Where a cluster's CTAs are too few
+// for a long sequence, the partial sums go through the workspace instead (ln_sums_kernel).
 #include <cooperative_groups.h>
 
 #include <algorithm>
 #include <cmath>
 
 #include "dp_common.cuh"
+#include "ptx_sm100.cuh"
 
 namespace dpg {
 
@@ -142,10 +147,11 @@ struct LnForward {
   float eps;
 };
 
-template <typename T, int NV, bool kVec>
-__global__ void __launch_bounds__(512, 1)
+// four blocks of 256 threads per SM (64 registers): what hides the latency is rows in flight
+template <typename T, int NV, bool kVec, int kThreads>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads)
 ln_forward_kernel(const LnForward P) {
-  __shared__ float red[4 * 16];
+  __shared__ float red[4 * (kThreads / 32)];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int W = P.W, width = W * 32, group = warp / W, groups = (blockDim.x >> 5) / W;
   const int tid = threadIdx.x - group * width;
@@ -210,120 +216,283 @@ struct LnBackward {
   void* dX; long long lddx;
   float* gain_sums; float* shift_sums; float* sq;
   float* partials;               // [B][parts][2][p], or nullptr where the parts are a cluster
-  int T, p, W, parts;
+  int T, p, parts;
+  int bulk;                      // rows come by bulk copies: 16-byte boundaries, p % 8 == 0
+  int vec_out;                   // dX is written in 16-byte pieces
+  int rows, buffers;             // of a tile; tiles in shared memory
 };
 
-template <typename T, int NV, bool kVec>
-__global__ void __launch_bounds__(512, 1)
+// Shared memory of a block: buffers of tiles of G and X rows (16-byte pitch), which the sums take over at the end; the gain as
+// floats; per row of each buffer its mean and rstd; the warps' parts of the means of a tile's rows; barriers; squares.
+struct LnSmem {
+  int pitch;                     // bytes of a row
+  size_t tile, gain, stats, means, bars, squares, red, bytes;
+  __host__ __device__ LnSmem(int p, int es, int rows, int buffers, int warps) {
+    pitch = (p * es + 15) / 16 * 16;
+    tile = size_t(rows) * 2 * pitch;
+    size_t at = tile * buffers;
+    if (at < size_t(2) * p * sizeof(float)) at = size_t(2) * p * sizeof(float);
+    gain = at = (at + 15) / 16 * 16;
+    at += size_t(pitch / es) * sizeof(float);
+    stats = at; at += size_t(buffers) * rows * 2 * sizeof(float);
+    means = at; at += size_t(rows) * warps * 2 * sizeof(float);
+    bars = at = (at + 15) / 16 * 16;
+    at += size_t(buffers) * sizeof(uint64_t);
+    squares = at; at += 16 * sizeof(float);
+    red = at; at += 32 * sizeof(float);
+    bytes = at;
+  }
+};
+
+constexpr int kLnMaxRows = 16, kLnMaxBuffers = 4;
+
+template <typename T> struct Piece;                    // 16 bytes of a row
+template <> struct Piece<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void unpack(const uint4& q, float (&v)[4]) {
+    v[0] = __uint_as_float(q.x); v[1] = __uint_as_float(q.y); v[2] = __uint_as_float(q.z); v[3] = __uint_as_float(q.w);
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&v)[4]) {
+    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+  }
+};
+template <> struct Piece<__nv_bfloat16> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void unpack(const uint4& q, float (&v)[8]) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[2 * e] = __uint_as_float(w[e] << 16);
+      v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&v)[8]) {
+    uint4 q;
+    __nv_bfloat162 h[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+    memcpy(&q, h, 16);
+    return q;
+  }
+};
+
+// NV: pieces of 16 bytes per thread and row
+template <typename T, int NV, int kThreads>
+__global__ void __launch_bounds__(kThreads)
 ln_backward_kernel(const LnBackward P) {
-  extern __shared__ float sums[];              // [2][p], then the groups' reduction slots and 16 squares
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int W = P.W, width = W * 32, group = warp / W, groups = (blockDim.x >> 5) / W;
-  const int tid = threadIdx.x - group * width, p = P.p;
-  float* red = sums + 2 * p;
-  float* squares = red + 4 * (blockDim.x >> 5);
-  float* my_red = red + group * 4 * W;
-  int turn = 0;
+  constexpr int N = Piece<T>::N;
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int p = P.p, R = P.rows, nb = P.buffers, warps = blockDim.x >> 5;
+  const LnSmem at(p, sizeof(T), R, nb, warps);
+  float* sums = reinterpret_cast<float*>(smem);
+  float* gain = reinterpret_cast<float*>(smem + at.gain);
+  float* stats = reinterpret_cast<float*>(smem + at.stats);
+  float* means = reinterpret_cast<float*>(smem + at.means);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + at.bars);
+  float* squares = reinterpret_cast<float*>(smem + at.squares);
+  float* red = reinterpret_cast<float*>(smem + at.red);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int example = blockIdx.x / P.parts, part = blockIdx.x - example * P.parts;
   const int r0 = int((long long)P.T * part / P.parts), r1 = int((long long)P.T * (part + 1) / P.parts);
   const long long base = (long long)example * P.T;
+  const int tiles = (r1 - r0 + R - 1) / R, pieces = at.pitch / 16;
   const float inv_p = 1.f / float(p);
-  float gs[NV][8], ss[NV][8];
-#pragma unroll
-  for (int j = 0; j < NV; ++j)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) gs[j][e] = ss[j][e] = 0.f;
-  for (int r = r0 + group; r < r1; r += groups) {
-    const long long row = base + r;
-    LnChunk<T, kVec> gin[NV], xin[NV];
-    const T* g = static_cast<const T*>(P.G) + row * P.ldg;
-    const T* x = static_cast<const T*>(P.X) + row * P.ldx;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) { gin[j].load(g, j, tid, width, p); xin[j].load(x, j, tid, width, p); }
-    const float mean = P.mean[row], rstd = P.rstd[row];
-    float s[2] = {0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      float gv[8], h[8], a[8];
-      gin[j].raw.unpack(gv);
-      xin[j].raw.unpack(h);
-      ln_param<kVec>(P.gain, P.param_dt, 1.f, j, tid, width, p, a);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const bool in = kVec ? true : ln_col<kVec>(j, e, tid, width) < p;
-        h[e] = (h[e] - mean) * rstd;
-        const float u = gv[e] * a[e];                     // 0 past the row's end: its g is
-        s[0] += u;
-        if (in) {
-          s[1] = fmaf(u, h[e], s[1]);
-          gs[j][e] = fmaf(gv[e], h[e], gs[j][e]);
-          ss[j][e] += gv[e];
+
+  // tile k to its buffer: a bulk copy per row of G and of X, or element by element with zeros behind the row
+  auto fill = [&](int k) {
+    uint8_t* to = smem + size_t(k % nb) * at.tile;
+    const int first = r0 + k * R, n = min(R, r1 - first);
+    if (P.bulk) {
+      if (warp == 0) {
+        uint64_t* bar = full + k % nb;
+        const uint32_t bytes = uint32_t(p) * sizeof(T);
+        if (lane == 0) ptx::mbar_arrive_expect_tx(bar, 2 * uint32_t(n) * bytes);
+        __syncwarp();
+        if (lane < n) {
+          const long long row = base + first + lane;
+          ptx::bulk_load(to + size_t(2 * lane) * at.pitch, static_cast<const T*>(P.G) + row * P.ldg, bytes, bar);
+          ptx::bulk_load(to + size_t(2 * lane + 1) * at.pitch, static_cast<const T*>(P.X) + row * P.ldx, bytes, bar);
+        }
+      }
+    } else {
+      const int cols = at.pitch / int(sizeof(T));
+      for (int r = 0; r < n; ++r) {
+        const long long row = base + first + r;
+        const T* g = static_cast<const T*>(P.G) + row * P.ldg;
+        const T* x = static_cast<const T*>(P.X) + row * P.ldx;
+        T* tg = reinterpret_cast<T*>(to + size_t(2 * r) * at.pitch);
+        T* tx = reinterpret_cast<T*>(to + size_t(2 * r + 1) * at.pitch);
+        for (int c = tid; c < cols; c += blockDim.x) {
+          tg[c] = c < p ? g[c] : from_f32<T>(0.f);
+          tx[c] = c < p ? x[c] : from_f32<T>(0.f);
         }
       }
     }
+    if (tid < 2 * n)
+      stats[(k % nb) * 2 * R + tid] = (tid & 1 ? P.rstd : P.mean)[base + first + (tid >> 1)];
+  };
+
+  if (tid == 0 && P.bulk) {
+    for (int k = 0; k < nb; ++k) ptx::mbar_init(full + k, 1);
+    ptx::fence_mbar_init();
+  }
+  for (int c = tid; c < pieces * N; c += blockDim.x)
+    gain[c] = !P.gain ? 1.f : c >= p ? 0.f : P.param_dt == DP_F32 ? static_cast<const float*>(P.gain)[c]
+                                                                 : __bfloat162float(static_cast<const __nv_bfloat16*>(P.gain)[c]);
+  __syncthreads();
+  for (int k = 0; k < min(nb, tiles); ++k) fill(k);
+
+  // this thread's rows of a tile and its pieces of a row
+  const int groups = NV == 1 ? max(1, int(blockDim.x) / pieces) : 1;
+  const int group = NV == 1 ? tid / pieces : 0;
+  const int piece0 = NV == 1 ? tid - group * pieces : tid;
+  float gs[NV][N], ss[NV][N], a[NV][N];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int piece = piece0 + j * blockDim.x;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      gs[j][e] = ss[j][e] = 0.f;
+      a[j][e] = piece < pieces ? gain[piece * N + e] : 0.f;
+    }
+  }
+  // warps per row for the means, and how many rows they take at once
+  const int per_row = max(1, warps / R), at_once = warps / per_row;
+
+  for (int k = 0; k < tiles; ++k) {
+    const uint8_t* tile = smem + size_t(k % nb) * at.tile;
+    const float* st = stats + (k % nb) * 2 * R;
+    const int first = r0 + k * R, n = min(R, r1 - first);
+    if (!P.bulk) __syncthreads();                      // filled by every thread (and the statistics with it)
+    else {
+      if (k < nb || nb == 1) __syncthreads();          // the statistics; with more buffers later tiles' are a sync older
+      const long long t0 = clock64();
+      while (!ptx::mbar_try_wait(full + k % nb, (k / nb) & 1))
+        if (clock64() - t0 > ptx::kDefaultWaitLimit) break;      // copies of this block's own: they end
+    }
     if (P.dX) {
-      group_sum<2>(s, W, warp - group * W, lane, 1 + group, my_red, turn);
-      const float m1 = s[0] * inv_p, m2 = s[1] * inv_p;
+      for (int r = warp / per_row; r < n && warp < per_row * at_once; r += at_once) {
+        const uint4* g = reinterpret_cast<const uint4*>(tile + size_t(2 * r) * at.pitch);
+        const uint4* x = reinterpret_cast<const uint4*>(tile + size_t(2 * r + 1) * at.pitch);
+        const float mean = st[2 * r], rstd = st[2 * r + 1];
+        float s1 = 0.f, s2 = 0.f;
+        for (int c = (warp % per_row) * 32 + lane; c < pieces; c += per_row * 32) {
+          float gv[N], h[N];
+          Piece<T>::unpack(g[c], gv);
+          Piece<T>::unpack(x[c], h);
+          const float4* w = reinterpret_cast<const float4*>(gain + c * N);
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        float gv[8], h[8], a[8], d[8];
-        gin[j].raw.unpack(gv);
-        xin[j].raw.unpack(h);
-        ln_param<kVec>(P.gain, P.param_dt, 1.f, j, tid, width, p, a);
+          for (int q = 0; q < N / 4; ++q) {
+            const float4 b = w[q];
+            const float bb[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d[e] = (fmaf(gv[e], a[e], -m1) - (h[e] - mean) * rstd * m2) * rstd;
-        ln_store<T, kVec>(static_cast<T*>(P.dX) + row * P.lddx, d, j, tid, width, p);
+            for (int e = 0; e < 4; ++e) {
+              const float u = gv[4 * q + e] * bb[e];   // 0 behind the row
+              s1 += u;
+              s2 = fmaf(u, (h[4 * q + e] - mean) * rstd, s2);
+            }
+          }
+        }
+        s1 = warp_sum(s1);
+        s2 = warp_sum(s2);
+        if (lane == 0) {
+          means[(r * warps + warp % per_row) * 2] = s1;
+          means[(r * warps + warp % per_row) * 2 + 1] = s2;
+        }
+      }
+      __syncthreads();
+    }
+    if (group < groups) {
+      for (int r = group; r < n; r += groups) {
+        const uint4* g = reinterpret_cast<const uint4*>(tile + size_t(2 * r) * at.pitch);
+        const uint4* x = reinterpret_cast<const uint4*>(tile + size_t(2 * r + 1) * at.pitch);
+        const float mean = st[2 * r], rstd = st[2 * r + 1];
+        float m1 = 0.f, m2 = 0.f;
+        if (P.dX) {
+          for (int w = 0; w < per_row; ++w) { m1 += means[(r * warps + w) * 2]; m2 += means[(r * warps + w) * 2 + 1]; }
+          m1 *= inv_p;
+          m2 *= inv_p;
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          const int piece = piece0 + j * blockDim.x;
+          if (NV > 1 && piece >= pieces) break;
+          float gv[N], h[N], d[N];
+          Piece<T>::unpack(g[piece], gv);
+          Piece<T>::unpack(x[piece], h);
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            h[e] = (h[e] - mean) * rstd;
+            gs[j][e] = fmaf(gv[e], h[e], gs[j][e]);
+            ss[j][e] += gv[e];
+            d[e] = (fmaf(gv[e], a[j][e], -m1) - h[e] * m2) * rstd;
+          }
+          if (P.dX) {
+            T* out = static_cast<T*>(P.dX) + (base + first + r) * P.lddx + piece * N;
+            if (P.vec_out) *reinterpret_cast<uint4*>(out) = Piece<T>::pack(d);
+            else {
+#pragma unroll
+              for (int e = 0; e < N; ++e) if (piece * N + e < p) out[e] = from_f32<T>(d[e]);
+            }
+          }
+        }
       }
     }
+    __syncthreads();                                   // the buffer has been read
+    if (k + nb < tiles) fill(k + nb);
   }
   if (!P.gain_sums && !P.shift_sums && !P.sq) return;          // the same for every CTA
   // this CTA's sums, its groups one after the other
-  for (int k = 0; k < groups; ++k) {
-    if (group == k) {
+  if (tiles == 0) {
+    for (int c = tid; c < 2 * p; c += blockDim.x) sums[c] = 0.f;
+  }
+  for (int q = 0; q < groups && tiles; ++q) {
+    if (group == q) {
 #pragma unroll
       for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int c = ln_col<kVec>(j, e, tid, width);
+        for (int e = 0; e < N; ++e) {
+          const int c = (piece0 + j * int(blockDim.x)) * N + e;
           if (c < p) {
-            sums[c] = (k ? sums[c] : 0.f) + gs[j][e];
-            sums[p + c] = (k ? sums[p + c] : 0.f) + ss[j][e];
+            sums[c] = (q ? sums[c] : 0.f) + gs[j][e];
+            sums[p + c] = (q ? sums[p + c] : 0.f) + ss[j][e];
           }
         }
     }
     __syncthreads();
   }
+  __syncthreads();
   if (P.partials) {
     float* out = P.partials + (long long)blockIdx.x * 2 * p;
-    for (int c = threadIdx.x; c < 2 * p; c += blockDim.x) out[c] = sums[c];
+    for (int c = tid; c < 2 * p; c += blockDim.x) out[c] = sums[c];
     return;
   }
   cg::cluster_group cluster = cg::this_cluster();
   if (P.parts > 1) cluster.sync();
   const int c0 = int((long long)p * part / P.parts), c1 = int((long long)p * (part + 1) / P.parts);
   float sq = 0.f;
-  for (int c = c0 + threadIdx.x; c < c1; c += blockDim.x) {
-    float a = 0.f, b = 0.f;
+  for (int c = c0 + tid; c < c1; c += blockDim.x) {
+    float u = 0.f, v = 0.f;
     if (P.parts > 1) {
-      for (int k = 0; k < P.parts; ++k) {
-        const float* other = cluster.map_shared_rank(sums, k);
-        a += other[c];
-        b += other[p + c];
+      for (int q = 0; q < P.parts; ++q) {
+        const float* other = cluster.map_shared_rank(sums, q);
+        u += other[c];
+        v += other[p + c];
       }
     } else {
-      a = sums[c];
-      b = sums[p + c];
+      u = sums[c];
+      v = sums[p + c];
     }
-    if (P.gain_sums) P.gain_sums[(long long)example * p + c] = a;
-    if (P.shift_sums) P.shift_sums[(long long)example * p + c] = b;
-    sq = fmaf(a, a, fmaf(b, b, sq));
+    if (P.gain_sums) P.gain_sums[(long long)example * p + c] = u;
+    if (P.shift_sums) P.shift_sums[(long long)example * p + c] = v;
+    sq = fmaf(u, u, fmaf(v, v, sq));
   }
   sq = block_sum(sq, red);
-  if (threadIdx.x == 0) *(P.parts > 1 ? cluster.map_shared_rank(squares + part, 0) : squares) = sq;
+  if (tid == 0) *(P.parts > 1 ? cluster.map_shared_rank(squares + part, 0) : squares) = sq;
   if (P.parts > 1) cluster.sync();                             // no CTA leaves while its sums are read
-  if (P.sq && part == 0 && threadIdx.x == 0) {
+  if (P.sq && part == 0 && tid == 0) {
     float all = 0.f;
-    for (int k = 0; k < P.parts; ++k) all += squares[k];
+    for (int q = 0; q < P.parts; ++q) all += squares[q];
     P.sq[example] += all;
   }
 }
@@ -348,10 +517,11 @@ ln_sums_kernel(const float* partials, int parts, int p, float* gain_sums, float*
   if (threadIdx.x == 0) squares[example * gridDim.x + blockIdx.x] = sq;
 }
 
-// warps per row: as few as leave a thread four chunks, two where its columns are apart (a predicate each)
+// warps per row of the forward pass: as few as leave a thread three chunks (four spill), two where its columns are apart (a
+// predicate each)
 int ln_warps(int p, bool vec) {
   int W = 1;
-  while (W < 16 && W * 32 * (vec ? 4 : 2) * 8 < p) W *= 2;
+  while (W < 16 && W * 32 * (vec ? 3 : 2) * 8 < p) W *= 2;
   return W;
 }
 
@@ -359,33 +529,36 @@ bool ln_vec(const void* q, long long ld, int es) { return !q || (aligned16(q) &&
 
 constexpr int kLnMaxParts = 16;            // CTAs of a cluster
 
-// Parts an example's rows are cut into, and whether they are a cluster (else the sums go through the workspace).
+// Parts an example's rows are cut into, and whether they are a cluster (else the sums go through the workspace): about three
+// CTAs per SM, eight rows each at least.
 struct LnParts { int parts; bool cluster; };
-LnParts ln_parts(int B, int T, int p) {
-  const int groups = std::max(1, 8 / ln_warps(p, true));
-  const int wanted = ceil_div(2 * sm_count(), B);              // two CTAs per SM
-  const int most = ceil_div(T, groups);                        // a row per group at least
-  int parts = 1;
-  while (parts < wanted && parts < most && parts < kLnMaxParts) parts *= 2;
-  if (parts == kLnMaxParts && wanted >= 2 * kLnMaxParts && T >= 64 * groups * kLnMaxParts)
-    return {std::min(wanted, T / (32 * groups)), false};
-  return {parts, true};
+LnParts ln_parts(int B, int T) {
+  const int wanted = std::max(1, 3 * sm_count() / B);
+  const int most = ceil_div(T, 8);
+  if (wanted > 2 * kLnMaxParts && T >= 1024 * kLnMaxParts) return {std::min(wanted, T / 512), false};
+  return {std::max(1, std::min(std::min(wanted, most), kLnMaxParts)), true};
 }
 
-template <typename T, int NV, bool kVec>
-dp_status ln_back_launch(LnBackward& P, int B, bool cluster, cudaStream_t st) {
-  auto* kernel = ln_backward_kernel<T, NV, kVec>;
-  const int threads = std::max(kLnThreads, P.W * 32);
-  const size_t smem = (size_t(2) * P.p + 4 * (threads / 32) + kLnMaxParts) * sizeof(float);
+template <typename T, int NV, int kThreads>
+dp_status ln_back_launch(LnBackward& P, int B, int threads, bool cluster, cudaStream_t st) {
+  auto* kernel = ln_backward_kernel<T, NV, kThreads>;
+  // rows per tile and tiles: a third of an SM's shared memory where three CTAs share it, all of it for a CTA alone
+  const size_t most = (long long)B * P.parts > sm_count() ? 72 * 1024 : 200 * 1024;
+  const int pitch = (P.p * int(sizeof(T)) + 15) / 16 * 16;
+  P.rows = std::max(1, std::min(kLnMaxRows, int(24 * 1024 / (2 * pitch))));
+  P.rows = std::min(P.rows, std::max(1, ceil_div(P.T, P.parts)));
+  P.buffers = P.bulk ? kLnMaxBuffers : 1;
+  while (P.buffers > 1 && LnSmem(P.p, sizeof(T), P.rows, P.buffers, threads / 32).bytes > most) --P.buffers;
+  if (P.buffers == 1 && P.bulk && LnSmem(P.p, sizeof(T), P.rows, 2, threads / 32).bytes <= 225 * 1024) P.buffers = 2;
+  const LnSmem smem(P.p, sizeof(T), P.rows, P.buffers, threads / 32);
   if (first_use_on_this_device((const void*)kernel)) {
-    const size_t most = (size_t(2) * kLnMaxCols + 4 * 16 + kLnMaxParts) * sizeof(float);
-    DP_CUDA_OK(allow_shared(kernel, most));
+    DP_CUDA_OK(allow_shared(kernel, 227 * 1024));
     DP_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(B) * unsigned(P.parts));
   cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = smem.bytes;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -397,21 +570,33 @@ dp_status ln_back_launch(LnBackward& P, int B, bool cluster, cudaStream_t st) {
   return DP_OK;
 }
 
-template <typename T, bool kVec>
-dp_status ln_back_nv(LnBackward& P, int B, bool cluster, cudaStream_t st) {
-  switch (ceil_div(P.p, 8 * 32 * P.W)) {
-    case 1: return ln_back_launch<T, 1, kVec>(P, B, cluster, st);
-    case 2: return ln_back_launch<T, 2, kVec>(P, B, cluster, st);
-    case 3: return ln_back_launch<T, 3, kVec>(P, B, cluster, st);
-    default: return ln_back_launch<T, 4, kVec>(P, B, cluster, st);
+// Threads: as many whole rows of pieces as fill most of a block, 256 or so; wide rows take 512 threads and several pieces each.
+template <typename T>
+dp_status ln_back(LnBackward& P, int B, bool cluster, cudaStream_t st) {
+  const int pieces = ceil_div(P.p * int(sizeof(T)), 16);
+  if (pieces <= 512) {
+    int best = 0, used = 0;
+    for (int threads = 128; threads <= 512; threads += 32) {
+      if (threads < pieces) continue;
+      const int score = threads / pieces * pieces * 1024 / threads - std::abs(threads - 256) / 4;
+      if (!best || score > used) { best = threads; used = score; }
+    }
+    return best <= 256 ? ln_back_launch<T, 1, 256>(P, B, best, cluster, st) : ln_back_launch<T, 1, 512>(P, B, best, cluster, st);
+  }
+  switch (ceil_div(pieces, 512)) {
+    case 2: return ln_back_launch<T, 2, 512>(P, B, 512, cluster, st);
+    case 3: return ln_back_launch<T, 3, 512>(P, B, 512, cluster, st);
+    case 4: return ln_back_launch<T, 4, 512>(P, B, 512, cluster, st);
+    default: return ln_back_launch<T, 8, 512>(P, B, 512, cluster, st);
   }
 }
 
 template <typename T, int NV, bool kVec>
 dp_status ln_fwd_launch(const LnForward& P, cudaStream_t st) {
   const int threads = std::max(kLnThreads, P.W * 32), groups = threads / 32 / P.W;
-  const long long blocks = (P.rows + groups - 1) / groups;
-  ln_forward_kernel<T, NV, kVec><<<unsigned(std::min<long long>(blocks, 1 << 20)), threads, 0, st>>>(P);
+  const unsigned blocks = unsigned(std::min<long long>((P.rows + groups - 1) / groups, 1 << 20));
+  if (threads == 512) ln_forward_kernel<T, NV, kVec, 512><<<blocks, threads, 0, st>>>(P);
+  else ln_forward_kernel<T, NV, kVec, 256><<<blocks, threads, 0, st>>>(P);
   DP_LAUNCH_OK();
   return DP_OK;
 }
@@ -460,7 +645,7 @@ dp_status dp_layernorm(const void* X, int64_t ldx, dp_dtype dt, int64_t rows, in
 
 size_t dp_layernorm_backward_ws_bytes(int32_t B, int32_t T, int32_t p) {
   if (B <= 0 || T <= 0 || p <= 0 || p > kLnMaxCols) return 0;
-  const LnParts parts = ln_parts(B, T, p);
+  const LnParts parts = ln_parts(B, T);
   if (parts.cluster) return 0;
   return ln_partial_bytes(parts, B, p) + align_up(size_t(B) * ceil_div(p, 128) * sizeof(float), 256);
 }
@@ -476,7 +661,7 @@ dp_status dp_layernorm_backward(const void* G, int64_t ldg, const void* X, int64
   const int es = dt == DP_F32 ? 4 : 2, ps = param_dt == DP_F32 ? 4 : 2;
   if (!on_boundary(es, G, X, dX) || !on_boundary(ps, gain) || !on_boundary(4, mean, rstd, gain_sums, shift_sums, sq)) return DP_ERR_ALIGNMENT;
   if (p > kLnMaxCols) return DP_ERR_UNSUPPORTED;
-  const LnParts parts = ln_parts(B, T, p);
+  const LnParts parts = ln_parts(B, T);
   if ((long long)B * parts.parts > 0x7fffffffLL) return DP_ERR_UNSUPPORTED;
   float* partials = nullptr;
   float* squares = nullptr;
@@ -486,14 +671,14 @@ dp_status dp_layernorm_backward(const void* G, int64_t ldg, const void* X, int64
     partials = static_cast<float*>(ws);
     squares = reinterpret_cast<float*>(static_cast<char*>(ws) + ln_partial_bytes(parts, B, p));
   }
-  const bool vec = p % 8 == 0 && ln_vec(G, ldg, es) && ln_vec(X, ldx, es) && ln_vec(dX, lddx, es) &&
-                   ln_vec(gain, p, ps);
-  LnBackward P{G, ldg, X, ldx, gain, param_dt, mean, rstd, dX, lddx, gain_sums, shift_sums, sq, partials, T, p, ln_warps(p, vec), parts.parts};
+  LnBackward P{};
+  P.G = G; P.ldg = ldg; P.X = X; P.ldx = ldx; P.gain = gain; P.param_dt = param_dt; P.mean = mean; P.rstd = rstd; P.dX = dX; P.lddx = lddx;
+  P.gain_sums = gain_sums; P.shift_sums = shift_sums; P.sq = sq; P.partials = partials;
+  P.T = T; P.p = p; P.parts = parts.parts;
+  P.bulk = p % 8 == 0 && ln_vec(G, ldg, es) && ln_vec(X, ldx, es);
+  P.vec_out = p % 8 == 0 && ln_vec(dX, lddx, es);
   const cudaStream_t st = (cudaStream_t)stream;
-  const bool cluster = parts.cluster;
-  dp_status r;
-  if (dt == DP_F32) r = vec ? ln_back_nv<float, true>(P, B, cluster, st) : ln_back_nv<float, false>(P, B, cluster, st);
-  else r = vec ? ln_back_nv<__nv_bfloat16, true>(P, B, cluster, st) : ln_back_nv<__nv_bfloat16, false>(P, B, cluster, st);
+  const dp_status r = dt == DP_F32 ? ln_back<float>(P, B, parts.cluster, st) : ln_back<__nv_bfloat16>(P, B, parts.cluster, st);
   if (r != DP_OK || !partials) return r;
   const int slabs = ceil_div(p, 128);
   ln_sums_kernel<<<dim3(slabs, B), 128, 0, st>>>(partials, parts.parts, p, gain_sums, shift_sums, squares);
