@@ -361,7 +361,8 @@ dp_status dp_layernorm(const void* X, int64_t ldx, dp_dtype dt, int64_t rows, in
  * unless few examples have long sequences). */
 dp_status dp_layernorm_backward(const void* G, int64_t ldg, const void* X, int64_t ldx, dp_dtype dt, int32_t B, int32_t T, int32_t p,
                                 const void* gain, dp_dtype param_dt, const float* mean, const float* rstd, void* dX, int64_t lddx,
-                                float* gain_sums, float* shift_sums, float* sq, void* ws, size_t ws_bytes, void* stream);
+                                float* gain_sums, float* shift_sums, float* sq, void* ws, size_t ws_bytes, int32_t* dev_status,
+                                void* stream);
 size_t dp_layernorm_backward_ws_bytes(int32_t B, int32_t T, int32_t p);
 
 /* ---- preference loss of paired sequences on the LM head's logits, with the head's G ----

@@ -137,7 +137,7 @@ def load():
     L.dp_step_enqueue.argtypes = [vp, i32]
     L.dp_layernorm.argtypes = [vp, i64, i32, i64, i32, vp, vp, i32, f32, vp, i64, vp, i64, vp, vp, vp]
     L.dp_layernorm_backward.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32, vp, i32, vp, vp, vp, i64, vp, vp, vp,
-                                        vp, sz, vp]
+                                        vp, sz, vp, vp]
     L.dp_layernorm_backward_ws_bytes.argtypes = [i32, i32, i32]
     L.dp_layernorm_backward_ws_bytes.restype = sz
     L.dp_preference_loss.argtypes = [vp, i64, i32, i32, i32, i32, vp, vp, f32, f32, f32, vp, vp, vp, i64, vp, sz, vp, vp]
@@ -699,7 +699,7 @@ def dp_layernorm_backward_ws_bytes(B: int, T: int, p: int) -> int:
 
 
 def dp_layernorm_backward(G, X, gain, mean, rstd, dX=None, gain_sums=None, shift_sums=None, sq=None, p=None, ws=None,
-                          stream=None):
+                          dev_status=None, stream=None):
     """Backward pass of dp_layernorm for G (B,T,>=p): dX, every example's sums for gain and shift (B,p), and
     sq[i] += their squared norms.  The sums' clipped sum: dp_clip_accumulate_vectors on Vector(gain_sums.view(B, 1, p)), T = 1."""
     L = load()
@@ -707,10 +707,10 @@ def dp_layernorm_backward(G, X, gain, mean, rstd, dX=None, gain_sums=None, shift
         need = int(L.dp_layernorm_backward_ws_bytes(G.shape[0], G.shape[1], p if p is not None else G.shape[2]))
         if need:
             ws = _scratch(need, None, G.device, stream)
-    st = _marshal().layernorm_backward(_address["dp_layernorm_backward"], G, X, gain, mean, rstd, dX, gain_sums, shift_sums, sq, ws, p,
-                                       _raw(stream))
+    st = _marshal().layernorm_backward(_address["dp_layernorm_backward"], G, X, gain, mean, rstd, dX, gain_sums, shift_sums, sq, ws,
+                                       dev_status, p, _raw(stream))
     if st is None:                             # one of these says what is wrong
-        _on_one_device((G, X, gain, mean, rstd, dX, gain_sums, shift_sums, sq, ws))
+        _on_one_device((G, X, gain, mean, rstd, dX, gain_sums, shift_sums, sq, ws, dev_status))
         if G.dim() != 3:
             _complain("G: (B, T, p) is wanted")
         B, T = G.shape[:2]
@@ -723,6 +723,7 @@ def dp_layernorm_backward(G, X, gain, mean, rstd, dX=None, gain_sums=None, shift
         for t, n in ((gain_sums, "gain_sums"), (shift_sums, "shift_sums")):
             _dense(t, (B, p), torch.float32, n)
         _dense(sq, (B,), torch.float32, "sq")
+        _dense(dev_status, (1,), torch.int32, "dev_status")
         _dt(G)
         _complain("dp_layernorm_backward: arguments of the wrong kind")
     _check(st, "dp_layernorm_backward")

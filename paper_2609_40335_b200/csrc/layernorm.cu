@@ -5,19 +5,19 @@
 //              per example i:  gain_sums_i = sum_t g_t * h_t,  shift_sums_i = sum_t g_t   (the two v_i of
 //              vector_kernels.cu, one pass over g and x together with dx),  sq[i] += |gain_sums_i|^2 + |shift_sums_i|^2
 //
-// Statistics, sums and everything in between are fp32; y, h and dx are rounded once.
+// Statistics, sums and everything in between are fp32; y, h and dx are rounded once.  The variance is a second pass over registers,
+// not over memory, and is taken about the mean.
 //
-// Forward: a row belongs to a group of W warps with up to four chunks of eight columns per thread, which stay in registers (as stored:
-// a bf16 row is widened where it is used), so the variance is a second pass over registers, not over memory, and is taken about
-// the mean.  A warp alone (W = 1) does up to 1024 columns.
+// A row belongs to a group of lanes (part of a warp for narrow rows, up to 16 warps for wide ones), each with 16-byte pieces of it, at most
+// 32 columns, as fp32 in registers: one conversion per element and pass.  Rows on 16-byte boundaries come to shared memory by bulk copies
+// that a warp of its own issues several tiles ahead, a tile being a row per group; so few warps with many registers are enough.  Other
+// rows are loaded element by element, a warp's accesses side by side.  The backward pass keeps the sums for its columns of gain and shift in
+// registers too.  (GPT-2 medium's norm at B = 64, T = 512, backward: loads straight into registers, spilling at 128 of them, 204 us; means
+// by rows and sums by columns from shared memory, each element converted twice, 66 to 74; in this form 49.)
 //
-// Backward: a row's two means run along the row, the parameters' sums across rows.  Rows come to shared memory in tiles (bulk copies, two
-// or more tiles in flight); a warp takes a row's means, then each thread takes the same 16 bytes of columns of every row, writes
-// dx and keeps its columns' sums in registers.  (With a row's columns spread over a warp's registers, sums and all, GPT-2 medium's norm at
-// B = 64, T = 512 took 204 us: 128 registers with spills, too few rows in flight.)
-// The rows of an example are shared out over a cluster of CTAs: at the end each CTA adds a slice of the columns over the cluster through
-// distributed shared memory, and rank 0 adds up the squares: one launch, no workspace, a fixed order.  Where a cluster's CTAs are too few
-// for a long sequence, the partial sums go through the workspace instead (ln_sums_kernel).
+// Backward: the rows of an example are shared out over a cluster of CTAs: at the end each CTA adds a slice of the columns over the cluster
+// through distributed shared memory, and rank 0 adds up the squares: one launch, no workspace, a fixed order.  Where a cluster's CTAs are
+// too few for a long sequence, the partial sums go through the workspace instead (ln_sums_kernel).
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -32,107 +32,206 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kLnMaxCols = 16384;          // 16 warps x 32 lanes x 4 chunks x 8 columns
-constexpr int kLnThreads = 256;
+constexpr int kLnMaxCols = 16384;          // 16 warps x 32 lanes x 32 columns
+constexpr int kLnMaxBuffers = 8;           // tiles in flight
+constexpr int kLnMaxParts = 16;            // CTAs of a cluster
 
-// Eight columns of a thread's chunk j.  kVec: consecutive ones (16-byte accesses); else a warp's accesses are
-// consecutive and the columns of a thread a group's width apart.
-template <bool kVec>
-__device__ __forceinline__ int ln_col(int j, int e, int tid, int width) {
-  return kVec ? (j * width + tid) * 8 + e : (j * 8 + e) * width + tid;
-}
+// Two columns.  (As fma.rn.f32x2 and the like these took longer: 66 us instead of 59 for the backward pass above.)
+struct F2 { float x, y; };
+__device__ __forceinline__ F2 f2(float x, float y) { return F2{x, y}; }
+__device__ __forceinline__ F2 add2(F2 a, F2 b) { return F2{a.x + b.x, a.y + b.y}; }
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) { return F2{a.x * b.x, a.y * b.y}; }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { return F2{fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y)}; }
+__device__ __forceinline__ float2 floats(F2 v) { return make_float2(v.x, v.y); }
 
 template <typename T> __device__ __forceinline__ T from_f32(float v);
 template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-template <typename T, bool kVec>
-struct LnChunk {
-  Raw8<T> raw;
-  __device__ __forceinline__ void load(const T* row, int j, int tid, int width, int p) {
-    if (kVec) {
-      const int c = ln_col<true>(j, 0, tid, width);
-      if (c < p) raw.load(row + c, 8, true);             // p is a multiple of 8 here
-      else raw.zero();
-    } else {
-      T v[8];
+// 16 bytes of a row
+template <typename T> struct Piece;
+template <> struct Piece<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void open(const uint4& q, F2 (&v)[2]) {
+    v[0] = f2(__uint_as_float(q.x), __uint_as_float(q.y));
+    v[1] = f2(__uint_as_float(q.z), __uint_as_float(q.w));
+  }
+  static __device__ __forceinline__ uint4 close(const F2 (&v)[2]) {
+    const float2 a = floats(v[0]), b = floats(v[1]);
+    return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
+  }
+};
+template <> struct Piece<__nv_bfloat16> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void open(const uint4& q, F2 (&v)[4]) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int c = ln_col<false>(j, e, tid, width);
-        v[e] = c < p ? row[c] : from_f32<T>(0.f);
+    for (int e = 0; e < 4; ++e) v[e] = f2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
+  }
+  static __device__ __forceinline__ uint4 close(const F2 (&v)[4]) {
+    uint4 q;
+    __nv_bfloat162 h[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 f = floats(v[e]);
+      h[e] = __floats2bfloat162_rn(f.x, f.y);
+    }
+    memcpy(&q, h, 16);
+    return q;
+  }
+};
+
+// How a kernel's threads share out rows.
+struct LnShape {
+  int lanes, W;              // lanes of a warp that a row has, warps of a row (with all their lanes)
+  int columns;               // of a lane, as its kernel is compiled
+  int groups;                // rows at a time, which are a tile
+  int buffers;               // tiles in shared memory
+  int pitch;                 // bytes of a row there
+};
+
+// Shared memory of a block: the tiles of `rows` tensors, whose place the groups' sums take at the end; gain and shift as floats; the
+// warps' parts of a row's sums; barriers; squares; a reduction's slots.
+struct LnSmem {
+  size_t tile, gain, shift, parts, bars, squares, red, bytes;
+  __host__ __device__ LnSmem(const LnShape& S, int p, int rows, bool sums, int warps) {
+    tile = size_t(S.groups) * rows * S.pitch;
+    size_t at = tile * size_t(S.buffers);              // no buffers: rows are loaded, not copied
+    const size_t most = sums ? size_t(S.groups) * 2 * p * sizeof(float) : 0;
+    if (at < most) at = most;
+    // all pieces of every lane (see LnRow::place), and unaligned rows' columns
+    const int width = S.lanes * S.W, padded = S.columns * width > p ? S.columns * width : (p + 3) / 4 * 4;
+    gain = at = (at + 15) / 16 * 16;
+    at += size_t(padded) * sizeof(float);
+    shift = at; at += sums ? 0 : size_t(padded) * sizeof(float);
+    parts = at; at += size_t(warps) * 4 * sizeof(float);
+    bars = at = (at + 15) / 16 * 16;
+    at += size_t(2) * S.buffers * sizeof(uint64_t);
+    squares = at; at += 16 * sizeof(float);
+    red = at; at += 32 * sizeof(float);
+    bytes = at;
+  }
+};
+
+// A parameter vector as floats, `absent` where there is none.
+__device__ __forceinline__ float ln_param(const void* q, int dt, float absent, int c) {
+  return !q ? absent : dt == DP_F32 ? static_cast<const float*>(q)[c] : __bfloat162float(static_cast<const __nv_bfloat16*>(q)[c]);
+}
+
+// The copying warp's part of a tile: n rows of one tensor, `pitch` bytes apart in shared memory.  Returns the bytes that this lane has to
+// announce; go: makes the copies.
+template <typename T>
+__device__ __forceinline__ uint32_t ln_copy(const T* first, long long ld, int p, int n, uint8_t* to, int pitch, bool whole, uint64_t* bar,
+                                            int lane, bool go) {
+  uint32_t bytes = 0;
+  if (whole) {                                         // rows follow one another: one copy
+    if (lane == 0) {
+      bytes = uint32_t(n) * uint32_t(pitch);
+      if (go) ptx::bulk_load(to, first, bytes, bar);
+    }
+    return bytes;
+  }
+  for (int r = lane; r < n; r += 32) {
+    if (go) ptx::bulk_load(to + size_t(r) * pitch, first + r * ld, uint32_t(pitch), bar);
+    bytes += uint32_t(pitch);
+  }
+  return bytes;
+}
+
+// A lane's pieces of a row.  kAligned: 16 bytes each; else the columns of a piece lie a row's pieces apart, so that a
+// warp's accesses are consecutive.
+template <typename T, int NP, bool kAligned>
+struct LnRow {
+  static constexpr int N = Piece<T>::N, H = N / 2;
+  int tid, width, pieces, p;
+  __device__ __forceinline__ int piece(int j) const { return tid + j * width; }
+  __device__ __forceinline__ int column(int j, int e) const { return kAligned ? piece(j) * N + e : e * pieces + piece(j); }
+  __device__ __forceinline__ bool has(int j) const { return piece(j) < pieces; }
+  // Zeros behind the row, and all zeros where `there` is false.  kAny: any values of the row behind it, for lanes of several pieces,
+  // whose row is there or not for the whole warp, where zeros in the vectors take them out (selecting took a sixth of the backward
+  // pass's instructions).
+  template <bool kAny>
+  __device__ __forceinline__ void open(const void* row, bool there, F2 (&v)[NP][H]) const {
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+      if (kAligned) {
+        uint4 q = make_uint4(0u, 0u, 0u, 0u);
+        if (kAny && NP > 1) q = static_cast<const uint4*>(row)[has(j) ? piece(j) : tid];
+        else if (there && has(j)) q = static_cast<const uint4*>(row)[piece(j)];
+        Piece<T>::open(q, v[j]);
+      } else {
+        const T* x = static_cast<const T*>(row);
+#pragma unroll
+        for (int e = 0; e < H; ++e) {
+          const int a = column(j, 2 * e), b = column(j, 2 * e + 1);
+          v[j][e] = f2(there && has(j) && a < p ? to_f32(x[a]) : 0.f, there && has(j) && b < p ? to_f32(x[b]) : 0.f);
+        }
       }
-      raw.load(v, 8, false);
+    }
+  }
+  // Where a vector of floats has column c in shared memory.  kAligned: quads of columns in the order in which a warp's lanes read them,
+  // 16 bytes beside 16 bytes (in the columns' own order a lane's eight lie 32 bytes from its neighbour's: four lanes to a bank, which
+  // cost the backward pass a third of its time).
+  __device__ __forceinline__ int place(int c) const {
+    if (!kAligned) return c;
+    const int q = c / N, j = q / width, t = q - j * width, e = c - q * N;
+    return ((j * (N / 4) + e / 4) * width + t) * 4 + (e & 3);
+  }
+  __device__ __forceinline__ void vector(const float* v, int j, F2 (&f)[H]) const {
+    if (kAligned) {
+#pragma unroll
+      for (int q = 0; q < N / 4; ++q) {
+        const float4 w = reinterpret_cast<const float4*>(v)[(j * (N / 4) + q) * width + tid];
+        f[2 * q] = f2(w.x, w.y);
+        f[2 * q + 1] = f2(w.z, w.w);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < H; ++e) {
+        const int a = column(j, 2 * e), b = column(j, 2 * e + 1);
+        f[e] = f2(has(j) && a < p ? v[a] : 0.f, has(j) && b < p ? v[b] : 0.f);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(T* out, bool vec, int j, const F2 (&v)[H]) const {
+    if (!has(j)) return;
+    if (kAligned && vec) {
+      reinterpret_cast<uint4*>(out)[piece(j)] = Piece<T>::close(v);
+      return;
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float2 f = floats(v[e / 2]);
+      if (column(j, e) < p) out[column(j, e)] = from_f32<T>(e & 1 ? f.y : f.x);
     }
   }
 };
 
-template <typename T> __device__ __forceinline__ void store8(T* p, const float (&v)[8]);
-template <> __device__ __forceinline__ void store8<float>(float* p, const float (&v)[8]) {
-  reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-  reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-}
-template <> __device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16* p, const float (&v)[8]) {
-  uint4 q;
-  __nv_bfloat162 h[4];
+// Sums over a row's lanes.  Across warps they meet in `slots` (4 W floats of the group): two halves used in turn, so that one barrier per
+// sum suffices (a half is written again only behind the barrier of the sum between).
+template <int K>
+__device__ __forceinline__ void row_sum(float (&v)[K], const LnShape& S, int warp_in_group, int lane, int barrier, float* slots, int& turn) {
+  if (S.lanes == 32) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) h[e] = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
-  memcpy(&q, h, 16);
-  *reinterpret_cast<uint4*>(p) = q;
-}
-
-template <typename T, bool kVec>
-__device__ __forceinline__ void ln_store(T* row, const float (&v)[8], int j, int tid, int width, int p) {
-  if (kVec) {
-    const int c = ln_col<true>(j, 0, tid, width);
-    if (c < p) store8<T>(row + c, v);
+    for (int k = 0; k < K; ++k) v[k] = warp_sum(v[k]);
   } else {
+    for (int o = S.lanes >> 1; o > 0; o >>= 1) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int c = ln_col<false>(j, e, tid, width);
-      if (c < p) row[c] = from_f32<T>(v[e]);
+      for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
     }
   }
-}
-
-// eight values of a parameter vector, `absent` where there is none
-template <bool kVec>
-__device__ __forceinline__ void ln_param(const void* q, int dt, float absent, int j, int tid, int width, int p, float (&v)[8]) {
-  if (!q) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = absent;
-    return;
-  }
-  if (kVec && ln_col<true>(j, 0, tid, width) < p) {
-    const int c = ln_col<true>(j, 0, tid, width);
-    if (dt == DP_F32) load8<float>(static_cast<const float*>(q) + c, 8, true, v);
-    else load8<__nv_bfloat16>(static_cast<const __nv_bfloat16*>(q) + c, 8, true, v);
-    return;
-  }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int c = ln_col<kVec>(j, e, tid, width);
-    v[e] = c >= p ? 0.f : dt == DP_F32 ? static_cast<const float*>(q)[c] : __bfloat162float(static_cast<const __nv_bfloat16*>(q)[c]);
-  }
-}
-
-// Sums over the W warps of a row's group.  `red` holds 2 * 2 * W floats of the group: two slots used in turn, so one
-// barrier per sum suffices (a slot is written again only after the barrier of the sum between).
-template <int N>
-__device__ __forceinline__ void group_sum(float (&v)[N], int W, int warp_in_group, int lane, int barrier, float* red, int& turn) {
-#pragma unroll
-  for (int k = 0; k < N; ++k) v[k] = warp_sum(v[k]);
-  if (W == 1) return;
-  float* slot = red + turn * 2 * W;
+  if (S.W == 1) return;
+  float* half = slots + turn * 2 * S.W;
   turn ^= 1;
   if (lane == 0) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) slot[k * W + warp_in_group] = v[k];
+    for (int k = 0; k < K; ++k) half[k * S.W + warp_in_group] = v[k];
   }
-  asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(W * 32) : "memory");
+  asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(S.W * 32) : "memory");
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    float s = lane < W ? slot[k * W + lane] : 0.f;
-    v[k] = warp_sum(s);
+  for (int k = 0; k < K; ++k) {
+    v[k] = 0.f;
+    for (int w = 0; w < S.W; ++w) v[k] += half[k * S.W + w];
   }
 }
 
@@ -143,65 +242,116 @@ struct LnForward {
   void* H; long long ldh;
   float* mean; float* rstd;
   long long rows;
-  int p, W;
+  int p;
+  int whole, vec_y, vec_h;       // X's rows follow one another; outputs are written in 16-byte pieces (rows read in such)
   float eps;
+  LnShape S;
+  long long wait_limit;
 };
 
-// four blocks of 256 threads per SM (64 registers): what hides the latency is rows in flight
-template <typename T, int NV, bool kVec, int kThreads>
-__global__ void __launch_bounds__(kThreads, 1024 / kThreads)
+template <typename T, int NP, bool kAligned, int kThreads, int kBlocks>
+__global__ void __launch_bounds__(kThreads, kBlocks)
 ln_forward_kernel(const LnForward P) {
-  __shared__ float red[4 * (kThreads / 32)];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int W = P.W, width = W * 32, group = warp / W, groups = (blockDim.x >> 5) / W;
-  const int tid = threadIdx.x - group * width;
-  float* my_red = red + group * 4 * W;
-  int turn = 0;
-  for (long long row = (long long)blockIdx.x * groups + group; row < P.rows; row += (long long)gridDim.x * groups) {
-    const T* x = static_cast<const T*>(P.X) + row * P.ldx;
-    LnChunk<T, kVec> in[NV];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) in[j].load(x, j, tid, width, P.p);
-    float s[1] = {0.f};
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      float v[8];
-      in[j].raw.unpack(v);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s[0] += v[e];
+  constexpr int N = Piece<T>::N, H = N / 2;
+  extern __shared__ __align__(128) uint8_t smem[];
+  const LnShape& S = P.S;
+  const int p = P.p, warps = (blockDim.x >> 5) - (kAligned ? 1 : 0);       // the last warp copies
+  const LnSmem at(S, p, 1, false, warps);
+  float* gain = reinterpret_cast<float*>(smem + at.gain);
+  float* shift = reinterpret_cast<float*>(smem + at.shift);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + at.bars);
+  uint64_t* empty = full + S.buffers;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const long long r0 = P.rows * blockIdx.x / gridDim.x, r1 = P.rows * (blockIdx.x + 1) / gridDim.x;
+  const int tiles = int((r1 - r0 + S.groups - 1) / S.groups);
+  const T* X = static_cast<const T*>(P.X);
+  if (tid == 0) {
+    for (int k = 0; k < S.buffers; ++k) { ptx::mbar_init(full + k, 32); ptx::mbar_init(empty + k, warps); }
+    ptx::fence_mbar_init();
+  }
+  __syncthreads();
+  if (kAligned && warp == warps) {
+    int b = 0;
+    uint32_t phase = 1;                                  // of the use before
+    for (int k = 0; k < tiles; ++k) {
+      if (k >= S.buffers && !ptx::mbar_wait_own(empty + b, phase, P.wait_limit)) break;
+      const long long first = r0 + (long long)k * S.groups;
+      const int n = int(min((long long)S.groups, r1 - first));
+      uint8_t* to = smem + size_t(b) * at.tile;
+      ptx::mbar_arrive_expect_tx(full + b, ln_copy<T>(X + first * P.ldx, P.ldx, p, n, to, S.pitch, P.whole, full + b, lane, false));
+      ln_copy<T>(X + first * P.ldx, P.ldx, p, n, to, S.pitch, P.whole, full + b, lane, true);
+      if (++b == S.buffers) { b = 0; phase ^= 1; }
     }
-    group_sum<1>(s, W, warp - group * W, lane, 1 + group, my_red, turn);
-    const float mean = s[0] / float(P.p);
-    s[0] = 0.f;
+    return;
+  }
+  const int per_row = S.lanes * S.W, group = tid / per_row;
+  const LnRow<T, NP, kAligned> R{tid - group * per_row, per_row, (p + N - 1) / N, p};
+  for (int c = tid; c < max(p, per_row * NP * N); c += warps * 32) {
+    gain[R.place(c)] = c < p ? ln_param(P.gain, P.param_dt, 1.f, c) : 0.f;
+    shift[R.place(c)] = c < p ? ln_param(P.shift, P.param_dt, 0.f, c) : 0.f;
+  }
+  asm volatile("bar.sync 15, %0;" ::"r"(warps * 32) : "memory");
+  float* slots = reinterpret_cast<float*>(smem + at.parts) + (S.W > 1 ? group * 4 * S.W : 0);
+  const float inv_p = 1.f / float(p);
+  int b = 0, turn = 0;
+  uint32_t phase = 0;
+  bool ok = true;
+  for (int k = 0; k < tiles; ++k) {
+    if (kAligned && ok) ok = ptx::mbar_wait_own(full + b, phase, P.wait_limit);    // (one that ran out goes on: others meet it at barriers)
+    const long long row = r0 + (long long)k * S.groups + group;
+    const bool mine = group < S.groups && row < r1;
+    F2 v[NP][H];
+    if (kAligned) {
+      R.template open<false>(smem + size_t(b) * at.tile + size_t(mine ? group : 0) * S.pitch, mine, v);
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(empty + b);        // the row is in registers
+      if (++b == S.buffers) { b = 0; phase ^= 1; }
+    } else {
+      R.template open<false>(X + (mine ? row : r0) * P.ldx, mine, v);
+    }
+    F2 sum = f2(0.f, 0.f);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      float v[8];
-      in[j].raw.unpack(v);
+    for (int j = 0; j < NP; ++j)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float d = v[e] - mean;
-        if (ln_col<kVec>(j, e, tid, width) < P.p) s[0] = fmaf(d, d, s[0]);
+      for (int e = 0; e < H; ++e) sum = add2(sum, v[j][e]);
+    float s[1] = {floats(sum).x + floats(sum).y};
+    row_sum<1>(s, S, warp % S.W, lane, 1 + group, slots, turn);
+    // a true quotient where it is cheap: 1 / p rounded would move the mean by half a rounding more
+    const float mean = s[0] / float(p);
+    const F2 minus = f2(-mean, -mean);
+    sum = f2(0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < NP; ++j)
+#pragma unroll
+      for (int e = 0; e < H; ++e) {
+        v[j][e] = add2(v[j][e], minus);
+        if (!R.has(j)) v[j][e] = f2(0.f, 0.f);
+        else if (!kAligned) {
+          const float2 f = floats(v[j][e]);
+          v[j][e] = f2(R.column(j, 2 * e) < p ? f.x : 0.f, R.column(j, 2 * e + 1) < p ? f.y : 0.f);
+        }
+        sum = fma2(v[j][e], v[j][e], sum);
+      }
+    s[0] = floats(sum).x + floats(sum).y;
+    row_sum<1>(s, S, warp % S.W, lane, 1 + group, slots, turn);
+    const float rstd = 1.f / sqrtf(s[0] * inv_p + P.eps);
+    if (!mine) continue;
+    const F2 scale = f2(rstd, rstd);
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+#pragma unroll
+      for (int e = 0; e < H; ++e) v[j][e] = mul2(v[j][e], scale);
+      if (P.H) R.store(static_cast<T*>(P.H) + row * P.ldh, P.vec_h, j, v[j]);
+      if (P.Y && R.has(j)) {
+        F2 a[H], c[H];
+        R.vector(gain, j, a);
+        R.vector(shift, j, c);
+#pragma unroll
+        for (int e = 0; e < H; ++e) v[j][e] = fma2(v[j][e], a[e], c[e]);
+        R.store(static_cast<T*>(P.Y) + row * P.ldy, P.vec_y, j, v[j]);
       }
     }
-    group_sum<1>(s, W, warp - group * W, lane, 1 + group, my_red, turn);
-    const float rstd = 1.f / sqrtf(s[0] / float(P.p) + P.eps);
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      float v[8];
-      in[j].raw.unpack(v);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = (v[e] - mean) * rstd;
-      if (P.H) ln_store<T, kVec>(static_cast<T*>(P.H) + row * P.ldh, v, j, tid, width, P.p);
-      if (P.Y) {
-        float a[8], b[8];
-        ln_param<kVec>(P.gain, P.param_dt, 1.f, j, tid, width, P.p, a);
-        ln_param<kVec>(P.shift, P.param_dt, 0.f, j, tid, width, P.p, b);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e], a[e], b[e]);
-        ln_store<T, kVec>(static_cast<T*>(P.Y) + row * P.ldy, v, j, tid, width, P.p);
-      }
-    }
-    if (tid == 0) {
+    if (R.tid == 0) {
       if (P.mean) P.mean[row] = mean;
       if (P.rstd) P.rstd[row] = rstd;
     }
@@ -217,251 +367,169 @@ struct LnBackward {
   float* gain_sums; float* shift_sums; float* sq;
   float* partials;               // [B][parts][2][p], or nullptr where the parts are a cluster
   int T, p, parts;
-  int bulk;                      // rows come by bulk copies: 16-byte boundaries, p % 8 == 0
-  int vec_out;                   // dX is written in 16-byte pieces
-  int rows, buffers;             // of a tile; tiles in shared memory
+  int whole_g, whole_x, vec_out;
+  LnShape S;
+  int* dev_status;
+  long long wait_limit;
 };
 
-// Shared memory of a block: buffers of tiles of G and X rows (16-byte pitch), which the sums take over at the end; the gain as
-// floats; per row of each buffer its mean and rstd; the warps' parts of the means of a tile's rows; barriers; squares.
-struct LnSmem {
-  int pitch;                     // bytes of a row
-  size_t tile, gain, stats, means, bars, squares, red, bytes;
-  __host__ __device__ LnSmem(int p, int es, int rows, int buffers, int warps) {
-    pitch = (p * es + 15) / 16 * 16;
-    tile = size_t(rows) * 2 * pitch;
-    size_t at = tile * buffers;
-    if (at < size_t(2) * p * sizeof(float)) at = size_t(2) * p * sizeof(float);
-    gain = at = (at + 15) / 16 * 16;
-    at += size_t(pitch / es) * sizeof(float);
-    stats = at; at += size_t(buffers) * rows * 2 * sizeof(float);
-    means = at; at += size_t(rows) * warps * 2 * sizeof(float);
-    bars = at = (at + 15) / 16 * 16;
-    at += size_t(buffers) * sizeof(uint64_t);
-    squares = at; at += 16 * sizeof(float);
-    red = at; at += 32 * sizeof(float);
-    bytes = at;
-  }
-};
-
-constexpr int kLnMaxRows = 16, kLnMaxBuffers = 4;
-
-template <typename T> struct Piece;                    // 16 bytes of a row
-template <> struct Piece<float> {
-  static constexpr int N = 4;
-  static __device__ __forceinline__ void unpack(const uint4& q, float (&v)[4]) {
-    v[0] = __uint_as_float(q.x); v[1] = __uint_as_float(q.y); v[2] = __uint_as_float(q.z); v[3] = __uint_as_float(q.w);
-  }
-  static __device__ __forceinline__ uint4 pack(const float (&v)[4]) {
-    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-  }
-};
-template <> struct Piece<__nv_bfloat16> {
-  static constexpr int N = 8;
-  static __device__ __forceinline__ void unpack(const uint4& q, float (&v)[8]) {
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      v[2 * e] = __uint_as_float(w[e] << 16);
-      v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-    }
-  }
-  static __device__ __forceinline__ uint4 pack(const float (&v)[8]) {
-    uint4 q;
-    __nv_bfloat162 h[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) h[e] = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
-    memcpy(&q, h, 16);
-    return q;
-  }
-};
-
-// NV: pieces of 16 bytes per thread and row
-template <typename T, int NV, int kThreads>
-__global__ void __launch_bounds__(kThreads)
+template <typename T, int NP, bool kAligned, int kThreads, int kBlocks>
+__global__ void __launch_bounds__(kThreads, kBlocks)
 ln_backward_kernel(const LnBackward P) {
-  constexpr int N = Piece<T>::N;
-  extern __shared__ __align__(16) uint8_t smem[];
-  const int p = P.p, R = P.rows, nb = P.buffers, warps = blockDim.x >> 5;
-  const LnSmem at(p, sizeof(T), R, nb, warps);
+  constexpr int N = Piece<T>::N, H = N / 2;
+  extern __shared__ __align__(128) uint8_t smem[];
+  const LnShape& S = P.S;
+  const int p = P.p, warps = (blockDim.x >> 5) - (kAligned ? 1 : 0);       // the last warp copies
+  const LnSmem at(S, p, 2, true, warps);
   float* sums = reinterpret_cast<float*>(smem);
   float* gain = reinterpret_cast<float*>(smem + at.gain);
-  float* stats = reinterpret_cast<float*>(smem + at.stats);
-  float* means = reinterpret_cast<float*>(smem + at.means);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + at.bars);
+  uint64_t* empty = full + S.buffers;
   float* squares = reinterpret_cast<float*>(smem + at.squares);
   float* red = reinterpret_cast<float*>(smem + at.red);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int example = blockIdx.x / P.parts, part = blockIdx.x - example * P.parts;
   const int r0 = int((long long)P.T * part / P.parts), r1 = int((long long)P.T * (part + 1) / P.parts);
   const long long base = (long long)example * P.T;
-  const int tiles = (r1 - r0 + R - 1) / R, pieces = at.pitch / 16;
-  const float inv_p = 1.f / float(p);
-
-  // tile k to its buffer: a bulk copy per row of G and of X, or element by element with zeros behind the row
-  auto fill = [&](int k) {
-    uint8_t* to = smem + size_t(k % nb) * at.tile;
-    const int first = r0 + k * R, n = min(R, r1 - first);
-    if (P.bulk) {
-      if (warp == 0) {
-        uint64_t* bar = full + k % nb;
-        const uint32_t bytes = uint32_t(p) * sizeof(T);
-        if (lane == 0) ptx::mbar_arrive_expect_tx(bar, 2 * uint32_t(n) * bytes);
-        __syncwarp();
-        if (lane < n) {
-          const long long row = base + first + lane;
-          ptx::bulk_load(to + size_t(2 * lane) * at.pitch, static_cast<const T*>(P.G) + row * P.ldg, bytes, bar);
-          ptx::bulk_load(to + size_t(2 * lane + 1) * at.pitch, static_cast<const T*>(P.X) + row * P.ldx, bytes, bar);
-        }
-      }
-    } else {
-      const int cols = at.pitch / int(sizeof(T));
-      for (int r = 0; r < n; ++r) {
-        const long long row = base + first + r;
-        const T* g = static_cast<const T*>(P.G) + row * P.ldg;
-        const T* x = static_cast<const T*>(P.X) + row * P.ldx;
-        T* tg = reinterpret_cast<T*>(to + size_t(2 * r) * at.pitch);
-        T* tx = reinterpret_cast<T*>(to + size_t(2 * r + 1) * at.pitch);
-        for (int c = tid; c < cols; c += blockDim.x) {
-          tg[c] = c < p ? g[c] : from_f32<T>(0.f);
-          tx[c] = c < p ? x[c] : from_f32<T>(0.f);
-        }
-      }
-    }
-    if (tid < 2 * n)
-      stats[(k % nb) * 2 * R + tid] = (tid & 1 ? P.rstd : P.mean)[base + first + (tid >> 1)];
-  };
-
-  if (tid == 0 && P.bulk) {
-    for (int k = 0; k < nb; ++k) ptx::mbar_init(full + k, 1);
+  const int tiles = (r1 - r0 + S.groups - 1) / S.groups;
+  const T* G = static_cast<const T*>(P.G);
+  const T* X = static_cast<const T*>(P.X);
+  if (tid == 0) {
+    for (int k = 0; k < S.buffers; ++k) { ptx::mbar_init(full + k, 32); ptx::mbar_init(empty + k, warps); }
     ptx::fence_mbar_init();
   }
-  for (int c = tid; c < pieces * N; c += blockDim.x)
-    gain[c] = !P.gain ? 1.f : c >= p ? 0.f : P.param_dt == DP_F32 ? static_cast<const float*>(P.gain)[c]
-                                                                 : __bfloat162float(static_cast<const __nv_bfloat16*>(P.gain)[c]);
   __syncthreads();
-  for (int k = 0; k < min(nb, tiles); ++k) fill(k);
+  const int per_row = S.lanes * S.W, group = tid / per_row;
+  const LnRow<T, NP, kAligned> R{tid - group * per_row, per_row, (p + N - 1) / N, p};
+  F2 gs[NP][H], ss[NP][H];
+#pragma unroll
+  for (int j = 0; j < NP; ++j)
+#pragma unroll
+    for (int e = 0; e < H; ++e) gs[j][e] = ss[j][e] = f2(0.f, 0.f);
 
-  // this thread's rows of a tile and its pieces of a row
-  const int groups = NV == 1 ? max(1, int(blockDim.x) / pieces) : 1;
-  const int group = NV == 1 ? tid / pieces : 0;
-  const int piece0 = NV == 1 ? tid - group * pieces : tid;
-  float gs[NV][N], ss[NV][N], a[NV][N];
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int piece = piece0 + j * blockDim.x;
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      gs[j][e] = ss[j][e] = 0.f;
-      a[j][e] = piece < pieces ? gain[piece * N + e] : 0.f;
+  if (kAligned && warp == warps) {
+    // ------------------------------------------------------------------ copies
+    int b = 0;
+    uint32_t phase = 1;                                  // of the use before
+    for (int k = 0; k < tiles; ++k) {
+      if (k >= S.buffers && !ptx::mbar_wait_own(empty + b, phase, P.wait_limit)) break;
+      const int first = r0 + k * S.groups, n = min(S.groups, r1 - first);
+      const T* g = G + (base + first) * P.ldg;
+      const T* x = X + (base + first) * P.ldx;
+      uint8_t* to = smem + size_t(b) * at.tile;
+      uint8_t* to_x = to + size_t(S.groups) * S.pitch;
+      ptx::mbar_arrive_expect_tx(full + b, ln_copy<T>(g, P.ldg, p, n, to, S.pitch, P.whole_g, full + b, lane, false) +
+                                               ln_copy<T>(x, P.ldx, p, n, to_x, S.pitch, P.whole_x, full + b, lane, false));
+      ln_copy<T>(g, P.ldg, p, n, to, S.pitch, P.whole_g, full + b, lane, true);
+      ln_copy<T>(x, P.ldx, p, n, to_x, S.pitch, P.whole_x, full + b, lane, true);
+      if (++b == S.buffers) { b = 0; phase ^= 1; }
     }
-  }
-  // warps per row for the means, and how many rows they take at once
-  const int per_row = max(1, warps / R), at_once = warps / per_row;
-
-  for (int k = 0; k < tiles; ++k) {
-    const uint8_t* tile = smem + size_t(k % nb) * at.tile;
-    const float* st = stats + (k % nb) * 2 * R;
-    const int first = r0 + k * R, n = min(R, r1 - first);
-    if (!P.bulk) __syncthreads();                      // filled by every thread (and the statistics with it)
-    else {
-      if (k < nb || nb == 1) __syncthreads();          // the statistics; with more buffers later tiles' are a sync older
-      const long long t0 = clock64();
-      while (!ptx::mbar_try_wait(full + k % nb, (k / nb) & 1))
-        if (clock64() - t0 > ptx::kDefaultWaitLimit) break;      // copies of this block's own: they end
-    }
-    if (P.dX) {
-      for (int r = warp / per_row; r < n && warp < per_row * at_once; r += at_once) {
-        const uint4* g = reinterpret_cast<const uint4*>(tile + size_t(2 * r) * at.pitch);
-        const uint4* x = reinterpret_cast<const uint4*>(tile + size_t(2 * r + 1) * at.pitch);
-        const float mean = st[2 * r], rstd = st[2 * r + 1];
-        float s1 = 0.f, s2 = 0.f;
-        for (int c = (warp % per_row) * 32 + lane; c < pieces; c += per_row * 32) {
-          float gv[N], h[N];
-          Piece<T>::unpack(g[c], gv);
-          Piece<T>::unpack(x[c], h);
-          const float4* w = reinterpret_cast<const float4*>(gain + c * N);
+    // (copies in flight land before the block ends: its other warps wait for every tile, and give up after the same time)
+  } else {
+    // -------------------------------------------------------------------- work
+    for (int c = tid; c < max(p, per_row * NP * N); c += warps * 32)
+      gain[R.place(c)] = c < p ? ln_param(P.gain, P.param_dt, 1.f, c) : 0.f;
+    asm volatile("bar.sync 15, %0;" ::"r"(warps * 32) : "memory");
+    float* slots = reinterpret_cast<float*>(smem + at.parts) + (S.W > 1 ? group * 4 * S.W : 0);
+    const float inv_p = 1.f / float(p);
+    int b = 0, turn = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    T* out = static_cast<T*>(P.dX) + (base + r0 + group) * P.lddx;
+    const long long out_step = S.groups * P.lddx;      // (a row that is not there is a group's last)
+    // a row's statistics are fetched a tile ahead
+    float next_mean = 0.f, next_rstd = 0.f;
+    auto look = [&](int k) {
+      const int r = r0 + k * S.groups + group;
+      const bool there = group < S.groups && r < r1;
+      next_mean = there ? P.mean[base + r] : 0.f;
+      next_rstd = there ? P.rstd[base + r] : 0.f;
+    };
+    look(0);
+    for (int k = 0; k < tiles; ++k) {
+      // a warp whose wait has run out goes on without waiting: others meet it at barriers
+      if (kAligned && ok && !ptx::mbar_wait_own(full + b, phase, P.wait_limit)) {
+        ok = false;
+        if (P.dev_status && lane == 0) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
+      }
+      const int r = r0 + k * S.groups + group;
+      const bool mine = group < S.groups && r < r1;
+      const long long row = base + (mine ? r : r0 + k * S.groups);
+      // nothing of a row that is not there enters the sums: zeros, mean and rstd among them
+      const float mean = next_mean, rstd = next_rstd;
+      look(k + 1);
+      F2 g[NP][H], c[NP][H];
+      if (kAligned) {
+        const uint8_t* from = smem + size_t(b) * at.tile + size_t(mine ? group : 0) * S.pitch;
+        R.template open<true>(from, mine, g);
+        R.template open<true>(from + size_t(S.groups) * S.pitch, mine, c);
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(empty + b);      // the row is in registers
+        if (++b == S.buffers) { b = 0; phase ^= 1; }
+      } else {
+        R.template open<true>(G + row * P.ldg, mine, g);
+        R.template open<true>(X + row * P.ldx, mine, c);
+      }
+      if (NP > 1 && !mine) continue;                     // whole warps, and all of a group's
+      const F2 minus = f2(-mean, -mean), scale = f2(rstd, rstd);
+      F2 a1 = f2(0.f, 0.f), a2 = a1;
 #pragma unroll
-          for (int q = 0; q < N / 4; ++q) {
-            const float4 b = w[q];
-            const float bb[4] = {b.x, b.y, b.z, b.w};
+      for (int j = 0; j < NP; ++j) {
+        F2 w[H];
+        R.vector(gain, j, w);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float u = gv[4 * q + e] * bb[e];   // 0 behind the row
-              s1 += u;
-              s2 = fmaf(u, (h[4 * q + e] - mean) * rstd, s2);
-            }
-          }
-        }
-        s1 = warp_sum(s1);
-        s2 = warp_sum(s2);
-        if (lane == 0) {
-          means[(r * warps + warp % per_row) * 2] = s1;
-          means[(r * warps + warp % per_row) * 2 + 1] = s2;
+        for (int e = 0; e < H; ++e) {
+          c[j][e] = add2(c[j][e], minus);
+          ss[j][e] = add2(ss[j][e], g[j][e]);
+          g[j][e] = mul2(g[j][e], scale);
+          gs[j][e] = fma2(g[j][e], c[j][e], gs[j][e]);
+          g[j][e] = mul2(g[j][e], w[e]);                 // rstd u
+          a1 = add2(a1, g[j][e]);
+          a2 = fma2(g[j][e], c[j][e], a2);
         }
       }
-      __syncthreads();
-    }
-    if (group < groups) {
-      for (int r = group; r < n; r += groups) {
-        const uint4* g = reinterpret_cast<const uint4*>(tile + size_t(2 * r) * at.pitch);
-        const uint4* x = reinterpret_cast<const uint4*>(tile + size_t(2 * r + 1) * at.pitch);
-        const float mean = st[2 * r], rstd = st[2 * r + 1];
-        float m1 = 0.f, m2 = 0.f;
-        if (P.dX) {
-          for (int w = 0; w < per_row; ++w) { m1 += means[(r * warps + w) * 2]; m2 += means[(r * warps + w) * 2 + 1]; }
-          m1 *= inv_p;
-          m2 *= inv_p;
-        }
+      if (P.dX) {
+        // dx = rstd u - mean(rstd u) - (x - mean) rstd^2 mean(rstd u (x - mean))
+        float s[2] = {a1.x + a1.y, a2.x + a2.y};
+        row_sum<2>(s, S, warp % S.W, lane, 1 + group, slots, turn);
+        const float k1 = -s[0] * inv_p, k2 = -rstd * rstd * (s[1] * inv_p);
+        const F2 kk1 = f2(k1, k1), kk2 = f2(k2, k2);
+        if (mine) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-          const int piece = piece0 + j * blockDim.x;
-          if (NV > 1 && piece >= pieces) break;
-          float gv[N], h[N], d[N];
-          Piece<T>::unpack(g[piece], gv);
-          Piece<T>::unpack(x[piece], h);
+          for (int j = 0; j < NP; ++j) {
 #pragma unroll
-          for (int e = 0; e < N; ++e) {
-            h[e] = (h[e] - mean) * rstd;
-            gs[j][e] = fmaf(gv[e], h[e], gs[j][e]);
-            ss[j][e] += gv[e];
-            d[e] = (fmaf(gv[e], a[j][e], -m1) - h[e] * m2) * rstd;
-          }
-          if (P.dX) {
-            T* out = static_cast<T*>(P.dX) + (base + first + r) * P.lddx + piece * N;
-            if (P.vec_out) *reinterpret_cast<uint4*>(out) = Piece<T>::pack(d);
-            else {
-#pragma unroll
-              for (int e = 0; e < N; ++e) if (piece * N + e < p) out[e] = from_f32<T>(d[e]);
-            }
+            for (int e = 0; e < H; ++e) g[j][e] = add2(g[j][e], fma2(c[j][e], kk2, kk1));
+            R.store(out, P.vec_out, j, g[j]);
           }
         }
+        out += out_step;
       }
     }
-    __syncthreads();                                   // the buffer has been read
-    if (k + nb < tiles) fill(k + nb);
   }
   if (!P.gain_sums && !P.shift_sums && !P.sq) return;          // the same for every CTA
-  // this CTA's sums, its groups one after the other
-  if (tiles == 0) {
-    for (int c = tid; c < 2 * p; c += blockDim.x) sums[c] = 0.f;
+  // this CTA's sums: every group's in the place of the tiles, then added in order
+  __syncthreads();
+  if (warp < warps && group < S.groups) {
+    float* mine = sums + size_t(group) * 2 * p;
+#pragma unroll
+    for (int j = 0; j < NP; ++j)
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float2 u = floats(gs[j][e / 2]), v = floats(ss[j][e / 2]);
+        const int c = R.column(j, e);
+        if (R.has(j) && c < p) { mine[c] = e & 1 ? u.y : u.x; mine[p + c] = e & 1 ? v.y : v.x; }
+      }
   }
-  for (int q = 0; q < groups && tiles; ++q) {
-    if (group == q) {
-#pragma unroll
-      for (int j = 0; j < NV; ++j)
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-          const int c = (piece0 + j * int(blockDim.x)) * N + e;
-          if (c < p) {
-            sums[c] = (q ? sums[c] : 0.f) + gs[j][e];
-            sums[p + c] = (q ? sums[p + c] : 0.f) + ss[j][e];
-          }
-        }
+  __syncthreads();
+  if (S.groups > 1) {
+    for (int c = tid; c < 2 * p; c += blockDim.x) {
+      float u = sums[c];
+#pragma unroll 4
+      for (int q = 1; q < S.groups; ++q) u += sums[size_t(q) * 2 * p + c];
+      sums[c] = u;
     }
     __syncthreads();
   }
-  __syncthreads();
   if (P.partials) {
     float* out = P.partials + (long long)blockIdx.x * 2 * p;
     for (int c = tid; c < 2 * p; c += blockDim.x) out[c] = sums[c];
@@ -474,10 +542,17 @@ ln_backward_kernel(const LnBackward P) {
   for (int c = c0 + tid; c < c1; c += blockDim.x) {
     float u = 0.f, v = 0.f;
     if (P.parts > 1) {
-      for (int q = 0; q < P.parts; ++q) {
-        const float* other = cluster.map_shared_rank(sums, q);
-        u += other[c];
-        v += other[p + c];
+      for (int q = 0; q < P.parts; q += 4) {             // four CTAs' loads in flight
+        float t[4], w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float* other = cluster.map_shared_rank(sums, min(q + i, P.parts - 1));
+          t[i] = other[c];
+          w[i] = other[p + c];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (q + i < P.parts) { u += t[i]; v += w[i]; }
       }
     } else {
       u = sums[c];
@@ -517,52 +592,84 @@ ln_sums_kernel(const float* partials, int parts, int p, float* gain_sums, float*
   if (threadIdx.x == 0) squares[example * gridDim.x + blockIdx.x] = sq;
 }
 
-// warps per row of the forward pass: as few as leave a thread three chunks (four spill), two where its columns are apart (a
-// predicate each)
-int ln_warps(int p, bool vec) {
-  int W = 1;
-  while (W < 16 && W * 32 * (vec ? 3 : 2) * 8 < p) W *= 2;
-  return W;
-}
-
 bool ln_vec(const void* q, long long ld, int es) { return !q || (aligned16(q) && (ld * es) % 16 == 0); }
 
-constexpr int kLnMaxParts = 16;            // CTAs of a cluster
-
-// Parts an example's rows are cut into, and whether they are a cluster (else the sums go through the workspace): about three
-// CTAs per SM, eight rows each at least.
-struct LnParts { int parts; bool cluster; };
-LnParts ln_parts(int B, int T) {
-  const int wanted = std::max(1, 3 * sm_count() / B);
-  const int most = ceil_div(T, 8);
-  if (wanted > 2 * kLnMaxParts && T >= 1024 * kLnMaxParts) return {std::min(wanted, T / 512), false};
-  return {std::max(1, std::min(std::min(wanted, most), kLnMaxParts)), true};
+// Lanes and warps of a row: 16-byte pieces, at most 32 columns a lane.
+LnShape ln_shape(int p, int es) {
+  LnShape S{};
+  const int pieces = ceil_div(p * es, 16), most = 2 * es;              // pieces per lane
+  S.lanes = 1;
+  while (S.lanes < 32 && S.lanes < pieces) S.lanes *= 2;
+  S.W = 1;
+  while (S.W * 32 * most < pieces) S.W *= 2;
+  S.pitch = pieces * 16;
+  return S;
 }
 
-template <typename T, int NV, int kThreads>
-dp_status ln_back_launch(LnBackward& P, int B, int threads, bool cluster, cudaStream_t st) {
-  auto* kernel = ln_backward_kernel<T, NV, kThreads>;
-  // rows per tile and tiles: a third of an SM's shared memory where three CTAs share it, all of it for a CTA alone
-  const size_t most = (long long)B * P.parts > sm_count() ? 72 * 1024 : 200 * 1024;
-  const int pitch = (P.p * int(sizeof(T)) + 15) / 16 * 16;
-  P.rows = std::max(1, std::min(kLnMaxRows, int(24 * 1024 / (2 * pitch))));
-  P.rows = std::min(P.rows, std::max(1, ceil_div(P.T, P.parts)));
-  P.buffers = P.bulk ? kLnMaxBuffers : 1;
-  while (P.buffers > 1 && LnSmem(P.p, sizeof(T), P.rows, P.buffers, threads / 32).bytes > most) --P.buffers;
-  if (P.buffers == 1 && P.bulk && LnSmem(P.p, sizeof(T), P.rows, 2, threads / 32).bytes <= 225 * 1024) P.buffers = 2;
-  const LnSmem smem(P.p, sizeof(T), P.rows, P.buffers, threads / 32);
+// Pieces per lane that a kernel is compiled for.
+int ln_pieces(const LnShape& S, int p, int es) {
+  const int n = ceil_div(ceil_div(p * es, 16), S.lanes * S.W);
+  return es == 4 && n > 2 ? (n + 1) / 2 * 2 : n;
+}
+
+template <typename K>
+dp_status ln_smem_setup(K* kernel) {
   if (first_use_on_this_device((const void*)kernel)) {
     DP_CUDA_OK(allow_shared(kernel, 227 * 1024));
     DP_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   }
+  return DP_OK;
+}
+
+// Rows at a time and tiles in flight: an SM's shared memory divided by the blocks that share it, 48 KiB a tile at most.
+bool ln_fit(LnShape& S, int p, int rows, bool sums, int warps, int blocks, bool copied) {
+  S.groups = S.W > 1 ? warps / S.W : warps * 32 / S.lanes;
+  const size_t most = (blocks == 1 ? 224 : blocks == 2 ? 112 : 74) * 1024;
+  if (!copied) {
+    S.buffers = 0;
+    return LnSmem(S, p, rows, sums, warps).bytes <= 226 * 1024;
+  }
+  S.groups = std::max(1, std::min(S.groups, int(48 * 1024 / (rows * S.pitch))));
+  for (S.buffers = kLnMaxBuffers; S.buffers > 1; --S.buffers)
+    if (LnSmem(S, p, rows, sums, warps).bytes <= most) return true;
+  return LnSmem(S, p, rows, sums, warps).bytes <= 226 * 1024;
+}
+
+// Parts an example's rows are cut into, and whether they are a cluster (else the sums go through the workspace): as many CTAs as the
+// SMs hold at once, 16 rows each at least; clusters of more than eight, of which fewer fit the chip, only where eight would leave SMs idle.
+struct LnParts { int parts; bool cluster; };
+LnParts ln_parts(int B, int T, int blocks) {
+  const int sms = sm_count(), wanted = std::max(1, blocks * sms / B), most = ceil_div(T, 16);
+  if (wanted > 2 * kLnMaxParts && T >= 1024 * kLnMaxParts) return {std::min(wanted, T / 512), false};
+  return {std::max(1, std::min(std::min(wanted, most), 8 * B >= sms ? 8 : kLnMaxParts)), true};
+}
+
+// Working warps of a block and blocks per SM, by the registers that a lane's columns take: four of each in the backward pass, two in the
+// forward pass.
+constexpr int ln_columns(int NP, int es) { return NP * 16 / es; }
+struct LnBlock { int warps, blocks; };
+constexpr LnBlock ln_back_block(int columns, bool widest) {
+  return widest ? LnBlock{16, 1} : columns > 24 ? LnBlock{10, 1} : columns > 16 ? LnBlock{14, 1} : columns > 8 ? LnBlock{8, 2} : LnBlock{8, 3};
+}
+constexpr LnBlock ln_forward_block(bool widest) { return widest ? LnBlock{16, 1} : LnBlock{8, 2}; }
+
+template <typename T, int NP, bool kAligned, bool kWidest>
+dp_status ln_back_launch(LnBackward& P, int B, LnParts parts, cudaStream_t st) {
+  constexpr LnBlock kBlock = ln_back_block(ln_columns(NP, sizeof(T)), kWidest);
+  auto* kernel = ln_backward_kernel<T, NP, kAligned, (kBlock.warps + 1) * 32, kBlock.blocks>;
+  const int warps = P.S.W > 1 ? kBlock.warps / P.S.W * P.S.W : kBlock.warps;
+  P.S.columns = ln_columns(NP, sizeof(T));
+  if (!ln_fit(P.S, P.p, 2, true, warps, kBlock.blocks, kAligned)) return DP_ERR_UNSUPPORTED;
+  const dp_status r = ln_smem_setup(kernel);
+  if (r != DP_OK) return r;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(B) * unsigned(P.parts));
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem.bytes;
+  cfg.blockDim = dim3((warps + (kAligned ? 1 : 0)) * 32);
+  cfg.dynamicSmemBytes = LnSmem(P.S, P.p, 2, true, warps).bytes;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim = {cluster ? unsigned(P.parts) : 1u, 1u, 1u};
+  attr[0].val.clusterDim = {parts.cluster ? unsigned(P.parts) : 1u, 1u, 1u};
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   DP_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, P));
@@ -570,45 +677,58 @@ dp_status ln_back_launch(LnBackward& P, int B, int threads, bool cluster, cudaSt
   return DP_OK;
 }
 
-// Threads: as many whole rows of pieces as fill most of a block, 256 or so; wide rows take 512 threads and several pieces each.
-template <typename T>
-dp_status ln_back(LnBackward& P, int B, bool cluster, cudaStream_t st) {
-  const int pieces = ceil_div(P.p * int(sizeof(T)), 16);
-  if (pieces <= 512) {
-    int best = 0, used = 0;
-    for (int threads = 128; threads <= 512; threads += 32) {
-      if (threads < pieces) continue;
-      const int score = threads / pieces * pieces * 1024 / threads - std::abs(threads - 256) / 4;
-      if (!best || score > used) { best = threads; used = score; }
-    }
-    return best <= 256 ? ln_back_launch<T, 1, 256>(P, B, best, cluster, st) : ln_back_launch<T, 1, 512>(P, B, best, cluster, st);
-  }
-  switch (ceil_div(pieces, 512)) {
-    case 2: return ln_back_launch<T, 2, 512>(P, B, 512, cluster, st);
-    case 3: return ln_back_launch<T, 3, 512>(P, B, 512, cluster, st);
-    case 4: return ln_back_launch<T, 4, 512>(P, B, 512, cluster, st);
-    default: return ln_back_launch<T, 8, 512>(P, B, 512, cluster, st);
-  }
-}
-
-template <typename T, int NV, bool kVec>
-dp_status ln_fwd_launch(const LnForward& P, cudaStream_t st) {
-  const int threads = std::max(kLnThreads, P.W * 32), groups = threads / 32 / P.W;
-  const unsigned blocks = unsigned(std::min<long long>((P.rows + groups - 1) / groups, 1 << 20));
-  if (threads == 512) ln_forward_kernel<T, NV, kVec, 512><<<blocks, threads, 0, st>>>(P);
-  else ln_forward_kernel<T, NV, kVec, 256><<<blocks, threads, 0, st>>>(P);
+template <typename T, int NP, bool kAligned, bool kWidest>
+dp_status ln_fwd_launch(LnForward& P, cudaStream_t st) {
+  constexpr LnBlock kBlock = ln_forward_block(kWidest);
+  auto* kernel = ln_forward_kernel<T, NP, kAligned, (kBlock.warps + 1) * 32, kBlock.blocks>;
+  const int warps = P.S.W > 1 ? kBlock.warps / P.S.W * P.S.W : kBlock.warps;
+  P.S.columns = ln_columns(NP, sizeof(T));
+  if (!ln_fit(P.S, P.p, 1, false, warps, kBlock.blocks, kAligned)) return DP_ERR_UNSUPPORTED;
+  const dp_status r = ln_smem_setup(kernel);
+  if (r != DP_OK) return r;
+  const long long blocks = std::min((P.rows + P.S.groups - 1) / P.S.groups, (long long)kBlock.blocks * sm_count());
+  kernel<<<unsigned(blocks), (warps + (kAligned ? 1 : 0)) * 32, LnSmem(P.S, P.p, 1, false, warps).bytes, st>>>(P);
   DP_LAUNCH_OK();
   return DP_OK;
 }
 
-template <typename T, bool kVec>
-dp_status ln_fwd_nv(const LnForward& P, cudaStream_t st) {
-  switch (ceil_div(P.p, 8 * 32 * P.W)) {
-    case 1: return ln_fwd_launch<T, 1, kVec>(P, st);
-    case 2: return ln_fwd_launch<T, 2, kVec>(P, st);
-    case 3: return ln_fwd_launch<T, 3, kVec>(P, st);
-    default: return ln_fwd_launch<T, 4, kVec>(P, st);
+// f.template run<T, NP, kAligned, kWidest>() for the pieces per lane at hand
+template <typename T, bool kAligned, typename F>
+dp_status ln_dispatch(int pieces, bool widest, F f) {
+  if (widest) return f.template run<T, sizeof(T) == 4 ? 8 : 4, kAligned, true>();
+  switch (pieces) {
+    case 1: return f.template run<T, 1, kAligned, false>();
+    case 2: return f.template run<T, 2, kAligned, false>();
+    case 3: return f.template run<T, sizeof(T) == 4 ? 4 : 3, kAligned, false>();
+    case 4: return f.template run<T, 4, kAligned, false>();
+    case 6: return f.template run<T, sizeof(T) == 4 ? 6 : 4, kAligned, false>();
+    default: return f.template run<T, sizeof(T) == 4 ? 8 : 4, kAligned, false>();
   }
+}
+
+struct RunForward {
+  LnForward& P;
+  cudaStream_t st;
+  template <typename T, int NP, bool kAligned, bool kWidest>
+  dp_status run() { return ln_fwd_launch<T, NP, kAligned, kWidest>(P, st); }
+};
+struct RunBackward {
+  LnBackward& P;
+  int B;
+  LnParts parts;
+  cudaStream_t st;
+  template <typename T, int NP, bool kAligned, bool kWidest>
+  dp_status run() { return ln_back_launch<T, NP, kAligned, kWidest>(P, B, parts, st); }
+};
+template <typename F>
+dp_status ln_run(dp_dtype dt, bool aligned, int pieces, bool widest, F f) {
+  if (dt == DP_F32) return aligned ? ln_dispatch<float, true>(pieces, widest, f) : ln_dispatch<float, false>(pieces, widest, f);
+  return aligned ? ln_dispatch<__nv_bfloat16, true>(pieces, widest, f) : ln_dispatch<__nv_bfloat16, false>(pieces, widest, f);
+}
+
+LnParts ln_parts_of(int B, int T, int p, int es) {
+  const LnShape S = ln_shape(p, es);
+  return ln_parts(B, T, ln_back_block(ln_columns(ln_pieces(S, p, es), es), S.W == 16).blocks);
 }
 
 bool known_dtype(int dt) { return dt == DP_F32 || dt == DP_BF16; }
@@ -632,27 +752,34 @@ dp_status dp_layernorm(const void* X, int64_t ldx, dp_dtype dt, int64_t rows, in
   if ((Y && ldy < p) || (X_hat && ldh < p) || !known_dtype(dt) || !known_dtype(param_dt)) return DP_ERR_INVALID_ARG;
   if (!std::isfinite(eps) || eps < 0.f || (Y && Y == X_hat)) return DP_ERR_INVALID_ARG;
   if ((Y == X && ldy != ldx) || (X_hat == X && ldh != ldx)) return DP_ERR_INVALID_ARG;
-  if (p > kLnMaxCols || rows > (int64_t(1) << 40)) return DP_ERR_UNSUPPORTED;
+  if (p > kLnMaxCols || rows > (int64_t(1) << 36)) return DP_ERR_UNSUPPORTED;
   const int es = dt == DP_F32 ? 4 : 2, ps = param_dt == DP_F32 ? 4 : 2;
   if (!on_boundary(es, X, Y, X_hat) || !on_boundary(ps, gain, shift) || !on_boundary(4, mean, rstd)) return DP_ERR_ALIGNMENT;
-  const bool vec = p % 8 == 0 && ln_vec(X, ldx, es) && ln_vec(Y, ldy, es) && ln_vec(X_hat, ldh, es) && ln_vec(gain, p, ps) &&
-                   ln_vec(shift, p, ps);
-  const LnForward P{X, ldx, gain, shift, param_dt, Y, ldy, X_hat, ldh, mean, rstd, rows, p, ln_warps(p, vec), eps};
-  const cudaStream_t st = (cudaStream_t)stream;
-  if (dt == DP_F32) return vec ? ln_fwd_nv<float, true>(P, st) : ln_fwd_nv<float, false>(P, st);
-  return vec ? ln_fwd_nv<__nv_bfloat16, true>(P, st) : ln_fwd_nv<__nv_bfloat16, false>(P, st);
+  LnForward P{};
+  P.X = X; P.ldx = ldx; P.gain = gain; P.shift = shift; P.param_dt = param_dt; P.Y = Y; P.ldy = ldy; P.H = X_hat; P.ldh = ldh;
+  P.mean = mean; P.rstd = rstd; P.rows = rows; P.p = p; P.eps = eps; P.wait_limit = g_wait_limit;
+  P.S = ln_shape(p, es);
+  const bool aligned = p * es % 16 == 0 && ln_vec(X, ldx, es);
+  P.whole = aligned && ldx == p;
+  P.vec_y = ln_vec(Y, ldy, es);
+  P.vec_h = ln_vec(X_hat, ldh, es);
+  return ln_run(dt, aligned, ln_pieces(P.S, p, es), P.S.W == 16, RunForward{P, (cudaStream_t)stream});
 }
 
 size_t dp_layernorm_backward_ws_bytes(int32_t B, int32_t T, int32_t p) {
   if (B <= 0 || T <= 0 || p <= 0 || p > kLnMaxCols) return 0;
-  const LnParts parts = ln_parts(B, T);
-  if (parts.cluster) return 0;
-  return ln_partial_bytes(parts, B, p) + align_up(size_t(B) * ceil_div(p, 128) * sizeof(float), 256);
+  size_t most = 0;                                    // of either type of G and X
+  for (const int es : {2, 4}) {
+    const LnParts parts = ln_parts_of(B, T, p, es);
+    if (!parts.cluster) most = std::max(most, ln_partial_bytes(parts, B, p) + align_up(size_t(B) * ceil_div(p, 128) * sizeof(float), 256));
+  }
+  return most;
 }
 
 dp_status dp_layernorm_backward(const void* G, int64_t ldg, const void* X, int64_t ldx, dp_dtype dt, int32_t B, int32_t T, int32_t p,
                                 const void* gain, dp_dtype param_dt, const float* mean, const float* rstd, void* dX, int64_t lddx,
-                                float* gain_sums, float* shift_sums, float* sq, void* ws, size_t ws_bytes, void* stream) {
+                                float* gain_sums, float* shift_sums, float* sq, void* ws, size_t ws_bytes, int32_t* dev_status,
+                                void* stream) {
   if (!G || !X || !mean || !rstd || B <= 0 || T <= 0 || p <= 0 || ldg < p || ldx < p) return DP_ERR_INVALID_ARG;
   if ((dX && lddx < p) || !known_dtype(dt) || !known_dtype(param_dt)) return DP_ERR_INVALID_ARG;
   const bool sums = gain_sums || shift_sums || sq;
@@ -661,7 +788,7 @@ dp_status dp_layernorm_backward(const void* G, int64_t ldg, const void* X, int64
   const int es = dt == DP_F32 ? 4 : 2, ps = param_dt == DP_F32 ? 4 : 2;
   if (!on_boundary(es, G, X, dX) || !on_boundary(ps, gain) || !on_boundary(4, mean, rstd, gain_sums, shift_sums, sq)) return DP_ERR_ALIGNMENT;
   if (p > kLnMaxCols) return DP_ERR_UNSUPPORTED;
-  const LnParts parts = ln_parts(B, T);
+  const LnParts parts = ln_parts_of(B, T, p, es);
   if ((long long)B * parts.parts > 0x7fffffffLL) return DP_ERR_UNSUPPORTED;
   float* partials = nullptr;
   float* squares = nullptr;
@@ -674,11 +801,14 @@ dp_status dp_layernorm_backward(const void* G, int64_t ldg, const void* X, int64
   LnBackward P{};
   P.G = G; P.ldg = ldg; P.X = X; P.ldx = ldx; P.gain = gain; P.param_dt = param_dt; P.mean = mean; P.rstd = rstd; P.dX = dX; P.lddx = lddx;
   P.gain_sums = gain_sums; P.shift_sums = shift_sums; P.sq = sq; P.partials = partials;
-  P.T = T; P.p = p; P.parts = parts.parts;
-  P.bulk = p % 8 == 0 && ln_vec(G, ldg, es) && ln_vec(X, ldx, es);
-  P.vec_out = p % 8 == 0 && ln_vec(dX, lddx, es);
+  P.T = T; P.p = p; P.parts = parts.parts; P.dev_status = dev_status; P.wait_limit = g_wait_limit;
+  P.S = ln_shape(p, es);
+  const bool aligned = p * es % 16 == 0 && ln_vec(G, ldg, es) && ln_vec(X, ldx, es);
+  P.whole_g = aligned && ldg == p;
+  P.whole_x = aligned && ldx == p;
+  P.vec_out = ln_vec(dX, lddx, es);
   const cudaStream_t st = (cudaStream_t)stream;
-  const dp_status r = dt == DP_F32 ? ln_back<float>(P, B, parts.cluster, st) : ln_back<__nv_bfloat16>(P, B, parts.cluster, st);
+  const dp_status r = ln_run(dt, aligned, ln_pieces(P.S, p, es), P.S.W == 16, RunBackward{P, B, parts, st});
   if (r != DP_OK || !partials) return r;
   const int slabs = ceil_div(p, 128);
   ln_sums_kernel<<<dim3(slabs, B), 128, 0, st>>>(partials, parts.parts, p, gain_sums, shift_sums, squares);

@@ -374,34 +374,35 @@ PyObject* layernorm(PyObject*, PyObject* const* a, Py_ssize_t na) {
   return PyLong_FromLong(long(r));
 }
 
-// (address, G, X, gain, mean, rstd, dX, gain_sums, shift_sums, sq, ws, p, stream)
+// (address, G, X, gain, mean, rstd, dX, gain_sums, shift_sums, sq, ws, dev_status, p, stream)
 PyObject* layernorm_backward(PyObject*, PyObject* const* a, Py_ssize_t na) {
-  if (na != 13) { PyErr_SetString(PyExc_TypeError, "layernorm_backward takes 13 arguments"); return nullptr; }
+  if (na != 14) { PyErr_SetString(PyExc_TypeError, "layernorm_backward takes 14 arguments"); return nullptr; }
   const auto call = function<decltype(&dp_layernorm_backward)>(a[0]);
-  const at::Tensor* t[10];
-  enum { G, X, GAIN, MEAN, RSTD, DX, GS, SS, SQ, WS };
+  const at::Tensor* t[11];
+  enum { G, X, GAIN, MEAN, RSTD, DX, GS, SS, SQ, WS, STATUS };
   int64_t p, ldg, ldx, ldd;
   int32_t param;
   void* st;
-  if (!call || !here(a + 1, 10, t) || !t[G] || t[G]->dim() != 3 || dtype_of(*t[G]) == kOther || !t[X] || !t[MEAN] || !t[RSTD]) Py_RETURN_NONE;
+  if (!call || !here(a + 1, 11, t) || !t[G] || t[G]->dim() != 3 || dtype_of(*t[G]) == kOther || !t[X] || !t[MEAN] || !t[RSTD]) Py_RETURN_NONE;
   const auto type = t[G]->scalar_type();
   const int64_t B = t[G]->size(0), T = t[G]->size(1);
-  if (!whole(a[11], t[G]->size(2), &p) || !stream_of(a[12], &st) || p <= 0 || p > INT32_MAX || B > INT32_MAX || T > INT32_MAX) Py_RETURN_NONE;
+  if (!whole(a[12], t[G]->size(2), &p) || !stream_of(a[13], &st) || p <= 0 || p > INT32_MAX || B > INT32_MAX || T > INT32_MAX) Py_RETURN_NONE;
   if (!norm_params(t + GAIN, 1, p, &param) || !spaced(t[G], B * T, p, type, &ldg) || !spaced(t[X], B * T, p, type, &ldx) ||
       !spaced(t[DX], B * T, p, type, &ldd) || !dense(t[MEAN], B * T, at::kFloat) || !dense(t[RSTD], B * T, at::kFloat) ||
       !dense(t[GS], B * p, at::kFloat) || !dense(t[SS], B * p, at::kFloat) || !dense(t[SQ], B, at::kFloat) ||
-      (t[WS] && !t[WS]->is_contiguous()))
+      !dense(t[STATUS], 1, at::kInt) || (t[WS] && !t[WS]->is_contiguous()))
     Py_RETURN_NONE;
   const void *g = pointer<const void>(t[G]), *x = pointer<const void>(t[X]), *gain = pointer<const void>(t[GAIN]);
   const float *mean = pointer<const float>(t[MEAN]), *rstd = pointer<const float>(t[RSTD]);
   void *dx = pointer<void>(t[DX]), *ws = pointer<void>(t[WS]);
+  int32_t* status = pointer<int32_t>(t[STATUS]);
   float *gs = pointer<float>(t[GS]), *ss = pointer<float>(t[SS]), *sq = pointer<float>(t[SQ]);
   const size_t bytes = t[WS] ? t[WS]->nbytes() : 0;
   dp_status r;
   {
     const Unlock unlock;
     r = call(g, ldg, x, ldx, dp_dtype(dtype_of(*t[G])), int32_t(B), int32_t(T), int32_t(p), gain, dp_dtype(param), mean, rstd, dx, ldd, gs,
-             ss, sq, ws, bytes, st);
+             ss, sq, ws, bytes, status, st);
   }
   return PyLong_FromLong(long(r));
 }

@@ -98,6 +98,16 @@ __device__ __forceinline__ bool mbar_wait_relaxed(uint64_t* bar, uint32_t parity
   return true;
 }
 
+// The same where the block waits for its own copies and warps only, with no other role to tell.
+__device__ __forceinline__ bool mbar_wait_own(uint64_t* bar, uint32_t parity, long long limit) {
+  if (mbar_try_wait(bar, parity)) return true;
+  if (limit <= 0) return false;
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity))
+    if (clock64() - t0 > limit) return false;
+  return true;
+}
+
 // ---- the same primitives on 32-bit shared-memory addresses --------------------------------
 // The single-thread roles (TMA producer, MMA issuer) sit on the latency chain of every pipeline
 // stage, so their per-stage instruction count matters: they keep shared addresses as 32-bit

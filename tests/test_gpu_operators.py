@@ -137,7 +137,9 @@ def test_layernorm_backward(B, T, p, dtype, params, pad, offset):
     dx = tensor((B, T, p), dt, 9, pitch=p + pad, offset=offset)
     gs, ss = torch.full((B, p), 7.0, device="cuda"), torch.full((B, p), 7.0, device="cuda")
     sq = torch.full((B,), 0.5, device="cuda")
-    dp.dp_layernorm_backward(g, x, gain, mean, rstd, dX=dx, gain_sums=gs, shift_sums=ss, sq=sq)
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    dp.dp_layernorm_backward(g, x, gain, mean, rstd, dX=dx, gain_sums=gs, shift_sums=ss, sq=sq, dev_status=st)
+    assert int(st.item()) == 0
     m, r = f64(mean), f64(rstd)
     wdx, wgs, wss, wsq = O.layernorm_backward(f64(g), f64(x), f64(gain), m, r)
     hat = (f64(x) - m[..., None]) * r[..., None]

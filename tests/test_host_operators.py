@@ -42,7 +42,7 @@ def test_layernorm(lib, kw, want):
 
 def backward(lib, **kw):
     a = dict(G=A[0], ldg=64, X=A[1], ldx=64, dt=1, B=3, T=20, p=64, gain=A[2], pdt=0, mean=A[3], rstd=A[4], dX=A[5], lddx=64, gs=A[6],
-             ss=A[7], sq=A[8], ws=None, n=0)
+             ss=A[7], sq=A[8], ws=None, n=0, status=None)
     assert not set(kw) - set(a)
     a.update(kw)
     return lib.dp_layernorm_backward(*a.values(), None)
