@@ -303,8 +303,7 @@ ln_forward_kernel(const LnForward P) {
     F2 v[NP][H];
     if (kAligned) {
       R.template open<false>(smem + size_t(b) * at.tile + size_t(mine ? group : 0) * S.pitch, mine, v);
-      __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(empty + b);        // the row is in registers
+      ptx::release_to_copies(empty + b, lane);           // the row is in registers
       if (++b == S.buffers) { b = 0; phase ^= 1; }
     } else {
       R.template open<false>(X + (mine ? row : r0) * P.ldx, mine, v);
@@ -463,8 +462,7 @@ ln_backward_kernel(const LnBackward P) {
         const uint8_t* from = smem + size_t(b) * at.tile + size_t(mine ? group : 0) * S.pitch;
         R.template open<true>(from, mine, g);
         R.template open<true>(from + size_t(S.groups) * S.pitch, mine, c);
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(empty + b);      // the row is in registers
+        ptx::release_to_copies(empty + b, lane);         // the row is in registers
         if (++b == S.buffers) { b = 0; phase ^= 1; }
       } else {
         R.template open<true>(G + row * P.ldg, mine, g);

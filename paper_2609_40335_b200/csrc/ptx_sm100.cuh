@@ -220,6 +220,14 @@ __device__ __forceinline__ void fence_proxy_async_smem() {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
+// A warp gives a buffer that it has read by ordinary loads back to the thread that fills it by bulk copies.  All lanes call it.  The
+// fence keeps the copy behind the loads: without it a warp whose loads still queued behind its stores read the next copy's bytes.
+__device__ __forceinline__ void release_to_copies(uint64_t* bar, int lane) {
+  fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) mbar_arrive(bar);
+}
+
 // ------------------------------------------------------------------- tcgen05
 __device__ __forceinline__ void tmem_alloc(uint32_t* smem_result, uint32_t ncols) {
   asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
