@@ -358,7 +358,7 @@ dp_status dp_layernorm(const void* X, int64_t ldx, dp_dtype dt, int64_t rows, in
  *   sq[i] += ||gain_sums[i]||^2 + ||shift_sums[i]||^2   (both parameters' blocks of Eq. 6)         [dev, B floats, or NULL]
  * The sums are the v_i of dp_clip_accumulate_vectors, so their clipped sum is that call on them with T = 1 (DP_F32): G and X are
  * read once for dX, norms and sums.  dX may be G or X itself (same pitch).  Workspace: dp_layernorm_backward_ws_bytes (0
- * unless few examples have long sequences). */
+ * unless few examples have long sequences).  dev_status [dev, or NULL]: DP_DEV_TIMEOUT if a wait inside ran out. */
 dp_status dp_layernorm_backward(const void* G, int64_t ldg, const void* X, int64_t ldx, dp_dtype dt, int32_t B, int32_t T, int32_t p,
                                 const void* gain, dp_dtype param_dt, const float* mean, const float* rstd, void* dX, int64_t lddx,
                                 float* gain_sums, float* shift_sums, float* sq, void* ws, size_t ws_bytes, int32_t* dev_status,
@@ -374,8 +374,10 @@ size_t dp_layernorm_backward_ws_bytes(int32_t B, int32_t T, int32_t p);
  *   h_i = beta * ((l_c - ref_c) - (l_r - ref_r)),   loss[i] = -(1 - smoothing) log s(h_i) - smoothing log s(-h_i)
  * (s the logistic function), logp [dev, (B, 2) floats] = l, and G [dev, (2*B*T, V) of dt] = scale * d loss / d logits, the G of an
  * LM head in dp_ghost_norms and dp_clip_accumulate* with sequences of 2*T tokens.  loss, logp, G: each may be NULL, not all; G may
- * be logits itself (same pitch).  Columns past V are neither read nor written.  Any alignment of whole elements works; beta >= 0,
- * 0 <= smoothing <= 1. */
+ * be logits itself (same pitch).  Columns past V are neither read nor written.  Any alignment of whole elements works; rows of G that lie
+ * on their 16 bytes as those of logits do take the vector path.  A row that counts needs a logit above -2.3e38 (its softmax is NaN
+ * otherwise; -inf and the type's lowest value are fine beside one).  beta >= 0, 0 <= smoothing <= 1; 2*B*T < 2^31; ws on an
+ * 8-byte boundary. */
 dp_status dp_preference_loss(const void* logits, int64_t ldl, dp_dtype dt, int32_t B, int32_t T, int32_t V, const int32_t* targets,
                              const float* ref_logp, float beta, float smoothing, float scale, float* loss, float* logp, void* G,
                              int64_t ldg, void* ws, size_t ws_bytes, int32_t* dev_status, void* stream);

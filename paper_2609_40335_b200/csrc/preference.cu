@@ -8,17 +8,17 @@
 // rescaled when the maximum moves).  The gradient needs both sequences' sums, so a row is read again for it; rows whose target is
 // masked are not read, their gradient is 0.
 //
-// Two forms.  pair_kernel: a cluster of up to eight CTAs per pair, one launch, no workspace; the rows of a small call stay in the caches in
-// between.  preference_kernel: persistent CTAs draw rows in order, statistics of later pairs alternating with gradients of earlier ones, so
-// that a row's second reading comes soon enough after the first to find it in the L2: the call then reads logits once from memory and
-// writes the gradient once.  The CTA that finishes a pair's last row adds up its sequences.
+// Two launches: statistics of every row, then gradients, whose launch overlaps the first one's end and whose rows go from the last to the
+// first, so that the rows read last are still in the L2.  A CTA of the second adds up its pair itself, in a fixed order: 2T numbers
+// against a row of logits, and no counters, no third launch.  Both are bound by memory and, in the first, by the rate of ex2 (16 a
+// clock and SM: 46 us of the 76 for 206 M logits).  Measured with logits and G of (16, 2 x 128, 50257) in bf16 (412 MB each): statistics
+// 76 us, both 198; a copy's time for two reads and a write is 190, for one read 127.  Persistent CTAs that draw statistics of later pairs in
+// turn with gradients of earlier ones, to find every second reading in the L2, took 195 to 221 (reads and writes share the
+// machine worse, and the waits between rows show); clusters of eight CTAs per pair 41 us against 18 at (2, 2 x 16, 50257).
 //
 // Exponents are x log2 e - c and a row's sum is fp32; a token's log-probability is ((x_target log2 e - c) - log2(sum)) ln 2,
-// without the cancellation of x - (c ln 2 + log(sum)); sequences are added up in 64 bits, since h is
-// a small difference of long sums.
-#include <cooperative_groups.h>
-
-#include <algorithm>
+// without the cancellation of x - (c ln 2 + log(sum)), and held in 64 bits as its sequence's sum is, since h is a small difference
+// of long sums.
 #include <cmath>
 
 #include "dp_common.cuh"
@@ -27,9 +27,7 @@ namespace dpg {
 
 namespace {
 
-namespace cg = cooperative_groups;
-
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
 
 // 16 bytes of logits: eight bf16 or four fp32
 template <typename T> struct Quad;
@@ -52,6 +50,19 @@ template <> struct Quad<__nv_bfloat16> {
     return q;
   }
   static __device__ __forceinline__ __nv_bfloat16 round(float v) { return __float2bfloat16_rn(v); }
+  // largest of U pieces (NaN apart), two values at a time
+  template <int U>
+  static __device__ __forceinline__ float top(const uint4 (&q)[U]) {
+    __nv_bfloat162 m = two(q[0].x);
+#pragma unroll
+    for (int u = 0; u < U; ++u) m = __hmax2(m, __hmax2(__hmax2(two(q[u].x), two(q[u].y)), __hmax2(two(q[u].z), two(q[u].w))));
+    return fmaxf(__low2float(m), __high2float(m));
+  }
+  static __device__ __forceinline__ __nv_bfloat162 two(uint32_t w) {
+    __nv_bfloat162 h;
+    memcpy(&h, &w, 4);
+    return h;
+  }
 };
 template <> struct Quad<float> {
   static constexpr int N = 4;
@@ -62,6 +73,17 @@ template <> struct Quad<float> {
     return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
   }
   static __device__ __forceinline__ float round(float v) { return v; }
+  template <int U>
+  static __device__ __forceinline__ float top(const uint4 (&q)[U]) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float v[4];
+      unpack(q[u], v);
+      m = fmaxf(m, fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])));
+    }
+    return m;
+  }
 };
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -70,27 +92,37 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
-// Sum of 2^(x log2 e - c) over the values seen so far, c = (their maximum) * log2 e as rounded; -inf and 0 of none.  With the
-// rounded c as the reference everywhere its rounding cancels, and an exponent is one FMA.
+// Sum of 2^(x log2 e - c) over the values seen so far; c a reference near their maximum * log2 e, -inf of none.  The reference moves
+// only when a value exceeds it by 2: nearly every warp would meet a new maximum in every piece of a row otherwise.  An exponent is
+// one FMA, whose rounding is a term's error: 2^-24 of the exponent, which is at most 2 for the largest terms (a bound of 16 took the
+// same time and gave fp32 gradients twice the error).  The rounding of c cancels wherever the same c is used.
 struct Softmax {
   float c, s;
   static __device__ __forceinline__ float exponent(float x, float c) { return fmaf(x, kLog2e, c == -INFINITY ? 0.f : -c); }
+  __device__ __forceinline__ void reach(float top) {     // the largest of the next values, in units of c
+    if (top > c + 2.f) { s *= exp2_fast(c - top); c = top; }
+  }
   __device__ __forceinline__ void add(float x) {
-    const float top = x * kLog2e;
-    if (top > c) { s *= exp2_fast(c - top); c = top; }
+    reach(x * kLog2e);
     s += exp2_fast(exponent(x, c));
   }
-  template <int N>
-  __device__ __forceinline__ void add(const float (&v)[N]) {
-    float top = v[0];
-#pragma unroll
-    for (int e = 1; e < N; ++e) top = fmaxf(top, v[e]);
-    top *= kLog2e;
-    if (top > c) { s *= exp2_fast(c - top); c = top; }
+  // pieces of 16 bytes
+  template <typename T, int U>
+  __device__ __forceinline__ void add(const uint4 (&q)[U]) {
+    constexpr int N = Quad<T>::N;
+    reach(Quad<T>::template top<U>(q) * kLog2e);
     const float minus = c == -INFINITY ? 0.f : -c;
     float t[N];
 #pragma unroll
-    for (int e = 0; e < N; ++e) t[e] = exp2_fast(fmaf(v[e], kLog2e, minus));
+    for (int u = 0; u < U; ++u) {
+      float v[N];
+      Quad<T>::unpack(q[u], v);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float p = exp2_fast(fmaf(v[e], kLog2e, minus));
+        t[e] = u ? t[e] + p : p;
+      }
+    }
 #pragma unroll
     for (int w = N / 2; w > 0; w /= 2)
 #pragma unroll
@@ -111,14 +143,10 @@ struct PrefParams {
   const int32_t* targets;
   const float* ref;
   float* loss; float* logp;
-  float* row_logp; float* row_c; float* row_inv;       // [2BT] workspace
-  float* coef;                                         // [2B]
-  uint32_t* ticket; uint32_t* done; uint32_t* ready;   // the next row to draw; rows finished and sums made, [B] each
+  double* row_logp; float* row_c; float* row_inv;      // [2BT] workspace
   int* dev_status;
   int B, T, V;
-  long long rows, lag;                                 // a gradient follows the statistics of `lag` rows later
   float beta, smoothing, scale;
-  long long wait_limit;
 };
 
 // a row's target, or -1 where the row does not count
@@ -149,17 +177,11 @@ __device__ __forceinline__ Softmax scan_row(const T* x, int V, int tid, int n) {
     uint4 q[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) q[u] = xq[k + u * n];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      float v[N];
-      Quad<T>::unpack(q[u], v);
-      acc.add(v);
-    }
+    acc.add<T>(q);
   }
   for (; k < quads; k += n) {
-    float v[N];
-    Quad<T>::unpack(xq[k], v);
-    acc.add(v);
+    const uint4 q[1] = {xq[k]};
+    acc.add<T>(q);
   }
   for (int c = tid; c < head; c += n) acc.add(to_f32(x[c]));
   for (int c = head + quads * N + tid; c < V; c += n) acc.add(to_f32(x[c]));
@@ -175,7 +197,11 @@ __device__ __forceinline__ Softmax warp_join(Softmax a) {
   return a;
 }
 
-__device__ __forceinline__ float token_logp(float x, const Softmax& a) { return (Softmax::exponent(x, a.c) - log2f(a.s)) * kLn2; }
+// in 64 bits: thousands of these are added up, and the difference of two such sums is what the loss is of
+__device__ __forceinline__ double token_logp(float x, const Softmax& a) {
+  const double c = a.c == -INFINITY ? 0.0 : double(a.c);
+  return (fma(double(x), double(kLog2e), -c) - log2(double(a.s))) * 0.6931471805599453;
+}
 
 // This thread's share of a row's gradient: f = c / (sum of exponentials).  target < 0: zeros.
 template <typename T>
@@ -243,190 +269,110 @@ __device__ __forceinline__ double warp_sum(double v) {
   return v;
 }
 
-// ---- small calls: a cluster per pair ---------------------------------------------------------------
+constexpr int kThreads = 512, kWarps = kThreads / 32;
 
-constexpr int kPairThreads = 512;
-constexpr int kPairRows = 512;             // rows of a CTA, at most
-constexpr int kWarpRow = 2048;             // vocabularies up to this: a warp per row, else the CTA
+// A warp per row and kWarps rows per CTA where rows are short and many, else a CTA per row.  Statistics and gradients of 4096 bf16 rows, warps
+// against CTAs: 14 us against 43 with 1024 logits each, 18 against 45 with 2048, 25 against 49 with 4096, 37 against 57 with 8192; of 128 rows,
+// which leave most SMs without a warp of the first form: 12 against 10 with 2048, 25 against 12 with 8192.
+inline bool row_by_warp(long long rows, int V) { return V <= 8192 && rows * 512 > (long long)V * sm_count(); }
 
-template <typename T>
-__global__ void __launch_bounds__(kPairThreads)
-pair_kernel(const PrefParams P) {
-  __shared__ float row_c[kPairRows], row_inv[kPairRows], row_logp[kPairRows], sc[kPairThreads / 32], ss[kPairThreads / 32];
-  __shared__ double part[2];
-  __shared__ float factor;
-  cg::cluster_group cluster = cg::this_cluster();
-  const int ctas = cluster.num_blocks(), rank = cluster.block_rank(), pair = blockIdx.x / ctas;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int r0 = 2 * P.T * rank / ctas, n = 2 * P.T * (rank + 1) / ctas - r0;
-  const long long first = 2LL * P.T * pair + r0;
-  const T* logits = static_cast<const T*>(P.logits);
-  const bool by_warp = P.V <= kWarpRow;
-  for (int r = by_warp ? warp : 0; r < n; r += by_warp ? kPairThreads / 32 : 1) {
-    const T* x = logits + (first + r) * P.ldl;
-    const int target = row_target(P, first + r, by_warp ? lane == 0 : tid == 0);
-    Softmax a{-INFINITY, 0.f};
-    if (target >= 0) a = warp_join(scan_row(x, P.V, by_warp ? lane : tid, by_warp ? 32 : kPairThreads));
-    if (!by_warp) {
-      if (lane == 0) { sc[warp] = a.c; ss[warp] = a.s; }
-      __syncthreads();
-      a = Softmax{sc[0], ss[0]};
-      for (int w = 1; w < kPairThreads / 32; ++w) a.join(sc[w], ss[w]);
-      __syncthreads();
-    }
-    if (by_warp ? lane == 0 : tid == 0) {
-      row_c[r] = a.c;
-      row_inv[r] = target < 0 ? 0.f : 1.f / a.s;
-      row_logp[r] = target < 0 ? 0.f : token_logp(to_f32(x[target]), a);
-    }
+// This CTA's place: a block of rows of one pair, a warp or all of it on a row (known at compile time: so are the strides of the loops).
+template <bool kByWarp>
+struct Place {
+  static constexpr int kRows = kByWarp ? kWarps : 1, kLanes = kByWarp ? 32 : kThreads;
+  int pair, first;                         // the block's first row within the pair
+  int at, who;                             // this thread's row within the pair (2T or above: none) and its number on it
+  __device__ __forceinline__ Place(const PrefParams& P, unsigned block) {
+    const unsigned blocks = unsigned(2 * P.T + kRows - 1) / kRows;
+    pair = int(block / blocks);
+    first = int(block % blocks) * kRows;
+    at = first + (kByWarp ? int(threadIdx.x >> 5) : 0);
+    who = kByWarp ? int(threadIdx.x & 31) : int(threadIdx.x);
   }
-  __syncthreads();
-  if (warp < 2) {                                      // warp q: this CTA's rows of sequence q
-    double s = 0.0;
-    for (int r = lane; r < n; r += 32)
-      if ((r0 + r >= P.T) == (warp == 1)) s += double(row_logp[r]);
-    s = warp_sum(s);
-    if (lane == 0) part[warp] = s;
+};
+
+template <typename T, bool kByWarp>
+__global__ void __launch_bounds__(kThreads, 2048 / kThreads)
+row_stats_kernel(const PrefParams P) {
+  __shared__ float sc[kWarps], ss[kWarps];
+  cudaTriggerProgrammaticLaunchCompletion();             // the next kernel waits for this one's end itself
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const Place<kByWarp> p(P, blockIdx.x);
+  const bool here = p.at < 2 * P.T;
+  const long long row = 2LL * P.T * p.pair + p.at;
+  const int target = here ? row_target(P, row, p.who == 0) : -1;
+  const T* x = static_cast<const T*>(P.logits) + row * P.ldl;
+  Softmax a{-INFINITY, 0.f};
+  if (target >= 0) a = warp_join(scan_row(x, P.V, p.who, p.kLanes));
+  if (!kByWarp) {
+    if (lane == 0) { sc[warp] = a.c; ss[warp] = a.s; }
+    __syncthreads();
+    if (warp == 0) a = warp_join(lane < kWarps ? Softmax{sc[lane], ss[lane]} : Softmax{-INFINITY, 0.f});
   }
-  cluster.sync();
-  if (tid == 0) {
-    double lc = 0.0, lr = 0.0;
-    for (int k = 0; k < ctas; ++k) {
-      const double* other = cluster.map_shared_rank(part, k);
-      lc += other[0];
-      lr += other[1];
-    }
-    factor = pair_loss(P, pair, lc, lr, rank == 0);
+  if (here && p.who == 0) {
+    P.row_logp[row] = target < 0 ? 0.0 : token_logp(to_f32(x[target]), a);
+    P.row_c[row] = a.c;
+    P.row_inv[row] = target < 0 ? 0.f : 1.f / a.s;
   }
-  __syncthreads();
-  if (P.G) {
-    for (int r = by_warp ? warp : 0; r < n; r += by_warp ? kPairThreads / 32 : 1)
-      write_gradient(logits + (first + r) * P.ldl, static_cast<T*>(P.G) + (first + r) * P.ldg, P.V, row_target(P, first + r, false),
-                     r0 + r < P.T ? factor : -factor, row_c[r], row_inv[r], by_warp ? lane : tid, by_warp ? 32 : kPairThreads);
-  }
-  cluster.sync();                                      // no CTA leaves while its sums are read
 }
 
-// ---- large calls: rows in the order of their second reading -----------------------------------------
-
-constexpr int kRowThreads = 512, kRowBlocks = 2;       // per CTA, per SM
-
-// Which row the n-th draw is, and whether it is a gradient: `lag` statistics, then gradients and statistics in turn, then gradients.
-struct Draw { long long row; bool gradient; };
-__device__ __forceinline__ Draw draw_of(const PrefParams& P, long long n) {
-  if (!P.G || n < P.lag) return {n, false};
-  const long long u = n - P.lag, both = 2 * (P.rows - P.lag);
-  if (u >= both) return {P.rows - P.lag + (u - both), true};
-  return u & 1 ? Draw{P.lag + (u >> 1), false} : Draw{u >> 1, true};
-}
-
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads, kRowBlocks)
-preference_kernel(const PrefParams P) {
-  __shared__ float sc[kRowThreads / 32], ss[kRowThreads / 32];
-  __shared__ double part[2][kRowThreads / 32];
-  __shared__ uint32_t next;
-  __shared__ int last;
+// A pair's sequences added up, in a fixed order and by every CTA that needs them: its preferred rows' factor.
+__device__ __forceinline__ float factor_of(const PrefParams& P, int pair, bool write) {
+  __shared__ double part[2][kWarps];
   __shared__ float factor;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const long long draws = P.G ? 2 * P.rows : P.rows;
-  const int rows_of_pair = 2 * P.T;
-  long long n = blockIdx.x;                            // the first draws are the CTAs' own, the counter goes on behind them
-  while (n < draws) {
-    // the row after this one is drawn now: it comes later in the order than all that this one waits for
-    if (tid == 0) next = gridDim.x + atomicAdd(P.ticket, 1u);
-    const Draw d = draw_of(P, n);
-    const int pair = int(d.row / rows_of_pair), target = row_target(P, d.row, tid == 0 && !d.gradient);
-    const T* x = static_cast<const T*>(P.logits) + d.row * P.ldl;
-    if (!d.gradient) {
-      Softmax a{-INFINITY, 0.f};
-      if (target >= 0) {
-        a = warp_join(scan_row(x, P.V, tid, kRowThreads));
-        if (lane == 0) { sc[warp] = a.c; ss[warp] = a.s; }
-      }
-      __syncthreads();
-      if (tid == 0) {
-        if (target >= 0) {
-          a = Softmax{sc[0], ss[0]};
-          for (int w = 1; w < kRowThreads / 32; ++w) a.join(sc[w], ss[w]);
-        }
-        P.row_logp[d.row] = target < 0 ? 0.f : token_logp(to_f32(x[target]), a);
-        P.row_c[d.row] = a.c;
-        P.row_inv[d.row] = target < 0 ? 0.f : 1.f / a.s;
-        __threadfence();                               // the row's values before the count
-        last = atomicAdd(P.done + pair, 1u) == uint32_t(rows_of_pair - 1);
-      }
-      __syncthreads();
-      if (last) {                                      // every row of the pair is there: its sums, in a fixed order
-        __threadfence();
-        const float* l = P.row_logp + (long long)pair * rows_of_pair;
-        double s[2] = {0.0, 0.0};
-        for (int t = tid; t < P.T; t += kRowThreads) { s[0] += double(__ldcg(l + t)); s[1] += double(__ldcg(l + P.T + t)); }
+  const double* l = P.row_logp + 2LL * P.T * pair;
+  double s[2] = {0.0, 0.0};
+  for (int t = tid; t < P.T; t += kThreads) { s[0] += l[t]; s[1] += l[P.T + t]; }
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          s[q] = warp_sum(s[q]);
-          if (lane == 0) part[q][warp] = s[q];
-        }
-        __syncthreads();
-        if (tid == 0) {
-          s[0] = s[1] = 0.0;
-          for (int w = 0; w < kRowThreads / 32; ++w) { s[0] += part[0][w]; s[1] += part[1][w]; }
-          const float c = pair_loss(P, pair, s[0], s[1], true);
-          P.coef[2 * pair] = c;
-          P.coef[2 * pair + 1] = -c;
-          __threadfence();
-          atomicExch(P.ready + pair, 1u);
-        }
-      }
-    } else {
-      if (tid == 0) {
-        // rows that this one waits for were drawn before it, by CTAs that wait for nothing
-        const long long t0 = clock64();
-        bool ok = true;
-        while (*reinterpret_cast<volatile uint32_t*>(P.ready + pair) == 0u) {
-          if (clock64() - t0 > P.wait_limit) { ok = false; break; }
-          __nanosleep(100);
-        }
-        if (!ok && P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
-        __threadfence();
-        factor = __ldcg(P.coef + d.row / P.T);
-      }
-      __syncthreads();
-      write_gradient(x, static_cast<T*>(P.G) + d.row * P.ldg, P.V, target, factor, __ldcg(P.row_c + d.row), __ldcg(P.row_inv + d.row), tid,
-                     kRowThreads);
-    }
-    __syncthreads();
-    n = next;
-    __syncthreads();
+  for (int q = 0; q < 2; ++q) {
+    s[q] = warp_sum(s[q]);
+    if (lane == 0) part[q][warp] = s[q];
   }
+  __syncthreads();
+  if (tid == 0) {
+    s[0] = s[1] = 0.0;
+    for (int w = 0; w < kWarps; ++w) { s[0] += part[0][w]; s[1] += part[1][w]; }
+    factor = pair_loss(P, pair, s[0], s[1], write);
+  }
+  __syncthreads();
+  return factor;
 }
 
-// Bytes of logits up to which a call takes the cluster form.
-constexpr long long kSmallCall = 24LL << 20;
+template <typename T, bool kByWarp>
+__global__ void __launch_bounds__(kThreads, 2048 / kThreads)
+row_gradient_kernel(const PrefParams P) {
+  const Place<kByWarp> p(P, gridDim.x - 1 - blockIdx.x);
+  cudaGridDependencySynchronize();
+  const float c = factor_of(P, p.pair, p.first == 0);
+  if (p.at >= 2 * P.T) return;
+  const long long row = 2LL * P.T * p.pair + p.at;
+  write_gradient(static_cast<const T*>(P.logits) + row * P.ldl, static_cast<T*>(P.G) + row * P.ldg, P.V, row_target(P, row, false),
+                 p.at < P.T ? c : -c, P.row_c[row], P.row_inv[row], p.who, p.kLanes);
+}
 
-template <typename T>
-dp_status pref_launch(PrefParams& P, cudaStream_t st) {
-  const int ctas = std::min(8, 2 * P.T);
-  if (2 * P.T <= kPairRows * ctas && P.rows * P.V * (long long)sizeof(T) <= kSmallCall) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(P.B) * unsigned(ctas));
-    cfg.blockDim = dim3(kPairThreads);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim = {unsigned(ctas), 1u, 1u};
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    DP_CUDA_OK(cudaLaunchKernelEx(&cfg, pair_kernel<T>, P));
-    ++g_kernel_launches;
-    return DP_OK;
-  }
-  const long long blocks = std::min(P.rows, (long long)kRowBlocks * sm_count());
-  // far enough behind that a pair's rows are done when its first gradient is drawn, no further: the L2 holds what lies between
-  P.lag = std::min(P.rows, 2LL * P.T + blocks);
-  DP_CUDA_OK(cudaMemsetAsync(P.ticket, 0, (1 + 2 * size_t(P.B)) * sizeof(uint32_t), st));
-  preference_kernel<T><<<unsigned(blocks), kRowThreads, 0, st>>>(P);
+__global__ void __launch_bounds__(kThreads) pair_loss_kernel(const PrefParams P) {
+  cudaGridDependencySynchronize();
+  factor_of(P, blockIdx.x, true);
+}
+
+template <typename T, bool kByWarp>
+dp_status pref_launch(const PrefParams& P, cudaStream_t st) {
+  constexpr int per = Place<kByWarp>::kRows;
+  const unsigned blocks = unsigned(P.B) * (unsigned(2 * P.T + per - 1) / per);
+  row_stats_kernel<T, kByWarp><<<blocks, kThreads, 0, st>>>(P);
   DP_LAUNCH_OK();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(P.G ? blocks : unsigned(P.B));
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  DP_CUDA_OK(cudaLaunchKernelEx(&cfg, P.G ? row_gradient_kernel<T, kByWarp> : pair_loss_kernel, P));
+  ++g_kernel_launches;
   return DP_OK;
 }
 
@@ -440,7 +386,7 @@ extern "C" {
 
 size_t dp_preference_loss_ws_bytes(int32_t B, int32_t T) {
   if (B <= 0 || T <= 0) return 0;
-  return align_up((3 * 2 * size_t(B) * size_t(T) + 2 * size_t(B) + 1 + 2 * size_t(B)) * sizeof(float), 256);
+  return align_up(2 * size_t(B) * size_t(T) * (sizeof(double) + 2 * sizeof(float)), 256);
 }
 
 dp_status dp_preference_loss(const void* logits, int64_t ldl, dp_dtype dt, int32_t B, int32_t T, int32_t V, const int32_t* targets,
@@ -451,18 +397,19 @@ dp_status dp_preference_loss(const void* logits, int64_t ldl, dp_dtype dt, int32
   if (dt != DP_F32 && dt != DP_BF16) return DP_ERR_INVALID_ARG;
   if (!std::isfinite(beta) || beta < 0.f || !(smoothing >= 0.f && smoothing <= 1.f) || !std::isfinite(scale)) return DP_ERR_INVALID_ARG;
   if (G == logits && ldg != ldl) return DP_ERR_INVALID_ARG;
-  if (2LL * B * T > (1LL << 30)) return DP_ERR_UNSUPPORTED;         // draws are counted in 32 bits
+  if (2LL * B * T > 0x7fffffffLL) return DP_ERR_UNSUPPORTED;
   const size_t es = dt == DP_F32 ? 4 : 2;
   if (!on_boundary(es, logits, G) || !on_boundary(4, targets, ref_logp, loss, logp)) return DP_ERR_ALIGNMENT;
   if (!ws || ws_bytes < dp_preference_loss_ws_bytes(B, T)) return DP_ERR_WORKSPACE;
-  if (!on_boundary(4, ws)) return DP_ERR_ALIGNMENT;
-  const size_t rows = 2 * size_t(B) * size_t(T);
-  float* f = static_cast<float*>(ws);
-  uint32_t* u = reinterpret_cast<uint32_t*>(f + 3 * rows + 2 * size_t(B));
-  PrefParams P{logits, ldl, G, ldg, targets, ref_logp, loss, logp, f, f + rows, f + 2 * rows, f + 3 * rows, u, u + 1, u + 1 + B, dev_status,
-               B, T, V, (long long)rows, 0, beta, smoothing, scale, g_wait_limit};
+  if (!on_boundary(8, ws)) return DP_ERR_ALIGNMENT;
+  const long long rows = 2LL * B * T;
+  double* l = static_cast<double*>(ws);
+  float* f = reinterpret_cast<float*>(l + rows);
+  PrefParams P{logits, ldl, G, ldg, targets, ref_logp, loss, logp, l, f, f + rows, dev_status,
+               B, T, V, beta, smoothing, scale};
   const cudaStream_t st = (cudaStream_t)stream;
-  return dt == DP_F32 ? pref_launch<float>(P, st) : pref_launch<__nv_bfloat16>(P, st);
+  if (row_by_warp(rows, V)) return dt == DP_F32 ? pref_launch<float, true>(P, st) : pref_launch<__nv_bfloat16, true>(P, st);
+  return dt == DP_F32 ? pref_launch<float, false>(P, st) : pref_launch<__nv_bfloat16, false>(P, st);
 }
 
 }  // extern "C"
