@@ -34,7 +34,7 @@
 // (cta_group::2) with 256 x 256 tiles; else single CTAs with 128 x 128 tiles, for calls with few tiles.  Roles: two producer
 // warps (TMA, 64-wide K steps of the left and the right operand), the MMA issuer, a relay (pairs: tells rank 0's issuer
 // that rank 1's half of a stage has landed), 16 epilogue warps; two accumulators, so adding up a chunk and the epilogue of a
-// tile overlap the next ones.
+// tile overlap the next ones.  Calls whose matrices all have at most 64 by 256 numbers take ns_small_kernel.
 #include <cuda.h>
 #include <cuda_fp16.h>
 
@@ -198,6 +198,14 @@ __device__ __forceinline__ void store_out(const NsMat& L, int dt, int row, int c
   }
 }
 
+// A call's launches overlap: the next one's CTAs start where this one's leave room, set themselves up and wait here for its end (and so,
+// since every CTA waits, for the ends of all before it).  132 us -> 99 for a
+// 128 x 128 in 17 launches, 206 -> 176 for the layers of a block of width 256.
+__device__ __forceinline__ void follow_the_launch_before() {
+  cudaTriggerProgrammaticLaunchCompletion();
+  cudaGridDependencySynchronize();
+}
+
 template <Product kProduct, bool kPair>
 __global__ void __launch_bounds__(kThreads, 1)
 ns_product_kernel(const __grid_constant__ NsParams P) {
@@ -247,6 +255,7 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
   if (kPair) ptx::cluster_sync_all();         // the partner's barriers exist before anyone arrives on them
   ptx::tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  follow_the_launch_before();
 
   if (warp == 0 || warp == kProducerQWarp) {
     // ------------------------------------------------------------- TMA producers
@@ -518,6 +527,7 @@ __device__ __forceinline__ void ns_load8(const NsIn& L, int dt, int r, int c, fl
 __global__ void __launch_bounds__(256)
 ns_norm_kernel(const __grid_constant__ NsInParams P) {
   __shared__ double red[8];
+  cudaTriggerProgrammaticLaunchCompletion();
   const int l = blockIdx.x / kNormParts, part = blockIdx.x % kNormParts;
   const NsIn& L = P.mat[l];
   const int chunks = (L.d + 7) / 8;                   // of eight columns; a thread's lie 256 * kNormParts apart
@@ -554,11 +564,21 @@ ns_norm_kernel(const __grid_constant__ NsInParams P) {
   }
 }
 
+// f as a number in [1, 2) and two powers of two, since fp32 may hold neither it nor its inverse
+__device__ __forceinline__ void ns_factor(double f, float (&factor)[3]) {
+  int e = 0;
+  if (f > 0 && f <= 1.7e308) e = ilogb(f);
+  factor[0] = float(scalbn(f, -e));
+  factor[1] = float(scalbn(1.0, e / 2));
+  factor[2] = float(scalbn(1.0, e - e / 2));
+}
+
 // 64 x 64 blocks of M / (|M| + eps), scaled and split, transposed where M has more rows than columns
 __global__ void __launch_bounds__(256)
 ns_split_kernel(const __grid_constant__ NsInParams P) {
   __shared__ float tile[64][65];
   __shared__ float factor[3];
+  follow_the_launch_before();
   int lo = 0, hi = P.n_mats - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -569,15 +589,7 @@ ns_split_kernel(const __grid_constant__ NsInParams P) {
     double s = P.partials[lo * kNormParts + threadIdx.x];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (threadIdx.x == 0) {
-      // as a number in [1, 2) and two powers of two, since fp32 may hold neither the factor nor its inverse
-      const double f = double(P.scale) / (sqrt(s) + P.eps);
-      int e = 0;
-      if (f > 0 && f <= 1.7e308) e = ilogb(f);
-      factor[0] = float(scalbn(f, -e));
-      factor[1] = float(scalbn(1.0, e / 2));
-      factor[2] = float(scalbn(1.0, e - e / 2));
-    }
+    if (threadIdx.x == 0) ns_factor(double(P.scale) / (sqrt(s) + P.eps), factor);
   }
   const int local = blockIdx.x - L.block_begin, tiles_c = (L.d + 63) / 64;
   const int r0 = local / tiles_c * 64, c0 = local % tiles_c * 64;
@@ -621,7 +633,199 @@ ns_split_kernel(const __grid_constant__ NsInParams P) {
   }
 }
 
+// ---- small matrices: all steps of a matrix in one CTA ----------------------------------------------
+// X transposed, A and B in shared memory; products in fp32 FMAs, 4 x 4 sums per thread: 32 bytes of shared memory per 16 FMAs, which
+// bounds it (63 % of its rate; tiles on one side of the diagonal only, or twice the width, took the same time).  One launch instead of 17
+// that wait for one another: 40 us against 97 for one 64 x 64, 17 against 75 for 24 x 24; for the four layers of a block of width 64, the longest of
+// 256, 102 against 95, for those of 24 blocks 103 against 322.
+
+constexpr int kSmallM = 64, kSmallN = 256, kSmallPitch = kSmallM + 4, kSmallThreads = 512;
+constexpr int kSmallSteps = 16, kSmallMats = 96;      // per launch (parameter block)
+
+struct NsSmallMat {
+  const void* M; void* out;
+  long long ldm, ldo;
+  int p, d;
+  float scale;
+};
+struct NsSmallParams {
+  NsSmallMat mat[kSmallMats];
+  float coef[kSmallSteps][3];
+  double eps;
+  int steps, dt, out_dt;
+};
+__device__ __forceinline__ void ns_small_add(float4& to, float f, const float4& v) {
+  to.x = fmaf(f, v.x, to.x);
+  to.y = fmaf(f, v.y, to.y);
+  to.z = fmaf(f, v.z, to.z);
+  to.w = fmaf(f, v.w, to.w);
+}
+
+struct NsSmallSmem {
+  float X[kSmallN][kSmallPitch];                       // X[k][i]: column k of X, zeros from row m on
+  float A[kSmallM][kSmallPitch], B[kSmallM][kSmallPitch];
+  double red[kSmallThreads / 32];
+  float factor[3];
+};
+
+// sum over k0 <= k < k1 of U[k][i..i+3] U[k][j..j+3]; acc[c] are row j + c's four
+__device__ __forceinline__ void ns_small_square(const float (*U)[kSmallPitch], int k0, int k1, int i, int j, float4 (&acc)[4]) {
+#pragma unroll
+  for (int c = 0; c < 4; ++c) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+  for (int k = k0; k < k1; ++k) {
+    const float4 x = *reinterpret_cast<const float4*>(&U[k][i]), y = *reinterpret_cast<const float4*>(&U[k][j]);
+    ns_small_add(acc[0], y.x, x);
+    ns_small_add(acc[1], y.y, x);
+    ns_small_add(acc[2], y.z, x);
+    ns_small_add(acc[3], y.w, x);
+  }
+}
+
+__device__ __forceinline__ void ns_small_store(float (*to)[kSmallPitch], int i, int j, const float4 (&v)[4]) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) *reinterpret_cast<float4*>(&to[j + r][i]) = v[r];
+}
+
+// X <- a X + B X for four columns of X from c0 on, which a half-warp (`lanes`) alone reads and writes; rows i .. i + 3
+__device__ __forceinline__ void ns_small_apply(NsSmallSmem& S, float a, int m4, int i, int c0, uint32_t lanes) {
+  float4 sum[4];
+  if (i < m4) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float4 x = *reinterpret_cast<const float4*>(&S.X[c0 + r][i]);
+      sum[r] = make_float4(a * x.x, a * x.y, a * x.z, a * x.w);
+    }
+#pragma unroll 2
+    for (int k = 0; k < m4; k += 4) {
+      float4 b[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) b[q] = *reinterpret_cast<const float4*>(&S.B[k + q][i]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float4 x = *reinterpret_cast<const float4*>(&S.X[c0 + r][k]);
+        ns_small_add(sum[r], x.x, b[0]);
+        ns_small_add(sum[r], x.y, b[1]);
+        ns_small_add(sum[r], x.z, b[2]);
+        ns_small_add(sum[r], x.w, b[3]);
+      }
+    }
+  }
+  __syncwarp(lanes);
+  if (i < m4) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) *reinterpret_cast<float4*>(&S.X[c0 + r][i]) = sum[r];
+  }
+}
+
+__global__ void __launch_bounds__(kSmallThreads)
+ns_small_kernel(const __grid_constant__ NsSmallParams P) {
+  extern __shared__ uint8_t smem_raw[];
+  NsSmallSmem& S = *reinterpret_cast<NsSmallSmem*>(smem_raw);
+  const NsSmallMat& L = P.mat[blockIdx.x];
+  const int tid = threadIdx.x, total = L.p * L.d;
+  const bool transposed = L.p > L.d;
+  const int m = transposed ? L.d : L.p, n = transposed ? L.p : L.d;
+  const int m4 = (m + 3) & ~3;
+  double s = 0.0;
+  for (int k0 = tid; k0 < total; k0 += 8 * kSmallThreads) {        // eight loads on their way at once
+    float v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int k = k0 + u * kSmallThreads, r = k / L.d, c = k - r * L.d;
+      const size_t at = size_t(r) * size_t(L.ldm) + c;
+      if (k < total) v[u] = P.dt == DP_F32 ? static_cast<const float*>(L.M)[at] : to_f32(static_cast<const __nv_bfloat16*>(L.M)[at]);
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int k = k0 + u * kSmallThreads, r = k / L.d, c = k - r * L.d;
+      if (k >= total) continue;
+      if (transposed) S.X[r][c] = v[u]; else S.X[c][r] = v[u];
+      s = fma(double(v[u]), double(v[u]), s);
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if ((tid & 31) == 0) S.red[tid >> 5] = s;
+  __syncthreads();
+  if (tid == 0) {
+    s = 0.0;
+    for (int w = 0; w < kSmallThreads / 32; ++w) s += S.red[w];
+    ns_factor(1.0 / (sqrt(s) + P.eps), S.factor);
+  }
+  __syncthreads();
+  const float f0 = S.factor[0], f1 = S.factor[1], f2 = S.factor[2];
+  for (int k = tid; k < ((n + 3) & ~3) * kSmallM; k += kSmallThreads) {
+    float& x = S.X[k / kSmallM][k % kSmallM];
+    x = k % kSmallM < m && k / kSmallM < n ? x * f1 * f2 * f0 : 0.f;
+  }
+  __syncthreads();
+  // products of 64 x 64: 256 threads on each half of the sum, the second's added by the first
+  const int half = tid >> 8, i = 4 * (tid & 15), j = 4 * (tid >> 4 & 15);
+  const bool here = i < m && j < m;
+  const int n_half = (n + 1) / 2, m_half = m4 / 2;
+  for (int step = 0; step < P.steps; ++step) {
+    const float a = P.coef[step][0], b = P.coef[step][1], c = P.coef[step][2];
+    float4 acc[4];
+    if (here) ns_small_square(S.X, half ? n_half : 0, half ? n : n_half, i, j, acc);
+    if (here && half) ns_small_store(S.A, i, j, acc);
+    __syncthreads();
+    if (here && !half) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) ns_small_add(acc[r], 1.f, *reinterpret_cast<const float4*>(&S.A[j + r][i]));
+      ns_small_store(S.A, i, j, acc);
+    }
+    __syncthreads();
+    if (here) ns_small_square(S.A, half ? m_half : 0, half ? m4 : m_half, i, j, acc);   // rows from m on are zeros
+    if (here && half) ns_small_store(S.B, i, j, acc);
+    __syncthreads();
+    if (here && !half) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float4 x = *reinterpret_cast<const float4*>(&S.A[j + r][i]);
+        ns_small_add(acc[r], 1.f, *reinterpret_cast<const float4*>(&S.B[j + r][i]));
+        acc[r] = make_float4(fmaf(c, acc[r].x, b * x.x), fmaf(c, acc[r].y, b * x.y), fmaf(c, acc[r].z, b * x.z), fmaf(c, acc[r].w, b * x.w));
+      }
+      ns_small_store(S.B, i, j, acc);
+    }
+    __syncthreads();
+    const uint32_t lanes = 0xffffu << (tid & 16);
+    for (int c0 = 4 * (tid >> 4); c0 < n; c0 += 4 * (kSmallThreads / 16)) ns_small_apply(S, a, m4, i, c0, lanes);
+    __syncthreads();
+  }
+  for (int k = tid; k < total; k += kSmallThreads) {
+    const int r = k / L.d, c = k - r * L.d;
+    const size_t at = size_t(r) * size_t(L.ldo) + c;
+    const float v = L.scale * (transposed ? S.X[r][c] : S.X[c][r]);
+    if (P.out_dt == DP_F32) static_cast<float*>(L.out)[at] = v; else static_cast<__nv_bfloat16*>(L.out)[at] = __float2bfloat16_rn(v);
+  }
+}
+
 // ---- host ----------------------------------------------------------------------------------------
+
+bool ns_small(const dp_matrix_desc* mats, int n, int steps) {
+  for (int k = 0; k < n; ++k)
+    if (std::min(mats[k].p, mats[k].d) > kSmallM || std::max(mats[k].p, mats[k].d) > kSmallN) return false;
+  return steps <= kSmallSteps;
+}
+
+dp_status ns_small_launch(const dp_matrix_desc* mats, int n, dp_dtype dt, dp_dtype out_dt, const float* coefs, int steps, float eps,
+                          cudaStream_t st) {
+  NsSmallParams P;
+  P.steps = steps; P.dt = dt; P.out_dt = out_dt; P.eps = eps;
+  std::memcpy(P.coef, coefs, sizeof(float) * 3 * size_t(steps));
+  if (first_use_on_this_device((const void*)ns_small_kernel)) DP_CUDA_OK(allow_shared(ns_small_kernel, sizeof(NsSmallSmem)));
+  for (int k0 = 0; k0 < n; k0 += kSmallMats) {
+    const int here = std::min(kSmallMats, n - k0);
+    for (int k = 0; k < here; ++k) {
+      const dp_matrix_desc& D = mats[k0 + k];
+      P.mat[k] = {D.M, D.out, D.ldm, D.ldo, D.p, D.d, D.scale};
+    }
+    ns_small_kernel<<<here, kSmallThreads, sizeof(NsSmallSmem), st>>>(P);
+    DP_LAUNCH_OK();
+  }
+  return DP_OK;
+}
 
 struct NsShape {
   int m, n, ldx, lda;
@@ -718,11 +922,13 @@ dp_status ns_launch(const NsParams& P, cudaStream_t st) {
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = kSmemBytes;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim = {kPair ? 2u : 1u, 1u, 1u};
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim = {2u, 1u, 1u};
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = kPair ? 2 : 1;
   DP_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, P));
   ++g_kernel_launches;
   return DP_OK;
@@ -815,8 +1021,17 @@ dp_status ns_group(const dp_matrix_desc* mats, int n, dp_dtype dt, dp_dtype out_
   In.n_mats = n; In.dt = dt; In.partials = partials; In.eps = eps; In.scale = float(sx);
   ns_norm_kernel<<<n * kNormParts, 256, 0, st>>>(In);
   DP_LAUNCH_OK();
-  ns_split_kernel<<<blocks, 256, 0, st>>>(In);
-  DP_LAUNCH_OK();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(blocks);
+  cfg.blockDim = dim3(256);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  DP_CUDA_OK(cudaLaunchKernelEx(&cfg, ns_split_kernel, In));
+  ++g_kernel_launches;
 
   const NsForm form = choose_form(shapes, plan, out_dt == DP_BF16);
   NsParams P;
@@ -955,6 +1170,7 @@ dp_status dp_orthogonalize(const dp_matrix_desc* mats, int32_t n, dp_dtype dt, d
   if (!plan_steps(coefs, steps, plan)) return DP_ERR_INVALID_ARG;
   if (!ws || ws_bytes < dp_orthogonalize_ws_bytes(mats, n)) return DP_ERR_WORKSPACE;
   if (!aligned16(ws)) return DP_ERR_ALIGNMENT;
+  if (ns_small(mats, n, steps)) return ns_small_launch(mats, n, dt, out_dt, coefs, steps, eps, (cudaStream_t)stream);
   const std::vector<int> order = ns_order(mats, n);
   const int groups = ns_groups(n);
   for (int g = 0; g < groups; ++g) {

@@ -375,6 +375,8 @@ def ns_room(shapes, out_dtype):
 NS_SETS = [
     [(1, 1)], [(1, 9)], [(9, 1)], [(7, 5)], [(64, 64)], [(65, 64)], [(64, 130)], [(200, 72)], [(129, 257)],
     [(64, 64), (65, 63), (1, 5), (300, 20)],                    # one call, every kind
+    [(64, 256), (256, 64), (63, 255), (1, 256), (30, 30), (254, 3)],   # a CTA each
+    [(257, 2)], [(2, 3), (2, 257)],                             # just too long for that
     [(256, 256)] * 3 + [(768, 256), (256, 1024)], [(768, 768)],
 ]
 
@@ -415,6 +417,18 @@ def test_orthogonalize_other_polynomials(coefs):
     dp.dp_orthogonalize([m], [o], coefs=coefs)
     want = O.orthogonalize(f64(m), coefs)
     assert np.linalg.norm(f64(o) - want) <= 2 * ns_room([m.shape], torch.float32) * np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("steps", [1, 16, 17])
+def test_orthogonalize_many_small_matrices_and_many_steps(steps):
+    """Small matrices take a CTA each, in several launches; with more steps than a launch holds, the tiles of larger ones."""
+    mats = [tensor((33, 60), torch.float32, k) for k in range(100)]
+    outs = [torch.empty_like(m) for m in mats]
+    coefs = ((1.5, -0.5, 0.0),) * steps
+    dp.dp_orthogonalize(mats, outs, coefs=coefs)
+    for k in (0, 50, 95, 96, 99):
+        want = O.orthogonalize(f64(mats[k]), coefs)
+        assert np.linalg.norm(f64(outs[k]) - want) <= 2 * ns_room([(33, 60)], torch.float32) * np.linalg.norm(want)
 
 
 def test_orthogonalize_extreme_inputs():
