@@ -6,6 +6,7 @@ Order (all enqueued on the current stream, no host synchronisation):
   tied head: cross term                       -> dp_tied_cross_term      (Eq. 11, Eq. 13)
   clipped sums per parameter tensor           -> dp_clip_accumulate[_embed]  (Eq. 2, Eq. 3, Eq. 7)
   Gaussian noise per parameter tensor         -> dp_add_noise            (Eq. 3)
+and, after a step, orthogonalised updates      -> dp_orthogonalize
 """
 from __future__ import annotations
 
@@ -516,6 +517,23 @@ def dp_step(ds: DeviceStep, seed: int = 0, step: int = 0, noise: bool = True, fu
     clip_phase(ds, stream)
     if noise:
         noise_phase(ds, seed, step, stream=stream)
+
+
+def orthogonal_updates(ds: DeviceStep, updates: Optional[Dict[str, torch.Tensor]] = None, scale: float = 1.0,
+                       coefs=dp.NEWTON_SCHULZ, eps: float = 1e-7, ws=None, stream=None) -> Dict[str, torch.Tensor]:
+    """After a step: the noised sums of the block linears orthogonalised, each scaled by scale * sqrt(max(1, p / d)) so that an
+    update's entries are alike whatever the layer's shape.  Post-processing of Eq. 3's output, so it costs no privacy.  The tables, the
+    head and the vectors keep their sums.  updates: tensors by the names of ds.outs, fp32 or all bf16 (the
+    sums themselves do); made where None."""
+    names = [f"linear{k}" for k in range(len(ds.linears))]
+    if not names:
+        return {}
+    if updates is None:
+        updates = {n: torch.empty_like(ds.outs[n]) for n in names}
+    mats = [ds.outs[n] for n in names]
+    dp.dp_orthogonalize(mats, [updates[n] for n in names], scales=[scale * max(1.0, m.shape[0] / m.shape[1]) ** 0.5 for m in mats],
+                        coefs=coefs, eps=eps, ws=ws, dev_status=ds.dev_status, stream=stream)
+    return updates
 
 
 class StepGraph:
