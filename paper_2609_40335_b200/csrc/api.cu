@@ -31,7 +31,7 @@ constexpr int kMaxDevices = 64;
 std::mutex g_device_mutex;
 }
 
-static int device_sm_count() {
+int device_sm_count() {
   static int n[kMaxDevices] = {};
   int dev = 0, v = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 148;

@@ -43,6 +43,7 @@ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 // number of SMs of the current device (cached per device)
 int sm_count();
+int device_sm_count();               // all of them, reserved or not
 
 // One-time set-up that CUDA keeps PER DEVICE (function attributes such as the dynamic
 // shared-memory limit): true the first time `key` is seen with the current device, false

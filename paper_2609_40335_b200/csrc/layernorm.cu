@@ -16,12 +16,15 @@
 // by rows and sums by columns from shared memory, each element converted twice, 66 to 74; in this form 49.)
 //
 // Backward: the rows of an example are shared out over a cluster of CTAs: at the end each CTA adds a slice of the columns over the cluster
-// through distributed shared memory, and rank 0 adds up the squares: one launch, no workspace, a fixed order.  Where a cluster's CTAs are
-// too few for a long sequence, the partial sums go through the workspace instead (ln_sums_kernel).
+// through distributed shared memory, and rank 0 adds up the squares: one launch, no workspace, a fixed order.  Where too few clusters fit
+// the chip at once, the partial sums go through the workspace instead (ln_sums_kernel).
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <array>
 #include <cmath>
+#include <map>
+#include <mutex>
 
 #include "dp_common.cuh"
 #include "ptx_sm100.cuh"
@@ -529,6 +532,7 @@ ln_backward_kernel(const LnBackward P) {
     __syncthreads();
   }
   if (P.partials) {
+    cudaTriggerProgrammaticLaunchCompletion();
     float* out = P.partials + (long long)blockIdx.x * 2 * p;
     for (int c = tid; c < 2 * p; c += blockDim.x) out[c] = sums[c];
     return;
@@ -570,24 +574,36 @@ ln_backward_kernel(const LnBackward P) {
   }
 }
 
-// The parts' sums through the workspace: a thread per column of an example, parts in order.
-__global__ void __launch_bounds__(128)
-ln_sums_kernel(const float* partials, int parts, int p, float* gain_sums, float* shift_sums, float* squares) {
-  __shared__ float red[32];
-  const int example = blockIdx.y, c = blockIdx.x * 128 + threadIdx.x;
-  float a = 0.f, b = 0.f;
-  if (c < p) {
+// The parts' sums through the workspace: a thread per column, parts in order, an example's columns over a cluster whose rank 0 adds up the
+// squares.  Its launch overlaps the end of the other one.
+constexpr int kLnSumThreads = 128;
+__global__ void __launch_bounds__(kLnSumThreads)
+ln_sums_kernel(const float* partials, int parts, int p, float* gain_sums, float* shift_sums, float* sq) {
+  __shared__ float red[32], squares[8];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int ctas = cluster.num_blocks(), rank = cluster.block_rank(), example = blockIdx.x / ctas;
+  cudaGridDependencySynchronize();
+  float square = 0.f;
+  for (int c = rank * kLnSumThreads + threadIdx.x; c < p; c += ctas * kLnSumThreads) {
     const float* in = partials + (long long)example * parts * 2 * p + c;
-#pragma unroll 4
+    float a = 0.f, b = 0.f;
+#pragma unroll 8
     for (int k = 0; k < parts; ++k) {
       a += in[(long long)k * 2 * p];
       b += in[(long long)k * 2 * p + p];
     }
     if (gain_sums) gain_sums[(long long)example * p + c] = a;
     if (shift_sums) shift_sums[(long long)example * p + c] = b;
+    square = fmaf(a, a, fmaf(b, b, square));
   }
-  const float sq = block_sum(fmaf(a, a, b * b), red);
-  if (threadIdx.x == 0) squares[example * gridDim.x + blockIdx.x] = sq;
+  square = block_sum(square, red);
+  if (threadIdx.x == 0) *cluster.map_shared_rank(squares + rank, 0) = square;
+  cluster.sync();
+  if (sq && rank == 0 && threadIdx.x == 0) {
+    float all = 0.f;
+    for (int q = 0; q < ctas; ++q) all += squares[q];
+    sq[example] += all;
+  }
 }
 
 bool ln_vec(const void* q, long long ld, int es) { return !q || (aligned16(q) && (ld * es) % 16 == 0); }
@@ -633,15 +649,6 @@ bool ln_fit(LnShape& S, int p, int rows, bool sums, int warps, int blocks, bool 
   return LnSmem(S, p, rows, sums, warps).bytes <= 226 * 1024;
 }
 
-// Parts an example's rows are cut into, and whether they are a cluster (else the sums go through the workspace): as many CTAs as the
-// SMs hold at once, 16 rows each at least; clusters of more than eight, of which fewer fit the chip, only where eight would leave SMs idle.
-struct LnParts { int parts; bool cluster; };
-LnParts ln_parts(int B, int T, int blocks) {
-  const int sms = sm_count(), wanted = std::max(1, blocks * sms / B), most = ceil_div(T, 16);
-  if (wanted > 2 * kLnMaxParts && T >= 1024 * kLnMaxParts) return {std::min(wanted, T / 512), false};
-  return {std::max(1, std::min(std::min(wanted, most), 8 * B >= sms ? 8 : kLnMaxParts)), true};
-}
-
 // Working warps of a block and blocks per SM, by the registers that a lane's columns take: four of each in the backward pass, two in the
 // forward pass.
 constexpr int ln_columns(int NP, int es) { return NP * 16 / es; }
@@ -650,6 +657,58 @@ constexpr LnBlock ln_back_block(int columns, bool widest) {
   return widest ? LnBlock{16, 1} : columns > 24 ? LnBlock{10, 1} : columns > 16 ? LnBlock{14, 1} : columns > 8 ? LnBlock{8, 2} : LnBlock{8, 3};
 }
 constexpr LnBlock ln_forward_block(bool widest) { return widest ? LnBlock{16, 1} : LnBlock{8, 2}; }
+
+// [c]: clusters of c CTAs, one CTA per SM, that run at once on the current device: fewer than SMs / c, since a cluster stays within a group of
+// SMs (7 of 16, 15 of 8, 37 of 4 on a B200 with 148).
+using LnClusters = std::array<int, kLnMaxParts + 1>;
+const LnClusters& clusters_at_once() {
+  static std::mutex mutex;
+  static std::map<int, LnClusters> known;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) dev = -1;
+  std::lock_guard<std::mutex> lock(mutex);
+  const auto seen = known.find(dev);
+  if (seen != known.end()) return seen->second;
+  LnClusters& most = known[dev];                       // stays where it is
+  auto* kernel = ln_backward_kernel<__nv_bfloat16, 4, true, (ln_back_block(32, true).warps + 1) * 32, ln_back_block(32, true).blocks>;
+  for (int c = 1; c <= kLnMaxParts; ++c) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(c));
+    cfg.blockDim = dim3((ln_back_block(32, true).warps + 1) * 32);
+    cfg.dynamicSmemBytes = 200 * 1024;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {unsigned(c), 1u, 1u};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (dev < 0 || ln_smem_setup(kernel) != DP_OK || cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
+      (void)cudaGetLastError();
+      n = std::max(1, device_sm_count() / (c + c / 4));
+    }
+    most[c] = n;
+  }
+  return most;
+}
+
+// Parts an example's rows are cut into, and whether they are a cluster (else the sums go through the workspace): whichever takes least, in
+// rows of a CTA.  A wave of CTAs costs 128 rows beside its own, the other launch 64 and one per part.  16 rows per part at least.
+// Measured with T = 1024, p = 768 in bf16, clusters of 16, of 8 and the workspace (37 to 148 CTAs in all): 16, 21 and 19 us of 6 examples, 30, 21 and 20 of
+// 8, 40, 41 and 23 of 16; p = 256: 11, 15 and 24; 12, 16 and 23; 16, 18 and 19.
+struct LnParts { int parts; bool cluster; };
+LnParts ln_parts(int B, int T, int blocks) {
+  const int sms = device_sm_count();
+  const LnClusters& at_once = clusters_at_once();
+  LnParts best{1, true};
+  long long least = 0;
+  for (int c = 1; c <= std::min(kLnMaxParts, ceil_div(T, 16)); c *= 2) {
+    const long long waves = ceil_div(B, blocks * at_once[c]), cost = waves * (ceil_div(T, c) + 128);
+    if (c == 1 || cost < least) { least = cost; best = {c, true}; }
+  }
+  const int through = std::min(std::min(blocks * sms / B, ceil_div(T, 16)), int(std::sqrt(double(T))));
+  if (through > 1 && ceil_div(T, through) + 192 + through < least) best = {through, false};
+  return best;
+}
 
 template <typename T, int NP, bool kAligned, bool kWidest>
 dp_status ln_back_launch(LnBackward& P, int B, LnParts parts, cudaStream_t st) {
@@ -769,7 +828,7 @@ size_t dp_layernorm_backward_ws_bytes(int32_t B, int32_t T, int32_t p) {
   size_t most = 0;                                    // of either type of G and X
   for (const int es : {2, 4}) {
     const LnParts parts = ln_parts_of(B, T, p, es);
-    if (!parts.cluster) most = std::max(most, ln_partial_bytes(parts, B, p) + align_up(size_t(B) * ceil_div(p, 128) * sizeof(float), 256));
+    if (!parts.cluster) most = std::max(most, ln_partial_bytes(parts, B, p));
   }
   return most;
 }
@@ -789,12 +848,10 @@ dp_status dp_layernorm_backward(const void* G, int64_t ldg, const void* X, int64
   const LnParts parts = ln_parts_of(B, T, p, es);
   if ((long long)B * parts.parts > 0x7fffffffLL) return DP_ERR_UNSUPPORTED;
   float* partials = nullptr;
-  float* squares = nullptr;
   if (!parts.cluster && sums) {
     if (!ws || ws_bytes < dp_layernorm_backward_ws_bytes(B, T, p)) return DP_ERR_WORKSPACE;
     if (!on_boundary(4, ws)) return DP_ERR_ALIGNMENT;
     partials = static_cast<float*>(ws);
-    squares = reinterpret_cast<float*>(static_cast<char*>(ws) + ln_partial_bytes(parts, B, p));
   }
   LnBackward P{};
   P.G = G; P.ldg = ldg; P.X = X; P.ldx = ldx; P.gain = gain; P.param_dt = param_dt; P.mean = mean; P.rstd = rstd; P.dX = dX; P.lddx = lddx;
@@ -808,10 +865,21 @@ dp_status dp_layernorm_backward(const void* G, int64_t ldg, const void* X, int64
   const cudaStream_t st = (cudaStream_t)stream;
   const dp_status r = ln_run(dt, aligned, ln_pieces(P.S, p, es), P.S.W == 16, RunBackward{P, B, parts, st});
   if (r != DP_OK || !partials) return r;
-  const int slabs = ceil_div(p, 128);
-  ln_sums_kernel<<<dim3(slabs, B), 128, 0, st>>>(partials, parts.parts, p, gain_sums, shift_sums, squares);
-  DP_LAUNCH_OK();
-  return sq ? launch_reduce_partials(squares, slabs, B, sq, 1.f, nullptr, st) : DP_OK;
+  const unsigned ctas = unsigned(std::min(8, ceil_div(p, kLnSumThreads)));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(B) * ctas);
+  cfg.blockDim = dim3(kLnSumThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim = {ctas, 1u, 1u};
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  DP_CUDA_OK(cudaLaunchKernelEx(&cfg, ln_sums_kernel, (const float*)partials, parts.parts, p, gain_sums, shift_sums, sq));
+  ++g_kernel_launches;
+  return DP_OK;
 }
 
 }  // extern "C"

@@ -121,7 +121,8 @@ def test_layernorm_rows_of_equal_values_and_values_that_are_not_finite():
 BACK = [
     # B, T, p: one token; one example; odd; wide; ragged against the cluster's parts; more parts than rows
     (1, 1, 1), (4, 16, 64), (3, 1, 768), (2, 5, 7), (5, 33, 100), (21, 40, 257), (2, 203, 768), (1, 300, 1001), (7, 9, 1024),
-    (2, 17, 1032), (1, 64, 2049), (3, 12, 4096), (1, 20, 8200), (1, 3, 16384), (2, 3, 16383), (300, 3, 64), (1, 1500, 64), (2, 1111, 776)]
+    (2, 17, 1032), (1, 64, 2049), (3, 12, 4096), (1, 20, 8200), (1, 3, 16384), (2, 3, 16383), (300, 3, 64), (1, 1500, 64), (2, 1111, 776),
+    (16, 640, 776), (1, 4100, 1001)]                            # sums through the workspace
 
 
 @pytest.mark.parametrize("B,T,p", BACK)

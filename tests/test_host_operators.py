@@ -63,6 +63,7 @@ def test_layernorm_backward(lib, kw, want):
 def test_layernorm_backward_needs_a_workspace_for_few_long_examples_only(lib):
     f = lib.dp_layernorm_backward_ws_bytes
     assert f(64, 256, 768) == 0 and f(4, 16, 64) == 0 and f(6, 1024, 768) == 0
+    assert f(16, 640, 776) > 0 and f(1, 4100, 1001) > 0
     assert f(1, 100000, 768) > 32 * 2 * 768 * 4 and f(0, 5, 5) == 0 and f(1, 100000, 16385) == 0
 
 
