@@ -141,20 +141,27 @@ __device__ __forceinline__ uint32_t ln_copy(const T* first, long long ld, int p,
   return bytes;
 }
 
-// A lane's pieces of a row.  kAligned: 16 bytes each; else the columns of a piece lie a row's pieces apart, so that a
-// warp's accesses are consecutive.
+// A lane's pieces of a row.  kAligned: 16 bytes each; else columns 32 apart, so that a warp's accesses are consecutive, their distances
+// constants, and whether a column is in the row one comparison with a constant (with columns as far apart as the row has pieces the forward pass
+// issued 67 instructions per column).
 template <typename T, int NP, bool kAligned>
 struct LnRow {
   static constexpr int N = Piece<T>::N, H = N / 2;
-  int tid, width, pieces, p;
+  int tid, width, limit;     // limit: pieces of the row; else this lane's columns
+  int first;                 // not aligned: this lane's first column; its others are 32 apart, a warp's all within 32 NP N
+  __device__ __forceinline__ LnRow(int tid, int width, int p) : tid(tid), width(width), first(tid / 32 * (32 * NP * N) + tid % 32) {
+    limit = kAligned ? (p + N - 1) / N : p > first ? (p - first + 31) / 32 : 0;
+  }
   __device__ __forceinline__ int piece(int j) const { return tid + j * width; }
-  __device__ __forceinline__ int column(int j, int e) const { return kAligned ? piece(j) * N + e : e * pieces + piece(j); }
-  __device__ __forceinline__ bool has(int j) const { return piece(j) < pieces; }
+  __device__ __forceinline__ int column(int j, int e) const { return kAligned ? piece(j) * N + e : first + (j * N + e) * 32; }
+  __device__ __forceinline__ bool has(int j) const { return kAligned ? piece(j) < limit : j * N < limit; }
+  __device__ __forceinline__ bool has(int j, int e) const { return kAligned ? piece(j) < limit : j * N + e < limit; }
   // Zeros behind the row, and all zeros where `there` is false.  kAny: any values of the row behind it, for lanes of several pieces,
   // whose row is there or not for the whole warp, where zeros in the vectors take them out (selecting took a sixth of the backward
   // pass's instructions).
   template <bool kAny>
   __device__ __forceinline__ void open(const void* row, bool there, F2 (&v)[NP][H]) const {
+    const int most = there ? limit : 0;
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
       if (kAligned) {
@@ -163,11 +170,10 @@ struct LnRow {
         else if (there && has(j)) q = static_cast<const uint4*>(row)[piece(j)];
         Piece<T>::open(q, v[j]);
       } else {
-        const T* x = static_cast<const T*>(row);
+        const T* x = static_cast<const T*>(row) + first;
 #pragma unroll
         for (int e = 0; e < H; ++e) {
-          const int a = column(j, 2 * e), b = column(j, 2 * e + 1);
-          v[j][e] = f2(there && has(j) && a < p ? to_f32(x[a]) : 0.f, there && has(j) && b < p ? to_f32(x[b]) : 0.f);
+          v[j][e] = f2(j * N + 2 * e < most ? to_f32(x[(j * N + 2 * e) * 32]) : 0.f, j * N + 2 * e + 1 < most ? to_f32(x[(j * N + 2 * e + 1) * 32]) : 0.f);
         }
       }
     }
@@ -191,8 +197,7 @@ struct LnRow {
     } else {
 #pragma unroll
       for (int e = 0; e < H; ++e) {
-        const int a = column(j, 2 * e), b = column(j, 2 * e + 1);
-        f[e] = f2(has(j) && a < p ? v[a] : 0.f, has(j) && b < p ? v[b] : 0.f);
+        f[e] = f2(v[column(j, 2 * e)], v[column(j, 2 * e + 1)]);        // (the vectors go on behind the row)
       }
     }
   }
@@ -205,7 +210,7 @@ struct LnRow {
 #pragma unroll
     for (int e = 0; e < N; ++e) {
       const float2 f = floats(v[e / 2]);
-      if (column(j, e) < p) out[column(j, e)] = from_f32<T>(e & 1 ? f.y : f.x);
+      if (has(j, e)) out[column(j, e)] = from_f32<T>(e & 1 ? f.y : f.x);
     }
   }
 };
@@ -288,7 +293,7 @@ ln_forward_kernel(const LnForward P) {
     return;
   }
   const int per_row = S.lanes * S.W, group = tid / per_row;
-  const LnRow<T, NP, kAligned> R{tid - group * per_row, per_row, (p + N - 1) / N, p};
+  const LnRow<T, NP, kAligned> R(tid - group * per_row, per_row, p);
   for (int c = tid; c < max(p, per_row * NP * N); c += warps * 32) {
     gain[R.place(c)] = c < p ? ln_param(P.gain, P.param_dt, 1.f, c) : 0.f;
     shift[R.place(c)] = c < p ? ln_param(P.shift, P.param_dt, 0.f, c) : 0.f;
@@ -330,7 +335,7 @@ ln_forward_kernel(const LnForward P) {
         if (!R.has(j)) v[j][e] = f2(0.f, 0.f);
         else if (!kAligned) {
           const float2 f = floats(v[j][e]);
-          v[j][e] = f2(R.column(j, 2 * e) < p ? f.x : 0.f, R.column(j, 2 * e + 1) < p ? f.y : 0.f);
+          v[j][e] = f2(R.has(j, 2 * e) ? f.x : 0.f, R.has(j, 2 * e + 1) ? f.y : 0.f);
         }
         sum = fma2(v[j][e], v[j][e], sum);
       }
@@ -402,7 +407,7 @@ ln_backward_kernel(const LnBackward P) {
   }
   __syncthreads();
   const int per_row = S.lanes * S.W, group = tid / per_row;
-  const LnRow<T, NP, kAligned> R{tid - group * per_row, per_row, (p + N - 1) / N, p};
+  const LnRow<T, NP, kAligned> R(tid - group * per_row, per_row, p);
   F2 gs[NP][H], ss[NP][H];
 #pragma unroll
   for (int j = 0; j < NP; ++j)
@@ -518,7 +523,7 @@ ln_backward_kernel(const LnBackward P) {
       for (int e = 0; e < N; ++e) {
         const float2 u = floats(gs[j][e / 2]), v = floats(ss[j][e / 2]);
         const int c = R.column(j, e);
-        if (R.has(j) && c < p) { mine[c] = e & 1 ? u.y : u.x; mine[p + c] = e & 1 ? v.y : v.x; }
+        if (R.has(j, e)) { mine[c] = e & 1 ? u.y : u.x; mine[p + c] = e & 1 ? v.y : v.x; }
       }
   }
   __syncthreads();
@@ -608,11 +613,11 @@ ln_sums_kernel(const float* partials, int parts, int p, float* gain_sums, float*
 
 bool ln_vec(const void* q, long long ld, int es) { return !q || (aligned16(q) && (ld * es) % 16 == 0); }
 
-// Lanes and warps of a row: 16-byte pieces, at most 32 columns a lane.
-LnShape ln_shape(int p, int es) {
+// Lanes and warps of a row: 16-byte pieces, at most 32 columns a lane; whole warps for rows that are not aligned.
+LnShape ln_shape(int p, int es, bool aligned) {
   LnShape S{};
   const int pieces = ceil_div(p * es, 16), most = 2 * es;              // pieces per lane
-  S.lanes = 1;
+  S.lanes = aligned ? 1 : 32;
   while (S.lanes < 32 && S.lanes < pieces) S.lanes *= 2;
   S.W = 1;
   while (S.W * 32 * most < pieces) S.W *= 2;
@@ -784,7 +789,7 @@ dp_status ln_run(dp_dtype dt, bool aligned, int pieces, bool widest, F f) {
 }
 
 LnParts ln_parts_of(int B, int T, int p, int es) {
-  const LnShape S = ln_shape(p, es);
+  const LnShape S = ln_shape(p, es, true);             // (the number of pieces per lane is the same for other rows)
   return ln_parts(B, T, ln_back_block(ln_columns(ln_pieces(S, p, es), es), S.W == 16).blocks);
 }
 
@@ -815,8 +820,8 @@ dp_status dp_layernorm(const void* X, int64_t ldx, dp_dtype dt, int64_t rows, in
   LnForward P{};
   P.X = X; P.ldx = ldx; P.gain = gain; P.shift = shift; P.param_dt = param_dt; P.Y = Y; P.ldy = ldy; P.H = X_hat; P.ldh = ldh;
   P.mean = mean; P.rstd = rstd; P.rows = rows; P.p = p; P.eps = eps; P.wait_limit = g_wait_limit;
-  P.S = ln_shape(p, es);
   const bool aligned = p * es % 16 == 0 && ln_vec(X, ldx, es);
+  P.S = ln_shape(p, es, aligned);
   P.whole = aligned && ldx == p;
   P.vec_y = ln_vec(Y, ldy, es);
   P.vec_h = ln_vec(X_hat, ldh, es);
@@ -857,8 +862,8 @@ dp_status dp_layernorm_backward(const void* G, int64_t ldg, const void* X, int64
   P.G = G; P.ldg = ldg; P.X = X; P.ldx = ldx; P.gain = gain; P.param_dt = param_dt; P.mean = mean; P.rstd = rstd; P.dX = dX; P.lddx = lddx;
   P.gain_sums = gain_sums; P.shift_sums = shift_sums; P.sq = sq; P.partials = partials;
   P.T = T; P.p = p; P.parts = parts.parts; P.dev_status = dev_status; P.wait_limit = g_wait_limit;
-  P.S = ln_shape(p, es);
   const bool aligned = p * es % 16 == 0 && ln_vec(G, ldg, es) && ln_vec(X, ldx, es);
+  P.S = ln_shape(p, es, aligned);
   P.whole_g = aligned && ldg == p;
   P.whole_x = aligned && ldx == p;
   P.vec_out = ln_vec(dX, lddx, es);
