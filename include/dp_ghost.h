@@ -347,10 +347,11 @@ dp_status dp_step_enqueue(const dp_step_desc* desc, int32_t phases);
  * dt: storage type of X, Y and X_hat; gain, shift [dev, p of param_dt, or NULL: 1 and 0].  Y, X_hat (the normalised input,
  * what dp_vector_norms reads as X of a gain), mean, rstd [dev, rows floats]: each may be NULL, not all of them.  Y or X_hat
  * may be X itself (same pitch), not both the same.  Any alignment works; 16-byte aligned tensors with p % 8 == 0 and pitches
- * that are multiples of 16 bytes take the vector path.  p <= 16384, eps >= 0. */
+ * that are multiples of 16 bytes take the vector path.  p <= 16384, eps >= 0.  dev_status [dev, or NULL]: DP_DEV_TIMEOUT if a wait inside
+ * ran out. */
 dp_status dp_layernorm(const void* X, int64_t ldx, dp_dtype dt, int64_t rows, int32_t p, const void* gain, const void* shift,
                        dp_dtype param_dt, float eps, void* Y, int64_t ldy, void* X_hat, int64_t ldh, float* mean, float* rstd,
-                       void* stream);
+                       int32_t* dev_status, void* stream);
 /* Its backward pass, with the reduction of the parameters' gradients by example.  G [dev, (B*T, p)]: gradient at Y; X, mean, rstd:
  * input of the forward call and what it returned.  With u = G*gain:
  *   dX = rstd * (u - mean(u) - h*mean(u*h))                                                      [dev, (B*T, p) of dt, or NULL]
@@ -375,8 +376,8 @@ size_t dp_layernorm_backward_ws_bytes(int32_t B, int32_t T, int32_t p);
  * (s the logistic function), logp [dev, (B, 2) floats] = l, and G [dev, (2*B*T, V) of dt] = scale * d loss / d logits, the G of an
  * LM head in dp_ghost_norms and dp_clip_accumulate* with sequences of 2*T tokens.  loss, logp, G: each may be NULL, not all; G may
  * be logits itself (same pitch).  Columns past V are neither read nor written.  Any alignment of whole elements works; rows of G that lie
- * on their 16 bytes as those of logits do take the vector path.  A row that counts needs a logit above -2.3e38 (its softmax is NaN
- * otherwise; -inf and the type's lowest value are fine beside one).  beta >= 0, 0 <= smoothing <= 1; 2*B*T < 2^31; ws on an
+ * on their 16 bytes as those of logits do take the vector path.  A row that counts needs its largest logit between -2.3e38 and
+ * 2.3e38 (its softmax is NaN otherwise; -inf and the type's lowest value are fine beside one).  beta >= 0, 0 <= smoothing <= 1; 2*B*T < 2^31; ws on an
  * 8-byte boundary. */
 dp_status dp_preference_loss(const void* logits, int64_t ldl, dp_dtype dt, int32_t B, int32_t T, int32_t V, const int32_t* targets,
                              const float* ref_logp, float beta, float smoothing, float scale, float* loss, float* logp, void* G,
@@ -388,7 +389,8 @@ size_t dp_preference_loss_ws_bytes(int32_t B, int32_t T);
  *   X = M / (||M||_F + eps);  `steps` times  A = X X^T, X <- a X + (b A + c A A) X  with (a, b, c) = coefs[3*k..]  [host, 3*steps];
  *   out [dev, (p, d) of out_dt, pitch ldo] = scale * X
  * (of the transpose where p > d: the same X).  All matrices run together.  Products are taken on fp16 operands of two terms (22 bits) with fp32
- * accumulation.  out may be M.  coefs whose polynomials exceed 1e6 on the singular values that can occur are DP_ERR_INVALID_ARG.
+ * accumulation; matrices of at most 64 by 256 in fp32.  out may be M; an output that is another matrix's output or M is
+ * DP_ERR_INVALID_ARG, and none may overlap another's otherwise.  coefs whose polynomials exceed 1e6 on the singular values that can occur are DP_ERR_INVALID_ARG.
  * ws: dp_orthogonalize_ws_bytes (M, out and scale are not looked at), on a 16-byte boundary.  p, d <= 2^20. */
 typedef struct {
   const void* M;  int64_t ldm;

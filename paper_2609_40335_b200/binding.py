@@ -135,7 +135,7 @@ def load():
     L.dp_add_noise_slice.argtypes = [vp, i64, i64, f32, f32, f32, C.c_uint64, C.c_uint32, C.c_uint32, vp]
     L.dp_noise_step_device.argtypes = [vp]
     L.dp_step_enqueue.argtypes = [vp, i32]
-    L.dp_layernorm.argtypes = [vp, i64, i32, i64, i32, vp, vp, i32, f32, vp, i64, vp, i64, vp, vp, vp]
+    L.dp_layernorm.argtypes = [vp, i64, i32, i64, i32, vp, vp, i32, f32, vp, i64, vp, i64, vp, vp, vp, vp]
     L.dp_layernorm_backward.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32, vp, i32, vp, vp, vp, i64, vp, vp, vp,
                                         vp, sz, vp, vp]
     L.dp_layernorm_backward_ws_bytes.argtypes = [i32, i32, i32]
@@ -675,13 +675,14 @@ def _raw(stream):
     return None if stream is None else _stream(stream)
 
 
-def dp_layernorm(X, gain, shift, eps: float, Y=None, X_hat=None, mean=None, rstd=None, p=None, stream=None):
+def dp_layernorm(X, gain, shift, eps: float, Y=None, X_hat=None, mean=None, rstd=None, p=None, dev_status=None, stream=None):
     """Y = X_hat*gain + shift and X_hat = (X - mean)*rstd over the last axis (its first p columns); mean, rstd: floats, one per
     row.  gain, shift: p elements, float32 or bfloat16, or None."""
     load()
-    st = _marshal().layernorm(_address["dp_layernorm"], X, gain, shift, Y, X_hat, mean, rstd, eps, p, _raw(stream))
+    st = _marshal().layernorm(_address["dp_layernorm"], X, gain, shift, Y, X_hat, mean, rstd, dev_status, eps, p, _raw(stream))
     if st is None:                             # one of these says what is wrong
-        _on_one_device((X, gain, shift, Y, X_hat, mean, rstd))
+        _on_one_device((X, gain, shift, Y, X_hat, mean, rstd, dev_status))
+        _dense(dev_status, (1,), torch.int32, "dev_status")
         p = p if p is not None else X.shape[-1]
         rows = math.prod(X.shape[:-1])
         _ln_params((gain, shift), p)

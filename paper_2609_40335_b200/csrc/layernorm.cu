@@ -254,6 +254,7 @@ struct LnForward {
   int whole, vec_y, vec_h;       // X's rows follow one another; outputs are written in 16-byte pieces (rows read in such)
   float eps;
   LnShape S;
+  int* dev_status;
   long long wait_limit;
 };
 
@@ -281,7 +282,9 @@ ln_forward_kernel(const LnForward P) {
   if (kAligned && warp == warps) {
     int b = 0;
     uint32_t phase = 1;                                  // of the use before
-    for (int k = 0; k < tiles; ++k) {
+    int issued = 0;
+    for (; issued < tiles; ++issued) {
+      const int k = issued;
       if (k >= S.buffers && !ptx::mbar_wait_own(empty + b, phase, P.wait_limit)) break;
       const long long first = r0 + (long long)k * S.groups;
       const int n = int(min((long long)S.groups, r1 - first));
@@ -290,6 +293,7 @@ ln_forward_kernel(const LnForward P) {
       ln_copy<T>(X + first * P.ldx, P.ldx, p, n, to, S.pitch, P.whole, full + b, lane, true);
       if (++b == S.buffers) { b = 0; phase ^= 1; }
     }
+    if (lane == 0) ptx::drain_issued_copies(full, S.buffers, uint32_t(issued));       // before the block ends, also where a wait has run out
     return;
   }
   const int per_row = S.lanes * S.W, group = tid / per_row;
@@ -305,7 +309,11 @@ ln_forward_kernel(const LnForward P) {
   uint32_t phase = 0;
   bool ok = true;
   for (int k = 0; k < tiles; ++k) {
-    if (kAligned && ok) ok = ptx::mbar_wait_own(full + b, phase, P.wait_limit);    // (one that ran out goes on: others meet it at barriers)
+    // a warp whose wait has run out goes on without waiting: others meet it at barriers
+    if (kAligned && ok && !ptx::mbar_wait_own(full + b, phase, P.wait_limit)) {
+      ok = false;
+      if (P.dev_status && lane == 0) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
+    }
     const long long row = r0 + (long long)k * S.groups + group;
     const bool mine = group < S.groups && row < r1;
     F2 v[NP][H];
@@ -418,7 +426,9 @@ ln_backward_kernel(const LnBackward P) {
     // ------------------------------------------------------------------ copies
     int b = 0;
     uint32_t phase = 1;                                  // of the use before
-    for (int k = 0; k < tiles; ++k) {
+    int issued = 0;
+    for (; issued < tiles; ++issued) {
+      const int k = issued;
       if (k >= S.buffers && !ptx::mbar_wait_own(empty + b, phase, P.wait_limit)) break;
       const int first = r0 + k * S.groups, n = min(S.groups, r1 - first);
       const T* g = G + (base + first) * P.ldg;
@@ -431,7 +441,8 @@ ln_backward_kernel(const LnBackward P) {
       ln_copy<T>(x, P.ldx, p, n, to_x, S.pitch, P.whole_x, full + b, lane, true);
       if (++b == S.buffers) { b = 0; phase ^= 1; }
     }
-    // (copies in flight land before the block ends: its other warps wait for every tile, and give up after the same time)
+    // copies in flight land before the block ends, also where a wait has run out
+    if (lane == 0) ptx::drain_issued_copies(full, S.buffers, uint32_t(issued));
   } else {
     // -------------------------------------------------------------------- work
     for (int c = tid; c < max(p, per_row * NP * N); c += warps * 32)
@@ -809,7 +820,7 @@ extern "C" {
 
 dp_status dp_layernorm(const void* X, int64_t ldx, dp_dtype dt, int64_t rows, int32_t p, const void* gain, const void* shift,
                        dp_dtype param_dt, float eps, void* Y, int64_t ldy, void* X_hat, int64_t ldh, float* mean, float* rstd,
-                       void* stream) {
+                       int32_t* dev_status, void* stream) try {
   if (!X || rows <= 0 || p <= 0 || ldx < p || (!Y && !X_hat && !mean && !rstd)) return DP_ERR_INVALID_ARG;
   if ((Y && ldy < p) || (X_hat && ldh < p) || !known_dtype(dt) || !known_dtype(param_dt)) return DP_ERR_INVALID_ARG;
   if (!std::isfinite(eps) || eps < 0.f || (Y && Y == X_hat)) return DP_ERR_INVALID_ARG;
@@ -819,16 +830,19 @@ dp_status dp_layernorm(const void* X, int64_t ldx, dp_dtype dt, int64_t rows, in
   if (!on_boundary(es, X, Y, X_hat) || !on_boundary(ps, gain, shift) || !on_boundary(4, mean, rstd)) return DP_ERR_ALIGNMENT;
   LnForward P{};
   P.X = X; P.ldx = ldx; P.gain = gain; P.shift = shift; P.param_dt = param_dt; P.Y = Y; P.ldy = ldy; P.H = X_hat; P.ldh = ldh;
-  P.mean = mean; P.rstd = rstd; P.rows = rows; P.p = p; P.eps = eps; P.wait_limit = g_wait_limit;
+  P.mean = mean; P.rstd = rstd; P.rows = rows; P.p = p; P.eps = eps; P.dev_status = dev_status;
+  P.wait_limit = g_wait_limit;
   const bool aligned = p * es % 16 == 0 && ln_vec(X, ldx, es);
   P.S = ln_shape(p, es, aligned);
   P.whole = aligned && ldx == p;
   P.vec_y = ln_vec(Y, ldy, es);
   P.vec_h = ln_vec(X_hat, ldh, es);
   return ln_run(dt, aligned, ln_pieces(P.S, p, es), P.S.W == 16, RunForward{P, (cudaStream_t)stream});
+} catch (...) {                                        // host memory for the set-up of a device
+  return DP_ERR_UNSUPPORTED;
 }
 
-size_t dp_layernorm_backward_ws_bytes(int32_t B, int32_t T, int32_t p) {
+size_t dp_layernorm_backward_ws_bytes(int32_t B, int32_t T, int32_t p) try {
   if (B <= 0 || T <= 0 || p <= 0 || p > kLnMaxCols) return 0;
   size_t most = 0;                                    // of either type of G and X
   for (const int es : {2, 4}) {
@@ -836,12 +850,14 @@ size_t dp_layernorm_backward_ws_bytes(int32_t B, int32_t T, int32_t p) {
     if (!parts.cluster) most = std::max(most, ln_partial_bytes(parts, B, p));
   }
   return most;
+} catch (...) {
+  return 0;
 }
 
 dp_status dp_layernorm_backward(const void* G, int64_t ldg, const void* X, int64_t ldx, dp_dtype dt, int32_t B, int32_t T, int32_t p,
                                 const void* gain, dp_dtype param_dt, const float* mean, const float* rstd, void* dX, int64_t lddx,
                                 float* gain_sums, float* shift_sums, float* sq, void* ws, size_t ws_bytes, int32_t* dev_status,
-                                void* stream) {
+                                void* stream) try {
   if (!G || !X || !mean || !rstd || B <= 0 || T <= 0 || p <= 0 || ldg < p || ldx < p) return DP_ERR_INVALID_ARG;
   if ((dX && lddx < p) || !known_dtype(dt) || !known_dtype(param_dt)) return DP_ERR_INVALID_ARG;
   const bool sums = gain_sums || shift_sums || sq;
@@ -885,6 +901,8 @@ dp_status dp_layernorm_backward(const void* G, int64_t ldg, const void* X, int64
   DP_CUDA_OK(cudaLaunchKernelEx(&cfg, ln_sums_kernel, (const float*)partials, parts.parts, p, gain_sums, shift_sums, sq));
   ++g_kernel_launches;
   return DP_OK;
+} catch (...) {
+  return DP_ERR_UNSUPPORTED;
 }
 
 }  // extern "C"

@@ -346,30 +346,32 @@ template <typename F> F function(PyObject* o) {
   return f;
 }
 
-// (address, X, gain, shift, Y, X_hat, mean, rstd, eps, p, stream)
+// (address, X, gain, shift, Y, X_hat, mean, rstd, dev_status, eps, p, stream)
 PyObject* layernorm(PyObject*, PyObject* const* a, Py_ssize_t na) {
-  if (na != 11) { PyErr_SetString(PyExc_TypeError, "layernorm takes 11 arguments"); return nullptr; }
+  if (na != 12) { PyErr_SetString(PyExc_TypeError, "layernorm takes 12 arguments"); return nullptr; }
   const auto call = function<decltype(&dp_layernorm)>(a[0]);
-  const at::Tensor* t[7];
-  enum { X, GAIN, SHIFT, Y, HAT, MEAN, RSTD };
+  const at::Tensor* t[8];
+  enum { X, GAIN, SHIFT, Y, HAT, MEAN, RSTD, STATUS };
   int64_t p, ldx, ldy, ldh;
   int32_t param;
   double eps;
   void* st;
-  if (!call || !here(a + 1, 7, t) || !t[X] || t[X]->dim() < 2 || dtype_of(*t[X]) == kOther) Py_RETURN_NONE;
+  if (!call || !here(a + 1, 8, t) || !t[X] || t[X]->dim() < 2 || dtype_of(*t[X]) == kOther) Py_RETURN_NONE;
   const auto type = t[X]->scalar_type();
-  if (!number(a[8], &eps) || !whole(a[9], t[X]->size(-1), &p) || !stream_of(a[10], &st) || p <= 0 || p > INT32_MAX) Py_RETURN_NONE;
+  if (!number(a[9], &eps) || !whole(a[10], t[X]->size(-1), &p) || !stream_of(a[11], &st) || p <= 0 || p > INT32_MAX) Py_RETURN_NONE;
   const int64_t last = t[X]->size(-1), rows = last ? t[X]->numel() / last : 0;
   if (!norm_params(t + GAIN, 2, p, &param) || !spaced(t[X], rows, p, type, &ldx) || !spaced(t[Y], rows, p, type, &ldy) ||
-      !spaced(t[HAT], rows, p, type, &ldh) || !dense(t[MEAN], rows, at::kFloat) || !dense(t[RSTD], rows, at::kFloat))
+      !spaced(t[HAT], rows, p, type, &ldh) || !dense(t[MEAN], rows, at::kFloat) || !dense(t[RSTD], rows, at::kFloat) ||
+      !dense(t[STATUS], 1, at::kInt))
     Py_RETURN_NONE;
   const void *x = pointer<const void>(t[X]), *gain = pointer<const void>(t[GAIN]), *shift = pointer<const void>(t[SHIFT]);
   void *y = pointer<void>(t[Y]), *hat = pointer<void>(t[HAT]);
   float *mean = pointer<float>(t[MEAN]), *rstd = pointer<float>(t[RSTD]);
+  int32_t* status = pointer<int32_t>(t[STATUS]);
   dp_status r;
   {
     const Unlock unlock;
-    r = call(x, ldx, dp_dtype(dtype_of(*t[X])), rows, int32_t(p), gain, shift, dp_dtype(param), float(eps), y, ldy, hat, ldh, mean, rstd, st);
+    r = call(x, ldx, dp_dtype(dtype_of(*t[X])), rows, int32_t(p), gain, shift, dp_dtype(param), float(eps), y, ldy, hat, ldh, mean, rstd, status, st);
   }
   return PyLong_FromLong(long(r));
 }

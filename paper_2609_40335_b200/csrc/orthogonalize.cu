@@ -41,6 +41,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <utility>
 #include <vector>
 
 #include "dp_common.cuh"
@@ -1120,6 +1121,20 @@ dp_status check_matrix(const dp_matrix_desc& D, bool pointers) {
   return DP_OK;
 }
 
+// No two matrices share an output, and no output is another matrix's input: matrices of a call run together.
+bool distinct_outputs(const dp_matrix_desc* mats, int n) {
+  std::vector<std::pair<const void*, int>> outs(n);
+  for (int k = 0; k < n; ++k) outs[k] = {mats[k].out, k};
+  std::sort(outs.begin(), outs.end());
+  for (int k = 1; k < n; ++k)
+    if (outs[k].first == outs[k - 1].first) return false;
+  for (int k = 0; k < n; ++k) {
+    const auto at = std::lower_bound(outs.begin(), outs.end(), std::make_pair(mats[k].M, 0));
+    if (at != outs.end() && at->first == mats[k].M && at->second != k) return false;
+  }
+  return true;
+}
+
 // The order in which matrices are taken: long sums first, so that the tiles of a last wave are the short ones.
 std::vector<int> ns_order(const dp_matrix_desc* mats, int n) {
   std::vector<int> order(n);
@@ -1142,7 +1157,7 @@ using namespace dpg;
 
 extern "C" {
 
-size_t dp_orthogonalize_ws_bytes(const dp_matrix_desc* mats, int32_t n) {
+size_t dp_orthogonalize_ws_bytes(const dp_matrix_desc* mats, int32_t n) try {
   if (!mats || n <= 0) return 0;
   for (int k = 0; k < n; ++k)
     if (check_matrix(mats[k], false) != DP_OK) return 0;
@@ -1155,10 +1170,12 @@ size_t dp_orthogonalize_ws_bytes(const dp_matrix_desc* mats, int32_t n) {
     most = std::max(most, need);
   }
   return ns_partial_bytes(n) + most;
+} catch (...) {
+  return 0;
 }
 
 dp_status dp_orthogonalize(const dp_matrix_desc* mats, int32_t n, dp_dtype dt, dp_dtype out_dt, const float* coefs, int32_t steps,
-                           float eps, void* ws, size_t ws_bytes, int32_t* dev_status, void* stream) {
+                           float eps, void* ws, size_t ws_bytes, int32_t* dev_status, void* stream) try {
   if (!mats || n <= 0 || !coefs || steps <= 0 || !std::isfinite(eps) || eps < 0.f) return DP_ERR_INVALID_ARG;
   if ((dt != DP_F32 && dt != DP_BF16) || (out_dt != DP_F32 && out_dt != DP_BF16)) return DP_ERR_INVALID_ARG;
   for (int k = 0; k < n; ++k) {
@@ -1166,6 +1183,7 @@ dp_status dp_orthogonalize(const dp_matrix_desc* mats, int32_t n, dp_dtype dt, d
     if (r != DP_OK) return r;
     if (!on_boundary(dt == DP_F32 ? 4 : 2, mats[k].M) || !on_boundary(out_dt == DP_F32 ? 4 : 2, mats[k].out)) return DP_ERR_ALIGNMENT;
   }
+  if (!distinct_outputs(mats, n)) return DP_ERR_INVALID_ARG;
   std::vector<NsStep> plan;
   if (!plan_steps(coefs, steps, plan)) return DP_ERR_INVALID_ARG;
   if (!ws || ws_bytes < dp_orthogonalize_ws_bytes(mats, n)) return DP_ERR_WORKSPACE;
@@ -1181,6 +1199,8 @@ dp_status dp_orthogonalize(const dp_matrix_desc* mats, int32_t n, dp_dtype dt, d
     if (r != DP_OK) return r;
   }
   return DP_OK;
+} catch (...) {                                        // host memory for a call of this size
+  return DP_ERR_UNSUPPORTED;
 }
 
 }  // extern "C"

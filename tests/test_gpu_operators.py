@@ -182,6 +182,32 @@ def test_layernorm_backward_parts_of_the_outputs():
         assert torch.equal(out, dx) and torch.equal(again, gs)
 
 
+@pytest.mark.parametrize("B,T,p,dtype", [(8, 300, 768, "bf16"), (2, 500, 4096, "f32"), (1, 4100, 64, "f32"), (3, 40, 7, "bf16")])
+def test_layernorm_wait_limit_leaves_the_context_usable(B, T, p, dtype):
+    """Waits that run out are reported, or the result is right; the same call is right afterwards."""
+    x, g = tensor((B, T, p), DT[dtype], 1), tensor((B, T, p), DT[dtype], 2)
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def run():
+        y, dx, mean, rstd = torch.zeros_like(x), torch.zeros_like(x), torch.zeros(B, T, device="cuda"), torch.zeros(B, T, device="cuda")
+        gs, ss = torch.zeros(B, p, device="cuda"), torch.zeros(B, p, device="cuda")
+        dp.dp_layernorm(x, None, None, 1e-5, Y=y, mean=mean, rstd=rstd, dev_status=st)
+        dp.dp_layernorm_backward(g, x, None, mean, rstd, dX=dx, gain_sums=gs, shift_sums=ss, dev_status=st)
+        torch.cuda.synchronize()
+        return y, dx, mean, rstd, gs, ss
+    want = run()
+    assert int(st.item()) == 0
+    L = dp.load()
+    before = L.dp_debug_set_wait_limit(0)
+    try:
+        got = run()
+    finally:
+        L.dp_debug_set_wait_limit(before)
+    assert int(st.item()) == dp.DP_DEV_TIMEOUT or all(torch.equal(a, b) for a, b in zip(got, want))
+    st.zero_()
+    assert all(torch.equal(a, b) for a, b in zip(run(), want)) and int(st.item()) == 0
+
+
 def test_layernorm_sums_are_the_vectors_of_the_clipped_step():
     """The norms and the clipped sums of gains and shifts, as dp_vector_norms and dp_clip_accumulate_vectors make them of G and X."""
     B, T, p, C = 5, 50, 320, 0.4

@@ -23,7 +23,7 @@ def lib():
 
 def layernorm(lib, **kw):
     a = dict(X=A[0], ldx=64, dt=1, rows=40, p=64, gain=A[1], shift=A[2], pdt=0, eps=1e-5, Y=A[3], ldy=64, H=A[4], ldh=64, mean=A[5],
-             rstd=A[6])
+             rstd=A[6], status=None)
     assert not set(kw) - set(a)
     a.update(kw)
     return lib.dp_layernorm(*a.values(), None)
@@ -87,11 +87,12 @@ def test_preference_loss(lib, kw, want):
     assert preference(lib, **kw) == want
 
 
-def orthogonalize(lib, n=1, dt=0, out_dt=0, coefs=((3.4445, -4.7750, 2.0315),) * 5, steps=None, eps=1e-7, ws=A[2], size=1 << 30, **kw):
+def orthogonalize(lib, n=1, dt=0, out_dt=0, coefs=((3.4445, -4.7750, 2.0315),) * 5, steps=None, eps=1e-7, ws=A[2], size=1 << 30, second=None, **kw):
     arr = (binding._MatrixDesc * 2)()
     for D in arr:
         for k, v in dict(dict(M=A[0], ldm=64, out=A[1], ldo=64, p=96, d=64, scale=1.0), **kw).items():
             setattr(D, k, v)
+    arr[1].M, arr[1].out = second or ((arr[0].M or 0) + (1 << 24), (arr[0].out or 0) + (1 << 24))
     flat = [c for s in coefs for c in s]
     return lib.dp_orthogonalize(arr, n, dt, out_dt, (C.c_float * max(1, len(flat)))(*flat), len(coefs) if steps is None else steps, eps, ws,
                                 size, None, None)
@@ -104,6 +105,8 @@ def orthogonalize(lib, n=1, dt=0, out_dt=0, coefs=((3.4445, -4.7750, 2.0315),) *
     (dict(coefs=((30.0, 30.0, 30.0),) * 3), INVALID), (dict(M=A[0] + 2), ALIGNMENT), (dict(out=A[1] + 2), ALIGNMENT),
     (dict(dt=1, M=A[0] + 1), ALIGNMENT), (dict(ws=None), WORKSPACE), (dict(size=1000), WORKSPACE), (dict(ws=A[2] + 8), ALIGNMENT),
     (dict(p=(1 << 20) + 1), UNSUPPORTED),
+    (dict(n=2, second=(A[0], A[1])), INVALID), (dict(n=2, second=(A[1], A[4])), INVALID), (dict(n=2, second=(A[3], A[0])), INVALID),
+    (dict(n=2, second=(A[0], A[4])), CUDA), (dict(n=2, M=A[1]), CUDA),
     (dict(), CUDA), (dict(n=2, coefs=((1.5, -0.5, 0.0),), dt=1, out_dt=1, M=A[0] + 2, ldm=65), CUDA)])
 def test_orthogonalize(lib, kw, want):
     assert orthogonalize(lib, **kw) == want
