@@ -285,7 +285,7 @@ ln_forward_kernel(const LnForward P) {
     int issued = 0;
     for (; issued < tiles; ++issued) {
       const int k = issued;
-      if (k >= S.buffers && !ptx::mbar_wait_own(empty + b, phase, P.wait_limit)) break;
+      if (k >= S.buffers && !ptx::warp_ok(ptx::mbar_wait_own(empty + b, phase, P.wait_limit))) break;
       const long long first = r0 + (long long)k * S.groups;
       const int n = int(min((long long)S.groups, r1 - first));
       uint8_t* to = smem + size_t(b) * at.tile;
@@ -429,7 +429,7 @@ ln_backward_kernel(const LnBackward P) {
     int issued = 0;
     for (; issued < tiles; ++issued) {
       const int k = issued;
-      if (k >= S.buffers && !ptx::mbar_wait_own(empty + b, phase, P.wait_limit)) break;
+      if (k >= S.buffers && !ptx::warp_ok(ptx::mbar_wait_own(empty + b, phase, P.wait_limit))) break;
       const int first = r0 + k * S.groups, n = min(S.groups, r1 - first);
       const T* g = G + (base + first) * P.ldg;
       const T* x = X + (base + first) * P.ldx;
