@@ -940,9 +940,11 @@ int tiles_of(Product product, int m, int n, int tile) {
   return product == kApply ? tm * ceil_div(n, tile) : tm * (tm + 1) / 2;
 }
 
-// How a group of matrices runs: on CTA pairs or single CTAs, the same for all products, since symmetric matrices are stored by
-// the tile; and how far A's error may grow in fused steps, 1 where each is by itself.  Whichever takes less time in whole waves of K steps (a pair's is twice as long), a launch
-// counting three more.
+// How a group of matrices runs: on CTA pairs or single CTAs, the same for all products, since symmetric matrices are stored by the tile; and
+// how far A's error may grow in fused steps, 1 where each is by itself.  Whichever takes less time in whole waves of K steps, a launch counting
+// three more.  A pair's K step is 1.7 times as long for twice the work per CTA: a single CTA's reads 64 KB of shared memory's tiles anew for half
+// of the MMAs (tensor pipe at 45 %).  Pairs against single CTAs: layers of 6 blocks of width 768 1.43 ms against 1.56, of 24 of 1024 13.3
+// against 14.5; of one of 768, which leave pairs without work, 0.52 against 0.40.
 struct NsForm { bool pair; double growth; };
 NsForm choose_form(const std::vector<NsShape>& shapes, const std::vector<NsStep>& plan, bool bf16_out) {
   int least_m = shapes[0].m;
@@ -963,7 +965,7 @@ NsForm choose_form(const std::vector<NsShape>& shapes, const std::vector<NsStep>
         longest = std::max(longest, k);
       }
       const double waves = double((tiles + units - 1) / units);
-      cost[q] = 3.0 + (f.pair ? 2.0 : 1.0) * std::max(double(longest), waves * double(work) / double(tiles));
+      cost[q] = 3.0 + (f.pair ? 1.7 : 1.0) * std::max(double(longest), waves * double(work) / double(tiles));
     }
     double all = 0;
     for (size_t k = 0; k < plan.size();) {
