@@ -375,8 +375,8 @@ size_t dp_layernorm_backward_ws_bytes(int32_t B, int32_t T, int32_t p);
  *   h_i = beta * ((l_c - ref_c) - (l_r - ref_r)),   loss[i] = -(1 - smoothing) log s(h_i) - smoothing log s(-h_i)
  * (s the logistic function), logp [dev, (B, 2) floats] = l, and G [dev, (2*B*T, V) of dt] = scale * d loss / d logits, the G of an
  * LM head in dp_ghost_norms and dp_clip_accumulate* with sequences of 2*T tokens.  loss, logp, G: each may be NULL, not all; G may
- * be logits itself (same pitch).  Columns past V are neither read nor written.  Any alignment of whole elements works; rows of G that lie
- * on their 16 bytes as those of logits do take the vector path.  A row that counts needs its largest logit between -2.3e38 and
+ * be logits itself (same pitch).  Columns past V are neither read nor written.  Any alignment of whole elements works.
+ * A row that counts needs its largest logit between -2.3e38 and
  * 2.3e38 (its softmax is NaN otherwise; -inf and the type's lowest value are fine beside one).  beta >= 0, 0 <= smoothing <= 1; 2*B*T < 2^31; ws on an
  * 8-byte boundary. */
 dp_status dp_preference_loss(const void* logits, int64_t ldl, dp_dtype dt, int32_t B, int32_t T, int32_t V, const int32_t* targets,

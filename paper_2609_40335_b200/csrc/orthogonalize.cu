@@ -12,7 +12,7 @@
 // bf16 product per product is off by 1e-2 after five steps, two bf16 terms by 2e-5, these by what the sums round.
 // An MMA rounds its sum towards zero, by as much as the sum is large.  So sums are taken in K steps of 64, each in an
 // accumulator of its own, that the epilogue adds up in registers to nearest: error of DistilGPT2's updates against 64 bits 2.2e-5
-// with one accumulator per tile (the diagonal of A, a sum of squares, came out 6e-6 too small at K = 3072).
+// with one accumulator per tile (the diagonal of A, a sum of squares, came out 6e-6 too small in the longest sums).
 //
 // Nothing is added to a product but on the diagonal, so no epilogue reads matrices: B = a I + b A + c A A = c A A' + a I with
 // A' = A + (b / c) I, which differs from A on the diagonal: A' is a copy of the diagonal's tiles.  X' = B X.  (Completing the square,

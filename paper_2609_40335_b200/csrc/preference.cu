@@ -203,6 +203,20 @@ __device__ __forceinline__ double token_logp(float x, const Softmax& a) {
   return (fma(double(x), double(kLog2e), -c) - log2(double(a.s))) * 0.6931471805599453;
 }
 
+// 16 bytes from byte `off` of a and b, a multiple of two
+__device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, uint32_t off) {
+  uint32_t w[5];
+  switch (off >> 2) {
+    case 0: w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; break;
+    case 1: w[0] = a.y; w[1] = a.z; w[2] = a.w; w[3] = b.x; w[4] = b.y; break;
+    case 2: w[0] = a.z; w[1] = a.w; w[2] = b.x; w[3] = b.y; w[4] = b.z; break;
+    default: w[0] = a.w; w[1] = b.x; w[2] = b.y; w[3] = b.z; w[4] = b.w; break;
+  }
+  const uint32_t bits = (off & 3) * 8;
+  return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
+                    __funnelshift_r(w[3], w[4], bits));
+}
+
 // This thread's share of a row's gradient: f = c / (sum of exponentials).  target < 0: zeros.
 template <typename T>
 __device__ __forceinline__ void write_gradient(const T* x, T* g, int V, int target, float c, float row_c, float inv, int tid, int n) {
@@ -212,11 +226,17 @@ __device__ __forceinline__ void write_gradient(const T* x, T* g, int V, int targ
     const float e = f * exp2_fast(Softmax::exponent(v, row_c));
     return k == target ? c - e : -e;
   };
-  // quads where reads and writes share their alignment, and the columns around them
-  const int head = head_of(g, V);
-  const bool aligned = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(g)) & 15) == 0;
-  const int quads = aligned || target < 0 ? (V - head) / N : 0;
-  const uint4* xq = reinterpret_cast<const uint4*>(x + head);
+  // quads of g, and the columns around them.  Where x lies otherwise on its 16 bytes (dense logits, a G whose rows are padded), a quad is put
+  // together from two of x, both within the row, the first `off` bytes before it.  ((8, 2 x 128, 50257) bf16: 112 us against 103 with the same
+  // alignment, and 230 element by element.)
+  int head = head_of(g, V);
+  const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(x + head) & 15);
+  int quads = (V - head) / N;
+  if (off && target >= 0) {
+    if (head * int(sizeof(T)) < int(off)) head = min(V, head + N);
+    quads = max(0, int(((long long)(V - head) * int(sizeof(T)) + int(off)) / 16) - 1);
+  }
+  const uint4* xq = reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(x + head) - off);
   uint4* gq = reinterpret_cast<uint4*>(g + head);
   // x and g may be one tensor: a thread has read what it writes
   auto one = [&](int k, const uint4& q) {
@@ -234,6 +254,8 @@ __device__ __forceinline__ void write_gradient(const T* x, T* g, int V, int targ
   };
   if (target < 0) {
     for (int k = tid; k < quads; k += n) __stcs(gq + k, make_uint4(0u, 0u, 0u, 0u));
+  } else if (off) {
+    for (int k = tid; k < quads; k += n) one(k, shifted(xq[k], xq[k + 1], off));
   } else {
     int k = tid;
     for (; k + (U - 1) * n < quads; k += U * n) {

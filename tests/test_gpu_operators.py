@@ -305,6 +305,21 @@ def test_preference_loss_other_alignment_of_the_gradient_and_in_place(dtype):
     surroundings_untouched(z, V + 3, 2)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,T,V", [(1, 9, 1), (1, 9, 7), (1, 9, 8), (1, 9, 16), (1, 9, 17), (1, 9, 33), (1, 9, 40), (40, 20, 100), (40, 20, 1001),
+                                   (1, 9, 5003)])
+def test_preference_gradient_where_rows_of_logits_and_gradient_lie_differently(dtype, B, T, V):
+    """Every difference of the two within 16 bytes."""
+    x, t, ref = pref_inputs(B, T, V, dtype, 5, pad=5)
+    want = torch.empty(B, 2 * T, V + 5, dtype=DT[dtype], device="cuda")[..., :V]
+    dp.dp_preference_loss(x, t, ref, 0.1, G=want)
+    for pad in range(8):
+        g = tensor((B, 2 * T, V), DT[dtype], 3, pitch=V + pad, offset=pad)
+        dp.dp_preference_loss(x, t, ref, 0.1, G=g)
+        assert torch.equal(g, want), pad
+        surroundings_untouched(g, V + pad, pad)
+
+
 def test_preference_loss_alone_and_in_place_on_long_rows():
     """Rows of a whole CTA: loss and log-probabilities are the same without a gradient, the gradient the same in place."""
     B, T, V = 4, 40, 50257
