@@ -53,7 +53,8 @@ def preference_loss(logits, targets, ref, beta, smoothing=0.0, scale=1.0):
                     soft[q, t] = (k, e / e.sum())
         r = np.zeros(2) if ref is None else np.asarray(ref[i], dtype=np.float64)
         h = beta * ((logp[i, 0] - r[0]) - (logp[i, 1] - r[1]))
-        loss[i] = (1 - smoothing) * _softplus(-h) + smoothing * _softplus(h)
+        # a term of weight 0 is not there, also where the other one's h is infinite (a target whose logit is -inf)
+        loss[i] = sum(w * _softplus(v) for w, v in ((1 - smoothing, -h), (smoothing, h)) if w > 0)
         slope = scale * beta * (smoothing * _logistic(h) - (1 - smoothing) * _logistic(-h))
         for (q, t), (k, p) in soft.items():
             c = slope if q == 0 else -slope

@@ -274,12 +274,15 @@ __device__ __forceinline__ void write_gradient(const T* x, T* g, int V, int targ
 __device__ __forceinline__ double softplus(double x) { return fmax(x, 0.0) + log1p(exp(-fabs(x))); }
 __device__ __forceinline__ double logistic(double x) { return 1.0 / (1.0 + exp(-x)); }
 
+// A term of weight 0 is not there: h is infinite where a target's logit is -inf, and its other term 0.
+__device__ __forceinline__ double weighted(double w, double v) { return w > 0.0 ? w * v : 0.0; }
+
 // The factor of a pair's preferred rows (the others' is its negative); its loss and log-probabilities if `write`.
 __device__ float pair_loss(const PrefParams& P, int pair, double lc, double lr, bool write) {
   const double rc = P.ref ? double(P.ref[2 * pair]) : 0.0, rr = P.ref ? double(P.ref[2 * pair + 1]) : 0.0;
   const double h = double(P.beta) * ((lc - rc) - (lr - rr)), e = double(P.smoothing);
   if (write) {
-    if (P.loss) P.loss[pair] = float((1.0 - e) * softplus(-h) + e * softplus(h));
+    if (P.loss) P.loss[pair] = float(weighted(1.0 - e, softplus(-h)) + weighted(e, softplus(h)));
     if (P.logp) { P.logp[2 * pair] = float(lc); P.logp[2 * pair + 1] = float(lr); }
   }
   return float(double(P.scale) * double(P.beta) * (e * logistic(h) - (1.0 - e) * logistic(-h)));

@@ -370,6 +370,29 @@ def test_preference_loss_numbers_that_are_not_finite_stay_in_their_pair():
     assert torch.isnan(bad[0][1]) and torch.isnan(bad[2][1]).all() and torch.isnan(bad[0][2])
 
 
+@pytest.mark.parametrize("V", [50, 20000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("smoothing", [0.0, 0.1, 1.0])
+def test_preference_loss_of_answers_that_cannot_be(dtype, smoothing, V):
+    """A target whose logit is -inf: loss 0 or inf as the definition has it, gradients that are numbers, other pairs as they were."""
+    x, t, ref = pref_inputs(3, 4, V, dtype, 10)
+    t[:] = 3
+    x[1, 6, 3] = x[2, 1, 3] = float("-inf")                           # the other answer, the preferred one
+    loss, logp, G = torch.empty(3, device="cuda"), torch.empty(3, 2, device="cuda"), torch.empty_like(x)
+    dp.dp_preference_loss(x, t, ref, 0.3, loss=loss, logp=logp, G=G, smoothing=smoothing)
+    wl, wp, wg = O.preference_loss(f64(x), t.cpu().numpy(), f64(ref), 0.3, smoothing)
+    assert (f64(loss)[1:] == wl[1:]).all() and {0.0: wl[1] == 0, 1.0: wl[2] == 0}.get(smoothing, True)
+    assert (np.isneginf(f64(logp)) == np.isneginf(wp)).all() and np.isneginf(wp).sum() == 2
+    # a logit's exponent is 20 log2 e at most: 29 U, twice for its row's sum, and as in check_pref otherwise; the factor is beta or 0
+    # where h is infinite, and has the rounding of 8 tokens and of ref else
+    e = 29 * (U + 2 ** -26) + 2 ** -22
+    row = e + (V / 500 + 40) * U + 4 * U * 29
+    h_err = 0.3 * (8 * row + 2 * U * (np.abs(wp[0]).sum() + np.abs(f64(ref[0])).sum()))
+    assert abs(f64(loss)[0] - wl[0]) <= h_err + 2 * U * wl[0]
+    room = np.abs(wg) * (2 * row + 4 * U + np.array([np.expm1(h_err), 0, 0])[:, None, None]) + 0.3 * 2 * U
+    close(G, wg, room, DT[dtype])
+
+
 @pytest.mark.parametrize("shift", [3e4, -2e5])
 def test_preference_loss_large_logits(shift):
     """The maximum's rounding cancels: logits far from zero give what the same logits near zero give, as far as they are the same."""

@@ -64,3 +64,20 @@ def test_newton_schulz_acts_on_the_singular_values(shape):
     for a, b, c in coefs:
         s = a * s + b * s ** 3 + c * s ** 5
     assert np.abs(O.orthogonalize(M, coefs, 1e-7, 1.5) - 1.5 * (u * s) @ vt).max() < 1e-12
+
+
+@pytest.mark.parametrize("smoothing", [0.0, 0.1, 1.0])
+def test_preference_loss_of_answers_that_cannot_be(smoothing):
+    """A target at -inf: h is infinite, and a term of weight 0 is not in the loss."""
+    rng = np.random.default_rng(4)
+    x, t = rng.normal(size=(2, 4, 5)), np.ones((2, 2, 2), dtype=int)
+    x[0, 3, 1] = x[1, 0, 1] = -np.inf                # the other answer, the preferred one
+    loss, logp, G = O.preference_loss(x, t, None, 0.5, smoothing)
+    want = {0.0: [0.0, np.inf], 0.1: [np.inf, np.inf], 1.0: [np.inf, 0.0]}[smoothing]
+    assert list(loss) == want
+    assert logp[0, 1] == -np.inf and logp[1, 0] == -np.inf and np.isfinite(logp[0, 0]) and np.isfinite(logp[1, 1])
+    soft = np.exp(x) / np.exp(x).sum(-1, keepdims=True)
+    for i, slope in enumerate((0.5 * smoothing, -0.5 * (1 - smoothing))):        # beta (e s(h) - (1 - e) s(-h)) at either end
+        for r in range(4):
+            c = slope if r < 2 else -slope
+            assert np.abs(G[i, r] - c * (np.eye(5)[1] - soft[i, r])).max() < 1e-15
