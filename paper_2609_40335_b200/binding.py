@@ -249,10 +249,16 @@ def _outputs(tensors):
     return (C.c_void_p * n).from_buffer(buf), (C.c_int64 * n).from_buffer(buf, 8 * n)
 
 
-def _ws(nbytes: int, ws: Optional[torch.Tensor], device) -> torch.Tensor:
+def _ws(nbytes: int, ws: Optional[torch.Tensor], device, stream) -> torch.Tensor:
+    """The caller's workspace, or a new one of `stream`'s own memory: what the allocator hands out for another stream may
+    still be in use there, and could be handed out there again while the call runs."""
     if ws is not None:
         return ws
-    return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    make = lambda: torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    if stream is None or device.type != "cuda":            # (a tensor elsewhere is refused by the call's own checks)
+        return make()
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream), device=device)):
+        return make()
 
 
 @dataclass
@@ -295,7 +301,7 @@ def dp_ghost_norms(layers: Sequence[Linear], B: int, T: int, sq: torch.Tensor, w
     arr = _descs(layers)
     dt = _dt(layers[0].A)
     need = int(L.dp_ghost_norms_ws_bytes(arr, len(layers), dt, B, T))
-    ws = _ws(need, ws, sq.device)
+    ws = _ws(need, ws, sq.device, stream)
     st = L.dp_ghost_norms(arr, len(layers), dt, B, T, _ptr(sq), _ptr(ws), ws.numel() * ws.element_size(),
                           _ptr(dev_status), _stream(stream))
     _check(st, "dp_ghost_norms")
@@ -308,7 +314,7 @@ def dp_embed_norms(ids: torch.Tensor, G: torch.Tensor, V: int, sq: torch.Tensor,
     B, T = ids.shape
     d = d if d is not None else G.shape[-1]
     need = int(L.dp_embed_norms_ws_bytes(B, T, d))
-    ws = _ws(need, ws, sq.device)
+    ws = _ws(need, ws, sq.device, stream)
     st = L.dp_embed_norms(_ptr(ids), _ptr(G), _rows_ld(G), _dt(G), B, T, d, V, _ptr(sq),
                           _ptr(first_occ), _ptr(ws), ws.numel() * ws.element_size(),
                           _ptr(dev_status), _stream(stream))
@@ -348,7 +354,7 @@ def dp_vector_norms(params: Sequence[Vector], B: int, T: int, sq: torch.Tensor, 
     L = load()
     arr = _vdescs(params)
     need = int(L.dp_vector_norms_ws_bytes(arr, len(params), B, T))
-    ws = _ws(need, ws, sq.device)
+    ws = _ws(need, ws, sq.device, stream)
     st = L.dp_vector_norms(arr, len(params), _dt(params[0].G), B, T, _ptr(sq), _ptr(ws),
                            ws.numel() * ws.element_size(), _stream(stream))
     _check(st, "dp_vector_norms")
@@ -364,7 +370,7 @@ def dp_clip_accumulate_vectors(params: Sequence[Vector], B: int, T: int, sq, C_:
     n = len(params)
     optr, _ = _outputs(outs)
     need = int(L.dp_clip_accumulate_vectors_ws_bytes(arr, n, B, T))
-    ws = _ws(need, ws, outs[0].device)
+    ws = _ws(need, ws, outs[0].device, stream)
     if noise is None:
         with_noise, sigma, scale, seed, tids, step = 0, 0.0, 1.0, 0, None, 0
     else:
@@ -397,7 +403,7 @@ def dp_tied_cross_term(ids, G_emb, A_lm, G_lm, V: int, sq=None, cross=None, d=No
     d = d if d is not None else G_emb.shape[-1]
     need = int(L.dp_tied_cross_term_ws_bytes(B, T, d, V))
     dev = G_emb.device
-    ws = _ws(need, ws, dev)
+    ws = _ws(need, ws, dev, stream)
     _one_dtype((G_emb, A_lm, G_lm), "cross term of tensors")
     st = L.dp_tied_cross_term(_ptr(ids), _ptr(G_emb), _rows_ld(G_emb), _ptr(A_lm), _rows_ld(A_lm),
                               _ptr(G_lm), _rows_ld(G_lm), _dt(G_emb), B, T, d, V, _ptr(sq),
@@ -433,7 +439,7 @@ def dp_clip_accumulate(A, G, sq, C_: float, out, beta: float = 0.0, d=None, p=No
     p = p if p is not None else G.shape[-1]
     dt = _dt(A)
     need = int(L.dp_clip_accumulate_ws_bytes(dt, B, T, d, p))
-    ws = _ws(need, ws, out.device)
+    ws = _ws(need, ws, out.device, stream)
     st = L.dp_clip_accumulate(_ptr(A), _rows_ld(A), _ptr(G), _rows_ld(G), dt, B, T, d, p, _ptr(sq),
                               float(C_), _ptr(clip), _ptr(out), out.stride(0), float(beta), _ptr(ws),
                               ws.numel() * ws.element_size(), _ptr(dev_status), _stream(stream))
@@ -455,7 +461,7 @@ def dp_clip_accumulate_grouped(layers: Sequence[Linear], B: int, T: int, sq, C_:
     n = len(layers)
     optr, ldos = _outputs(outs)
     need = int(L.dp_clip_accumulate_grouped_ws_bytes(arr, n, dt, B, T))
-    ws = _ws(need, ws, outs[0].device)
+    ws = _ws(need, ws, outs[0].device, stream)
     st = L.dp_clip_accumulate_grouped(arr, n, dt, B, T, _ptr(sq), float(C_), _ptr(clip), optr, ldos,
                                       float(beta), _ptr(ws), ws.numel() * ws.element_size(),
                                       _ptr(dev_status), _stream(stream))
@@ -475,7 +481,7 @@ def dp_clip_accumulate_noise_grouped(layers: Sequence[Linear], B: int, T: int, s
     optr, ldos = _outputs(outs)
     tids = (C.c_uint32 * n)(*[int(t) for t in tensor_ids])
     need = int(L.dp_clip_accumulate_grouped_ws_bytes(arr, n, dt, B, T))
-    ws = _ws(need, ws, outs[0].device)
+    ws = _ws(need, ws, outs[0].device, stream)
     st = L.dp_clip_accumulate_noise_grouped(arr, n, dt, B, T, _ptr(sq), float(C_), _ptr(clip), optr,
                                             ldos, float(beta), float(sigma), float(scale),
                                             int(seed) & (2 ** 64 - 1), tids, int(step), _ptr(ws),
@@ -492,7 +498,7 @@ def dp_clip_accumulate_embed_noise(ids, G, V: int, sq, C_: float, out, sigma: fl
     B, T = ids.shape
     d = d if d is not None else G.shape[-1]
     need = int(L.dp_clip_accumulate_embed_ws_bytes(B, T, d, V))
-    ws = _ws(need, ws, out.device)
+    ws = _ws(need, ws, out.device, stream)
     st = L.dp_clip_accumulate_embed_noise(_ptr(ids), _ptr(G), _rows_ld(G), _dt(G), B, T, d, V, _ptr(sq),
                                           float(C_), _ptr(clip), _ptr(out), out.stride(0), float(beta),
                                           float(sigma), float(scale), int(seed) & (2 ** 64 - 1),
@@ -508,7 +514,7 @@ def dp_clip_accumulate_embed(ids, G, V: int, sq, C_: float, out, beta: float = 0
     B, T = ids.shape
     d = d if d is not None else G.shape[-1]
     need = int(L.dp_clip_accumulate_embed_ws_bytes(B, T, d, V))
-    ws = _ws(need, ws, out.device)
+    ws = _ws(need, ws, out.device, stream)
     st = L.dp_clip_accumulate_embed(_ptr(ids), _ptr(G), _rows_ld(G), _dt(G), B, T, d, V, _ptr(sq),
                                     float(C_), _ptr(clip), _ptr(out), out.stride(0), float(beta),
                                     _ptr(perm), _ptr(seg), _ptr(ws), ws.numel() * ws.element_size(),
@@ -520,7 +526,7 @@ def dp_embed_sort(ids, V: int, perm, seg, ws=None, dev_status=None, stream=None)
     """Stable counting sort of the B*T token ids: perm (B*T int32), seg (V+1 int32)."""
     L = load()
     B, T = ids.shape
-    ws = _ws(int(L.dp_embed_sort_ws_bytes(B, T, V)), ws, ids.device)
+    ws = _ws(int(L.dp_embed_sort_ws_bytes(B, T, V)), ws, ids.device, stream)
     st = L.dp_embed_sort(_ptr(ids), B, T, V, _ptr(perm), _ptr(seg), _ptr(ws),
                          ws.numel() * ws.element_size(), _ptr(dev_status), _stream(stream))
     _check(st, "dp_embed_sort")
@@ -532,7 +538,7 @@ def dp_clip_accumulate_embed_sorted(ids, G, V: int, sq, C_: float, out, perm, se
     L = load()
     B, T = ids.shape
     d = d if d is not None else G.shape[-1]
-    ws = _ws(int(L.dp_clip_accumulate_embed_ws_bytes(B, T, d, V)), ws, out.device)
+    ws = _ws(int(L.dp_clip_accumulate_embed_ws_bytes(B, T, d, V)), ws, out.device, stream)
     st = L.dp_clip_accumulate_embed_sorted(_ptr(ids), _ptr(G), _rows_ld(G), _dt(G), B, T, d, V,
                                            _ptr(sq), float(C_), _ptr(clip), _ptr(out), out.stride(0),
                                            float(beta), _ptr(perm), _ptr(seg), _ptr(ws),
@@ -653,14 +659,10 @@ def _rows(t: Optional[torch.Tensor], rows: int, p: int, dtype, what: str) -> int
 
 
 def _scratch(need: int, ws: Optional[torch.Tensor], device, stream) -> torch.Tensor:
-    """The caller's workspace or a new one, which the allocator keeps until `stream` is through with it."""
-    if ws is None:
-        ws = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
-        if stream is not None:
-            ws.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream)))
-    elif not ws.is_contiguous():
+    """_ws, and complains of a workspace with holes."""
+    if ws is not None and not ws.is_contiguous():
         _complain("the workspace must be contiguous")
-    return ws
+    return _ws(need, ws, device, stream)
 
 
 def _ln_params(tensors, p: int) -> None:

@@ -524,12 +524,13 @@ def orthogonal_updates(ds: DeviceStep, updates: Optional[Dict[str, torch.Tensor]
     """After a step: the noised sums of the block linears orthogonalised, each scaled by scale * sqrt(max(1, p / d)) so that an
     update's entries are alike whatever the layer's shape.  Post-processing of Eq. 3's output, so it costs no privacy.  The tables, the
     head and the vectors keep their sums.  updates: tensors by the names of ds.outs, fp32 or all bf16 (the
-    sums themselves do); made where None."""
+    sums themselves do); made where None, as tensors of `stream`."""
     names = [f"linear{k}" for k in range(len(ds.linears))]
     if not names:
         return {}
     if updates is None:
-        updates = {n: torch.empty_like(ds.outs[n]) for n in names}
+        with torch.cuda.stream(stream if stream is None or isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream)):
+            updates = {n: torch.empty_like(ds.outs[n]) for n in names}
     mats = [ds.outs[n] for n in names]
     dp.dp_orthogonalize(mats, [updates[n] for n in names], scales=[scale * max(1.0, m.shape[0] / m.shape[1]) ** 0.5 for m in mats],
                         coefs=coefs, eps=eps, ws=ws, dev_status=ds.dev_status, stream=stream)

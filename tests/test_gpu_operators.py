@@ -623,3 +623,57 @@ def test_binding_refuses_what_would_be_misread():
         with pytest.raises(dp.DpGhostError):
             dp.dp_orthogonalize(mats, outs, **kw)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("raw", [False, True])
+@pytest.mark.parametrize("call", ["preference", "orthogonalize", "backward", "norms"])
+def test_workspaces_of_the_calls_themselves_are_not_in_use_on_another_stream(call, raw):
+    """A tensor freed while the current stream has yet to read it, then a call on another stream without a workspace of the same size."""
+    side = torch.cuda.Stream()
+    stream = side.cuda_stream if raw else side
+    if call == "preference":
+        B, T, V = 40, 500, 64
+        x, t, ref = pref_inputs(B, T, V, "f32", 1)
+        loss = torch.empty(B, device="cuda")
+        need, run = dp.dp_preference_loss_ws_bytes(B, T), lambda s: dp.dp_preference_loss(x, t, ref, 0.1, loss=loss, stream=s)
+        out = [loss]
+    elif call == "orthogonalize":
+        m = [tensor((200, 200), torch.float32, 1)]
+        out = [torch.empty_like(m[0])]
+        need, run = dp.dp_orthogonalize_ws_bytes(m), lambda s: dp.dp_orthogonalize(m, out, stream=s)
+    elif call == "backward":
+        B, T, p = 16, 640, 776
+        x, g = tensor((B, T, p), torch.bfloat16, 1), tensor((B, T, p), torch.bfloat16, 2)
+        mean, rstd = torch.zeros(B, T, device="cuda"), torch.ones(B, T, device="cuda")
+        out = [torch.empty(B, p, device="cuda")]
+        need = dp.dp_layernorm_backward_ws_bytes(B, T, p)
+        run = lambda s: dp.dp_layernorm_backward(g, x, None, mean, rstd, gain_sums=out[0], stream=s)
+    else:
+        B, T = 32, 256
+        layers = [dp.Linear(tensor((B, T, 512), torch.bfloat16, 1), tensor((B, T, 512), torch.bfloat16, 2))]
+        out = [torch.zeros(B, device="cuda")]
+        need = dp.dp_ghost_norms_ws_bytes(layers, B, T)
+
+        def run(s):
+            with torch.cuda.stream(side):
+                out[0].zero_()
+            dp.dp_ghost_norms(layers, B, T, out[0], stream=s)
+    assert need > 0
+    run(stream)                                                       # the allocator's pools and the kernels are set up
+    torch.cuda.synchronize()
+    want = [o.clone() for o in out]
+    for o in out:
+        o.fill_(5)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    bait = torch.full((need,), 7, dtype=torch.uint8, device="cuda")
+    kept = torch.empty_like(bait)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)                                    # some 100 ms
+    kept.copy_(bait)
+    del bait
+    run(stream)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(out, want))
+    torch.cuda.synchronize()
+    assert (kept == 7).all()
