@@ -21,11 +21,14 @@
 // instead.)
 //
 // Several steps go by A alone where X is longer than high: A_1 = B_0 A_0 B_0 and so on, all of them symmetric products of m x m, and X
-// meets the product of the Bs once at the end.  Five steps at once take 48 % less work for a GPT-2 block, 2 + 2 + 1 24 %.  A's error grows by
-// max |B|^2 a step (11.8 for the usual quintic) relative to its small eigenvalues, B = a I + ... sees it next to a.  Errors of the updates of
+// meets the product of the Bs once at the end.  For a GPT-2 block 3 + 2 steps at once take 36 % less work, 2 + 2 + 1 24 %.  A's error
+// grows by max |B|^2 a step (11.8 for the usual quintic) relative to its small eigenvalues, B = a I + ... sees it next to a.  Errors of the updates of
 // layers of d = 256, 768, 1000 (and the square one among them), in 1e-6: one by one 2.4 (1.4), 1.3 (1.4), 1.4 (1.4); two at once 1.9
 // (3.2), 2.8 (3.3), 3.4 (3.2); three 8.9 (5.4), 3.2 (4.3), 2.0 (3.6); five 22 (170), 13 (60), 14 (48); plain fp32 products
-// 2.5 (1.7), 2.8 (2.6), 3.3 (2.8).  So bf16 updates, whose rounding is 1.7e-3, take all steps at once, and fp32 updates two from m = 512 on.
+// 2.5 (1.7), 2.8 (2.6), 3.3 (2.8).  What grows is largest beside one dominant direction, where the others, 1e-3 of it, are amplified 485 times:
+// five steps at once then are 2.3e-2 off (of (512, 1500); plain fp32 products 1.5e-4), 3 + 2 less than shows beside bf16's rounding, 1.7e-3.  So bf16
+// updates take three steps at once.  fp32 ones take two from m = 640 on, where no such matrix was more than 1.3 times as far off as plain fp32
+// products make it (at (512, 2048) 1.6 times, 4.3e-6 against 2.7e-6).
 //
 // A and A A are symmetric: tiles on and below the diagonal are computed and stored, and a product that needs one above it reads the
 // stored one with rows and columns exchanged (the tensor core takes either order).
@@ -949,7 +952,7 @@ struct NsForm { bool pair; double growth; };
 NsForm choose_form(const std::vector<NsShape>& shapes, const std::vector<NsStep>& plan, bool bf16_out) {
   int least_m = shapes[0].m;
   for (const NsShape& s : shapes) least_m = std::min(least_m, s.m);
-  const double most = bf16_out ? 3e4 : least_m >= 512 ? 13.0 : 1.0;    // five, two and one of the usual quintic's steps
+  const double most = bf16_out ? 150.0 : least_m >= 640 ? 13.0 : 1.0;   // three, two and one of the usual quintic's steps
   NsForm best{};
   double least = INFINITY;
   for (int form = 0; form < 4; ++form) {

@@ -514,6 +514,60 @@ def test_orthogonalize_extreme_inputs():
     assert torch.equal(z, fresh)
 
 
+# Closer bounds.  An accumulator of the products holds 64 of K in twelve MMAs, whose sums are truncated by 2^-23 at most each, and is added to
+# nearest to the others'; two terms hold 22 bits of each operand, and the product of the low ones is left out.  Relative to the sum of the terms'
+# magnitudes:
+def product_error(K):
+    return 3 * 2.0 ** -22 + 12 * 2.0 ** -23 + math.ceil(K / 64) * U
+
+
+def dominated_room(shape, at_once):
+    """Error of the quintic's result, relative to its norm, on a matrix with one direction of singular value near 1 and others so small that
+    all steps amplify them by a = 3.4445.  With e = product_error: A is e off to begin with; A' = B A B is off by a^2 times that and by its
+    three products, a^2 e each (B's goes through b A B, less than that).  B, which is a I there, is off by |b| times A's error and its own e.
+    X and every X' = B X are off by e beside the large direction, which the steps left amplify.  The result's norm is 0.68 at least."""
+    a, b = QUINTIC[0][0], abs(QUINTIC[0][1])
+    e, total, left = product_error(max(shape)), 0.0, sum(at_once)
+    off = 2.0 ** -22 * a ** left                                       # X in two terms
+    for n in at_once:
+        err = e
+        for _ in range(n):
+            total += (b * err + e) / a
+            err = a * a * (err + 3 * e)
+        left -= n
+        off += e * a ** (left + n)
+    return total + off / 0.68
+
+
+def beyond_rounding(got, want):
+    """Norm of what `got` differs from `want` by beyond half a step of its type, relative to want's."""
+    bits = -math.log2(torch.finfo(got.dtype).eps)
+    got = f64(got)
+    top = np.floor(np.log2(np.maximum(np.maximum(np.abs(got), np.abs(want)), 1e-300)))
+    return np.linalg.norm(np.maximum(np.abs(got - want) - 2.0 ** (top - bits - 1), 0)) / np.linalg.norm(want)
+
+
+def dominated(shape, rest, seed):
+    """One direction, and noise whose norm is `rest` of its."""
+    rng = np.random.default_rng(seed)
+    u, v, x = rng.normal(size=(shape[0], 1)), rng.normal(size=(1, shape[1])), rng.normal(size=shape)
+    return torch.from_numpy(u @ v / (np.linalg.norm(u) * np.linalg.norm(v)) + rest * x / np.linalg.norm(x)).float().cuda()
+
+
+@pytest.mark.parametrize("rest", [0.1, 0.01, 1e-3])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("shapes", [[(300, 1000)], [(1500, 512)], [(700, 2100), (640, 640)]])
+def test_orthogonalize_one_dominant_direction(shapes, out, rest):
+    """What the steps amplify beside a dominant direction keeps its digits: bf16 updates are right to their rounding."""
+    mats = [dominated(s, rest, k) for k, s in enumerate(shapes)]
+    outs = [torch.empty_like(m, dtype=DT[out]) for m in mats]
+    dp.dp_orthogonalize(mats, outs)
+    for m, o in zip(mats, outs):
+        want = O.orthogonalize(f64(m), QUINTIC)
+        # no type takes more than three steps at once
+        assert beyond_rounding(o, want) < dominated_room(m.shape, (3, 2)), (m.shape, beyond_rounding(o, want))
+
+
 def test_orthogonalize_singular_values():
     m = tensor((200, 500), torch.float32, 7)
     o = torch.empty_like(m)
