@@ -259,13 +259,14 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
   if (kPair) ptx::cluster_sync_all();         // the partner's barriers exist before anyone arrives on them
   ptx::tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  uint32_t issued = 0;                        // a producer's stages so far
   follow_the_launch_before();
 
   if (warp == 0 || warp == kProducerQWarp) {
     // ------------------------------------------------------------- TMA producers
     // producers, issuer and relay: the whole warp runs the loop, an elected lane issues (see ptx::warp_ok)
     const bool right = warp != 0;
-    uint32_t stage = 0, phase = 0, issued = 0;
+    uint32_t stage = 0, phase = 0;
     int lay = 0;
     bool ok = true;
     for (int item = first_item; item < P.total_items && ok; item += item_stride) {
@@ -298,7 +299,6 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
     if (!ok && ptx::elect_one()) {
       *abort_flag = 1;
       if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
-      ptx::drain_issued_copies(full, kStages, issued);
     }
   } else if (warp == 1) {
     // --------------------------------------------------------------- MMA issuer
@@ -356,7 +356,6 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
       if (!ok && ptx::elect_one()) {
         *abort_flag = 1;
         if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
-        ptx::drain_issued_mmas(mma_done, kPair);
       }
     }
   } else if (warp == kRelayWarp) {
@@ -494,6 +493,8 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
 
   ptx::tc_fence_before();
   __syncthreads();
+  ptx::settle_after_abort(abort_flag, (warp == 0 || warp == kProducerQWarp) && lane == 0, full, kStages, issued,
+                          warp == 1 && rank == 0 && ptx::elect_one(), mma_done, kPair);
   if (kPair) ptx::cluster_sync_all();         // neither CTA leaves while the partner may still use its memory
   if (warp == 1) {
     ptx::tc_fence_after();

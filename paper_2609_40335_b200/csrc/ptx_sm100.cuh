@@ -149,7 +149,7 @@ __device__ __forceinline__ void tma_load_3d_a(uint32_t smem_dst, uint64_t tmap, 
       : "memory");
 }
 
-// After a producer gave up: wait (bounded, ~0.1 s per stage) until the copies it had already
+// After a role gave up: wait (bounded, ~0.1 s per stage) until the copies already
 // issued have landed, so that the CTA does not exit with TMA writes to its shared memory in
 // flight.  `issued` counts all stages armed so far on the ring of `n_stages` full-barriers.
 __device__ __forceinline__ void drain_issued_copies(uint64_t* full, int n_stages, uint32_t issued) {
@@ -491,7 +491,7 @@ __device__ __forceinline__ void mma_commit_pair_local(uint64_t* bar) {
                : "memory");
 }
 
-// After an MMA issuer gave up: wait (bounded, ~0.1 s) until the MMAs it had already issued have
+// After a role gave up: wait (bounded, ~0.1 s) until the MMAs that this thread had already issued have
 // retired, so that the CTA does not free tensor memory or exit under them.  `done` is a barrier
 // used for nothing else (count 1, fresh).
 __device__ __forceinline__ void drain_issued_mmas(uint64_t* done, bool pair) {
@@ -501,6 +501,19 @@ __device__ __forceinline__ void drain_issued_mmas(uint64_t* done, bool pair) {
   while (!mbar_try_wait(done, 0)) {
     if (clock64() - t0 > 150000000LL) break;
   }
+}
+
+// The end of a kernel of several roles, called by all threads behind a __syncthreads.  Where a wait ran out, whichever role's, others may
+// have left with copies or MMAs on their way: a producer that had issued all of its loads, an issuer whose last commit nobody waited for.
+// They end here, before the block does and its tensor memory is freed.  producer: this thread issued `issued` of the ring's stages; issuer: it issued the
+// MMAs (a commit is for those of its own thread).  Bounded, as the drains are.
+__device__ __forceinline__ void settle_after_abort(volatile int* abort_flag, bool producer, uint64_t* full, int n_stages, uint32_t issued,
+                                                   bool issuer, uint64_t* mma_done, bool pair) {
+  if (!*abort_flag) return;
+  if (producer) drain_issued_copies(full, n_stages, issued);
+  if (issuer) drain_issued_mmas(mma_done, pair);
+  __syncwarp();
+  __syncthreads();
 }
 
 // ---- descriptors -------------------------------------------------------------

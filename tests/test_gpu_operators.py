@@ -576,6 +576,28 @@ def test_orthogonalize_singular_values():
     assert s.min() > 0.6 and s.max() < 1.3
 
 
+@pytest.mark.parametrize("shapes", [[(100, 150)], [(128, 130)] * 3, [(70, 192), (260, 20)]])
+def test_orthogonalize_wait_limit_with_sums_no_longer_than_the_stages(shapes):
+    """Sums of three K steps at most: the copying warps have issued all before any other role's wait runs out."""
+    mats = [tensor(s, torch.float32, k) for k, s in enumerate(shapes)]
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    want, got = ([torch.empty_like(m) for m in mats] for _ in range(2))
+    dp.dp_orthogonalize(mats, want, dev_status=st)
+    assert int(st.item()) == 0
+    L = dp.load()
+    before = L.dp_debug_set_wait_limit(0)
+    try:
+        dp.dp_orthogonalize(mats, got, dev_status=st)
+        torch.cuda.synchronize()
+    finally:
+        L.dp_debug_set_wait_limit(before)
+    # a wait may still end at its one try, which the hardware may hold for a while: reported, or right
+    assert int(st.item()) == dp.DP_DEV_TIMEOUT or all(torch.equal(a, b) for a, b in zip(got, want))
+    st.zero_()
+    dp.dp_orthogonalize(mats, got, dev_status=st)
+    assert int(st.item()) == 0 and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_orthogonalize_wait_limit_leaves_the_context_usable():
     m = tensor((300, 300), torch.float32, 8)
     o, st = torch.empty_like(m), torch.zeros(1, dtype=torch.int32, device="cuda")
