@@ -83,10 +83,11 @@ cross_term_tc_kernel(const __grid_constant__ CrossParams P) {
   ptx::tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   const int per_ex = P.nt * P.ns;
+  uint32_t issued = 0;                        // the producer's stages so far
 
   if (warp == 0) {
     if (lane == 0) {
-      uint32_t stage = 0, phase = 0, issued = 0;
+      uint32_t stage = 0, phase = 0;
       bool ok = true;
       for (int item = blockIdx.x; item < P.total_items && ok; item += gridDim.x) {
         const int ex = item / per_ex, tp = item % per_ex, ti = tp / P.ns, tj = tp % P.ns;
@@ -103,7 +104,6 @@ cross_term_tc_kernel(const __grid_constant__ CrossParams P) {
       if (!ok) {
         *abort_flag = 1;
         if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
-        ptx::drain_issued_copies(full, kStages, issued);
       }
     }
   } else if (warp == 1) {
@@ -134,7 +134,6 @@ cross_term_tc_kernel(const __grid_constant__ CrossParams P) {
       if (!ok) {
         *abort_flag = 1;
         if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
-        ptx::drain_issued_mmas(mma_done, false);
       }
     }
   } else {
@@ -199,6 +198,7 @@ cross_term_tc_kernel(const __grid_constant__ CrossParams P) {
 
   ptx::tc_fence_before();
   __syncthreads();
+  ptx::settle_after_abort(abort_flag, warp == 0 && lane == 0, full, kStages, issued, warp == 1 && lane == 0, mma_done, false);
   if (warp == 1) {
     ptx::tc_fence_after();
     ptx::tmem_dealloc(tmem_base, kTmemCols);

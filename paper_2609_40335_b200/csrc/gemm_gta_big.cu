@@ -182,7 +182,7 @@ gemm_gta_big_kernel(const __grid_constant__ BigParams P) {
   uint64_t* empty = bars + 2 * kStages;       // MMAs retired
   uint64_t* acc_full = bars + 3 * kStages;    // [2]
   uint64_t* acc_empty = acc_full + 2;         // [2]
-  uint64_t* mma_done = acc_empty + 2;         // only used when the MMA issuer gives up
+  uint64_t* mma_done = acc_empty + 2;         // only used where a wait ran out
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(mma_done + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   uint32_t* sink = tmem_slot + 2;             // [kStages + 1] written by st.async, never read
@@ -212,13 +212,14 @@ gemm_gta_big_kernel(const __grid_constant__ BigParams P) {
   ptx::cluster_sync_all();                    // the partner's barriers exist before anyone arrives on them
   ptx::tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  uint32_t issued = 0;                        // a producer's stages so far
 
   if (warp == 0 || warp == kProducerXWarp || warp == kProducerY1Warp) {
     // ------------------------------------------------------------- TMA producers
     // the whole warp runs the loop, an elected lane issues (see ptx::warp_ok)
     const bool is_x = warp == kProducerXWarp;
     const int sub = warp == kProducerY1Warp ? 1 : 0;         // the Y part this warp loads
-    uint32_t stage = 0, phase = 0, issued = 0;
+    uint32_t stage = 0, phase = 0;
     int lay = 0;
     bool ok = true;
     for (int item = first_item; item < P.total_items && ok; item += item_stride) {
@@ -257,7 +258,6 @@ gemm_gta_big_kernel(const __grid_constant__ BigParams P) {
     if (!ok && ptx::elect_one()) {
       *abort_flag = 1;
       if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
-      ptx::drain_issued_copies(full, kStages, issued);   // copies in flight land before exit
     }
   } else if (warp == 1) {
     // --------------------------------------------------------------- MMA issuer
@@ -315,7 +315,6 @@ gemm_gta_big_kernel(const __grid_constant__ BigParams P) {
       if (!ok && ptx::elect_one()) {
         *abort_flag = 1;
         if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
-        ptx::drain_issued_mmas(mma_done, true);
       }
     }
   } else if (warp < kEpiWarp0) {
@@ -482,6 +481,8 @@ gemm_gta_big_kernel(const __grid_constant__ BigParams P) {
 
   ptx::tc_fence_before();
   __syncthreads();
+  ptx::settle_after_abort(abort_flag, (warp == 0 || warp == kProducerXWarp || warp == kProducerY1Warp) && lane == 0, full, kStages, issued,
+                          warp == 1 && rank == 0 && ptx::elect_one(), mma_done, true);
   ptx::cluster_sync_all();        // neither CTA leaves while the partner may still use its memory
   if (warp == 1) {
     ptx::tc_fence_after();

@@ -139,7 +139,7 @@ gemm_gta_kernel(const __grid_constant__ GtaParams P) {
   uint64_t* empty = bars + 2 * kStages;       // MMAs retired
   uint64_t* acc_full = bars + 3 * kStages;    // [2]
   uint64_t* acc_empty = acc_full + 2;         // [2]
-  uint64_t* mma_done = acc_empty + 2;         // only used when the MMA issuer gives up
+  uint64_t* mma_done = acc_empty + 2;         // only used where a wait ran out
   uint64_t* red_bar = mma_done + 1;           // [4] epilogue warps -> epilogue warp 0 (square-sum mode)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(red_bar + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -176,6 +176,7 @@ gemm_gta_kernel(const __grid_constant__ GtaParams P) {
   if (kPair) ptx::cluster_sync_all();     // the partner's barriers exist before anyone arrives on them
   ptx::tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  uint32_t issued = 0;                    // a producer's stages so far
 
   if (warp == 0 || warp == kProducerAWarp) {
     // ------------------------------------------------------------- TMA producers
@@ -189,7 +190,7 @@ gemm_gta_kernel(const __grid_constant__ GtaParams P) {
       constexpr int kBoxesA = Geo<kPair>::kAColsPerCta / 64;
       const uint32_t my_bytes = is_a ? uint32_t(Geo<kPair>::kABytes) : uint32_t(kGBytes);
       const int nbox = is_a ? kBoxesA : kBoxes;
-      uint32_t stage = 0, phase = 0, issued = 0;
+      uint32_t stage = 0, phase = 0;
       int lay = 0;
       bool ok = true;
       for (int item = first_item; item < P.total_items && ok; item += item_stride) {
@@ -215,7 +216,6 @@ gemm_gta_kernel(const __grid_constant__ GtaParams P) {
       if (!ok) {
         *abort_flag = 1;
         if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
-        ptx::drain_issued_copies(full, kStages, issued);   // copies in flight land before exit
       }
     }
   } else if (warp == 1) {
@@ -265,7 +265,6 @@ gemm_gta_kernel(const __grid_constant__ GtaParams P) {
       if (!ok) {
         *abort_flag = 1;
         if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
-        ptx::drain_issued_mmas(mma_done, kPair);
       }
     }
   } else if (warp < kEpiWarp0) {
@@ -471,6 +470,8 @@ gemm_gta_kernel(const __grid_constant__ GtaParams P) {
 
   ptx::tc_fence_before();
   __syncthreads();
+  ptx::settle_after_abort(abort_flag, (warp == 0 || warp == kProducerAWarp) && lane == 0, full, kStages, issued,
+                          warp == 1 && rank == 0 && lane == 0, mma_done, kPair);
   // pair: neither CTA may leave while the partner can still read its shared memory or arrive on
   // its barriers (every wait above is bounded, so both always get here)
   if (kPair) ptx::cluster_sync_all();

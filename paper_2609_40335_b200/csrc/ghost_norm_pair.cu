@@ -154,12 +154,13 @@ ghost_norm_pair_kernel(const __grid_constant__ PairParams P) {
   ptx::cluster_sync_all();        // the partner's barriers exist before anyone arrives on them
   ptx::tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  uint32_t issued = 0;            // the producer's stages so far
   const uint32_t tiles_a = ptx::smem_u32(tiles), full_a = ptx::smem_u32(full), empty_a = ptx::smem_u32(empty);
 
   if (warp == 0) {
     // ------------------------------------------------------------- TMA producer
     // producer, issuer and relay: the whole warp runs the loop, an elected lane issues (see ptx::warp_ok)
-    uint32_t stage = 0, phase = 0, issued = 0;
+    uint32_t stage = 0, phase = 0;
     int lay = 0;
     bool ok = true;
     for (int item = first_item; item < P.total_items && ok; item += item_stride) {
@@ -190,7 +191,6 @@ ghost_norm_pair_kernel(const __grid_constant__ PairParams P) {
     if (!ok && ptx::elect_one()) {
       *abort_flag = 1;
       if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
-      ptx::drain_issued_copies(full, kStages, issued);
     }
   } else if (warp == 1) {
     // --------------------------------------------------------------- MMA issuer
@@ -242,7 +242,6 @@ ghost_norm_pair_kernel(const __grid_constant__ PairParams P) {
       if (!ok && ptx::elect_one()) {
         *abort_flag = 1;
         if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
-        ptx::drain_issued_mmas(mma_done, true);
       }
     }
   } else if (warp == 2) {
@@ -342,6 +341,7 @@ ghost_norm_pair_kernel(const __grid_constant__ PairParams P) {
 
   ptx::tc_fence_before();
   __syncthreads();
+  ptx::settle_after_abort(abort_flag, warp == 0 && lane == 0, full, kStages, issued, warp == 1 && rank == 0 && ptx::elect_one(), mma_done, true);
   ptx::cluster_sync_all();        // neither CTA leaves while the partner may still use its memory
   if (warp == 1) {
     ptx::tc_fence_after();

@@ -93,7 +93,7 @@ ghost_norm_split_kernel(const __grid_constant__ SplitGramParams P) {
   uint64_t* in_empty = in_full + kStagesIn;        // [kStagesIn] converters -> TMA
   uint64_t* acc_full = in_empty + kStagesIn;       //             MMA -> epilogue
   uint64_t* acc_empty = acc_full + 1;              //             epilogue -> MMA
-  uint64_t* mma_done = acc_empty + 1;              // only used when the MMA issuer gives up
+  uint64_t* mma_done = acc_empty + 1;              // only used where a wait ran out
   uint64_t* red_bar = mma_done + 1;                // [4]         epilogue warps -> epilogue warp 0
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(red_bar + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -115,6 +115,7 @@ ghost_norm_split_kernel(const __grid_constant__ SplitGramParams P) {
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  uint32_t issued = 0;                             // the producer's stages so far
   const uint32_t tiles_a = ptx::smem_u32(tiles), in_a = ptx::smem_u32(in);
   const uint32_t full_a = ptx::smem_u32(full), empty_a = ptx::smem_u32(empty);
   const uint32_t in_full_a = ptx::smem_u32(in_full), in_empty_a = ptx::smem_u32(in_empty);
@@ -122,7 +123,7 @@ ghost_norm_split_kernel(const __grid_constant__ SplitGramParams P) {
   if (warp == 0) {
     // ------------------------------------------------------------- TMA producer
     // producer and issuer: the whole warp runs the loop, an elected lane issues (see ptx::warp_ok)
-    uint32_t stage = 0, phase = 0, issued = 0;
+    uint32_t stage = 0, phase = 0;
     int lay = 0;
     bool ok = true;
     const uint32_t bytes = uint32_t(P.rows) * 256u;
@@ -150,7 +151,6 @@ ghost_norm_split_kernel(const __grid_constant__ SplitGramParams P) {
     if (!ok && ptx::elect_one()) {
       *abort_flag = 1;
       if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
-      ptx::drain_issued_copies(in_full, kStagesIn, issued);
     }
   } else if (warp == 1) {
     // --------------------------------------------------------------- MMA issuer
@@ -193,7 +193,6 @@ ghost_norm_split_kernel(const __grid_constant__ SplitGramParams P) {
     if (!ok && ptx::elect_one()) {
       *abort_flag = 1;
       if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
-      ptx::drain_issued_mmas(mma_done, false);
     }
   } else if (warp >= kConvWarp0) {
     // --------------------------------------------------------------- converters
@@ -327,6 +326,7 @@ ghost_norm_split_kernel(const __grid_constant__ SplitGramParams P) {
 
   ptx::tc_fence_before();
   __syncthreads();
+  ptx::settle_after_abort(abort_flag, warp == 0 && lane == 0, in_full, kStagesIn, issued, warp == 1 && ptx::elect_one(), mma_done, false);
   if (warp == 1) {
     ptx::tc_fence_after();
     ptx::tmem_dealloc(tmem_base, kTmemCols);

@@ -133,7 +133,7 @@ ghost_norm_tc_kernel(const __grid_constant__ GhostParams P) {
   uint64_t* empty = bars + kMaxStages;     // [n_stages] MMA -> TMA
   uint64_t* acc_full = bars + 2 * kMaxStages; // [2]     MMA -> epilogue
   uint64_t* acc_empty = acc_full + 2;      // [2]        epilogue -> MMA
-  uint64_t* mma_done = acc_empty + 2;      // only used when the MMA issuer gives up
+  uint64_t* mma_done = acc_empty + 2;      // only used where a wait ran out
   uint64_t* red_bar = mma_done + 1;        // [4]        epilogue warps -> epilogue warp 0
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(red_bar + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -158,12 +158,13 @@ ghost_norm_tc_kernel(const __grid_constant__ GhostParams P) {
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  uint32_t issued = 0;                             // the producer's stages so far
   const uint32_t tiles_a = ptx::smem_u32(tiles), full_a = ptx::smem_u32(full), empty_a = ptx::smem_u32(empty);
 
   if (warp == 0) {
     // ------------------------------------------------------------- TMA producer
     // producer and issuer: the whole warp runs the loop, an elected lane issues (see ptx::warp_ok)
-    uint32_t stage = 0, phase = 0, issued = 0;
+    uint32_t stage = 0, phase = 0;
     int lay = 0;
     bool ok = true;
     for (int item = blockIdx.x; item < P.total_items && ok; item += gridDim.x) {
@@ -204,7 +205,6 @@ ghost_norm_tc_kernel(const __grid_constant__ GhostParams P) {
     if (!ok && ptx::elect_one()) {
       *abort_flag = 1;
       if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
-      ptx::drain_issued_copies(full, n_stages, issued);   // copies in flight land before exit
     }
   } else if (warp == 1) {
     // --------------------------------------------------------------- MMA issuer
@@ -259,7 +259,6 @@ ghost_norm_tc_kernel(const __grid_constant__ GhostParams P) {
     if (!ok && ptx::elect_one()) {
       *abort_flag = 1;
       if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
-      ptx::drain_issued_mmas(mma_done, false);
     }
   } else {
     // ----------------------------------------------------------------- epilogue
@@ -372,6 +371,7 @@ ghost_norm_tc_kernel(const __grid_constant__ GhostParams P) {
 
   ptx::tc_fence_before();
   __syncthreads();
+  ptx::settle_after_abort(abort_flag, warp == 0 && lane == 0, full, n_stages, issued, warp == 1 && ptx::elect_one(), mma_done, false);
   if (warp == 1) {
     ptx::tc_fence_after();
     ptx::tmem_dealloc(tmem_base, kTmemCols);

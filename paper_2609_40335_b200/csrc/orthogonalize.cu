@@ -226,7 +226,7 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
   uint64_t* empty = bars + 2 * kStages;       // MMAs retired
   uint64_t* acc_full = bars + 3 * kStages;    // [2]
   uint64_t* acc_empty = acc_full + 2;         // [2]
-  uint64_t* mma_done = acc_empty + 2;         // only used when the MMA issuer gives up
+  uint64_t* mma_done = acc_empty + 2;         // only used where a wait ran out
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(mma_done + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   uint32_t* sink = tmem_slot + 2;             // [kStages] written by st.async, never read
