@@ -312,6 +312,9 @@ gemm_gta_big_kernel(const __grid_constant__ BigParams P) {
         }
         slots.advance(it.nsub);
       }
+      // what rank 1's epilogue tells this CTA's barriers last has to arrive before the CTA ends
+      for (uint32_t b = 0; b < 2 && ok; ++b)
+        if (slots.uses(b)) ok = ptx::warp_ok(ptx::mbar_wait_cluster(&acc_empty[b], (slots.uses(b) - 1) & 1, abort_flag, P.wait_limit));
       if (!ok && ptx::elect_one()) {
         *abort_flag = 1;
         if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);

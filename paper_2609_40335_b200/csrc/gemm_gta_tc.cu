@@ -262,6 +262,10 @@ gemm_gta_kernel(const __grid_constant__ GtaParams P) {
           else ptx::mma_commit(&acc_full[buf]);
         }
       }
+      // what rank 1's epilogue tells this CTA's barriers last has to arrive before the CTA ends
+      if (kPair && ok)
+        for (uint32_t n = n_item > 2 ? n_item - 2 : 0; n < n_item && ok; ++n)
+          ok = ptx::mbar_wait_cluster(&acc_empty[n & 1], (n >> 1) & 1, abort_flag, P.wait_limit);
       if (!ok) {
         *abort_flag = 1;
         if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);

@@ -353,6 +353,10 @@ ns_product_kernel(const __grid_constant__ NsParams P) {
           if (++stage == kStages) { stage = 0; phase ^= 1; }
         }
       }
+      // what rank 1's epilogue tells this CTA's barriers last has to arrive before the CTA ends
+      if (kPair)
+        for (uint32_t n = n_acc > 2 ? n_acc - 2 : 0; n < n_acc && ok; ++n)
+          ok = ptx::warp_ok(ptx::mbar_wait_cluster(&acc_empty[n & 1], (n >> 1) & 1, abort_flag, P.wait_limit));
       if (!ok && ptx::elect_one()) {
         *abort_flag = 1;
         if (P.dev_status) atomicOr(P.dev_status, DP_DEV_TIMEOUT);
