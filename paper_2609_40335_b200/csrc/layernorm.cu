@@ -25,6 +25,7 @@
 #include <cmath>
 #include <map>
 #include <mutex>
+#include <utility>
 
 #include "dp_common.cuh"
 #include "ptx_sm100.cuh"
@@ -597,6 +598,7 @@ __global__ void __launch_bounds__(kLnSumThreads)
 ln_sums_kernel(const float* partials, int parts, int p, float* gain_sums, float* shift_sums, float* sq) {
   __shared__ float red[32], squares[8];
   cg::cluster_group cluster = cg::this_cluster();
+  auto begun = cluster.barrier_arrive();               // rank 0's memory is written only once its CTA runs
   const int ctas = cluster.num_blocks(), rank = cluster.block_rank(), example = blockIdx.x / ctas;
   cudaGridDependencySynchronize();
   float square = 0.f;
@@ -613,6 +615,7 @@ ln_sums_kernel(const float* partials, int parts, int p, float* gain_sums, float*
     square = fmaf(a, a, fmaf(b, b, square));
   }
   square = block_sum(square, red);
+  cluster.barrier_wait(std::move(begun));
   if (threadIdx.x == 0) *cluster.map_shared_rank(squares + rank, 0) = square;
   cluster.sync();
   if (sq && rank == 0 && threadIdx.x == 0) {

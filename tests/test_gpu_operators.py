@@ -161,6 +161,23 @@ def test_layernorm_backward(B, T, p, dtype, params, pad, offset):
     surroundings_untouched(dx, p + pad, offset)
 
 
+@pytest.mark.parametrize("B,T,p", [(16, 640, 776), (1, 4100, 1001), (16, 640, 2048), (1, 4100, 100)])
+def test_layernorm_backward_sums_through_the_workspace_repeat_bit_for_bit(B, T, p):
+    """Launches behind one another, clusters that begin while the launch before still runs."""
+    assert dp.dp_layernorm_backward_ws_bytes(B, T, p) > 0
+    x, g = tensor((B, T, p), torch.bfloat16, 1), tensor((B, T, p), torch.bfloat16, 2, 1e-2)
+    mean, rstd = torch.zeros(B, T, device="cuda"), torch.ones(B, T, device="cuda")
+    ws = torch.empty(dp.dp_layernorm_backward_ws_bytes(B, T, p), dtype=torch.uint8, device="cuda")
+    outs = [(torch.zeros(B, p, device="cuda"), torch.zeros(B, p, device="cuda"), torch.zeros(B, device="cuda")) for _ in range(40)]
+    for gs, ss, sq in outs:
+        dp.dp_layernorm_backward(g, x, None, mean, rstd, gain_sums=gs, shift_sums=ss, sq=sq, ws=ws)
+    for o in outs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(o, outs[0]))
+    gs, ss, sq = (f64(t) for t in outs[0])
+    # p squares of either sum, a thread's at most 16 one after the other, then a tree over 128 threads and 8 CTAs
+    assert np.abs(sq / ((gs ** 2).sum(-1) + (ss ** 2).sum(-1)) - 1).max() < (32 + 7 + 8 + 3) * U
+
+
 def test_layernorm_backward_parts_of_the_outputs():
     B, T, p = 3, 37, 264
     x, g = tensor((B, T, p), torch.bfloat16, 1), tensor((B, T, p), torch.bfloat16, 2, 1e-2)
