@@ -457,6 +457,9 @@ dp_status dp_debug_noise_error_scan(float t_max, double* out4, void* stream);
 int32_t dp_debug_bounds_checked(void);
 dp_status dp_debug_bounds_probe(int64_t idx, int64_t n, int32_t* dev_status, void* stream);
 int64_t dp_debug_tensor_map_encodes(void);
+/* How dp_orthogonalize would run these matrices (p and d are looked at): 0, a CTA per matrix; else twice the number of steps that
+ * the first launches take at once, plus 1 for CTA pairs (of the first group of launches, where there are several); -1, not at all. */
+int32_t dp_debug_orthogonalize_form(const dp_matrix_desc* mats, int32_t n, dp_dtype out_dt, const float* coefs, int32_t steps);
 /* Test knob for the failure path: device-side barrier waits give up after `cycles` (0: at the
  * first miss; negative: back to the default of about a second).  A kernel whose wait gives up
  * ORs DP_DEV_TIMEOUT into dev_status, lets its copies and MMAs in flight finish, frees its

@@ -64,7 +64,8 @@ EXPORTS = ["dp_vector_norms", "dp_vector_norms_ws_bytes", "dp_clip_accumulate_ve
            "dp_debug_tensor_map_encodes", "dp_debug_set_wait_limit",
            "dp_debug_ghost_single", "dp_set_reserved_sms", "dp_step_enqueue", "dp_step_ws_bytes",
            "dp_step_vectors_ws_bytes", "dp_layernorm", "dp_layernorm_backward", "dp_layernorm_backward_ws_bytes",
-           "dp_preference_loss", "dp_preference_loss_ws_bytes", "dp_orthogonalize", "dp_orthogonalize_ws_bytes"]
+           "dp_preference_loss", "dp_preference_loss_ws_bytes", "dp_orthogonalize", "dp_orthogonalize_ws_bytes",
+           "dp_debug_orthogonalize_form"]
 
 
 def lib_path() -> str:
@@ -146,6 +147,8 @@ def load():
     L.dp_orthogonalize.argtypes = [C.POINTER(_MatrixDesc), i32, i32, i32, C.POINTER(f32), i32, f32, vp, sz, vp, vp]
     L.dp_orthogonalize_ws_bytes.argtypes = [C.POINTER(_MatrixDesc), i32]
     L.dp_orthogonalize_ws_bytes.restype = sz
+    L.dp_debug_orthogonalize_form.argtypes = [C.POINTER(_MatrixDesc), i32, i32, C.POINTER(f32), i32]
+    L.dp_debug_orthogonalize_form.restype = i32
     L.dp_rdp_epsilon.argtypes = [C.c_double, C.c_double, i64, C.c_double, vp, vp]
     L.dp_sigma_for_epsilon.argtypes = [C.c_double, i64, C.c_double, C.c_double, C.c_double, vp]
     L.dp_status_string.argtypes = [i32]

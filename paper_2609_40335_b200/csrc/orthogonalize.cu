@@ -1184,6 +1184,23 @@ size_t dp_orthogonalize_ws_bytes(const dp_matrix_desc* mats, int32_t n) try {
   return 0;
 }
 
+int32_t dp_debug_orthogonalize_form(const dp_matrix_desc* mats, int32_t n, dp_dtype out_dt, const float* coefs, int32_t steps) try {
+  if (!mats || n <= 0 || !coefs || steps <= 0) return -1;
+  for (int k = 0; k < n; ++k)
+    if (check_matrix(mats[k], false) != DP_OK) return -1;
+  std::vector<NsStep> plan;
+  if (!plan_steps(coefs, steps, plan)) return -1;
+  if (ns_small(mats, n, steps)) return 0;
+  const std::vector<int> order = ns_order(mats, n);
+  const int groups = ns_groups(n);
+  std::vector<NsShape> shapes;
+  for (int k = 0; k < n; k += groups) shapes.push_back(NsShape(mats[order[k]]));
+  const NsForm form = choose_form(shapes, plan, out_dt == DP_BF16);
+  return 2 * fused_steps(plan, 0, form.growth) + (form.pair ? 1 : 0);
+} catch (...) {
+  return -1;
+}
+
 dp_status dp_orthogonalize(const dp_matrix_desc* mats, int32_t n, dp_dtype dt, dp_dtype out_dt, const float* coefs, int32_t steps,
                            float eps, void* ws, size_t ws_bytes, int32_t* dev_status, void* stream) try {
   if (!mats || n <= 0 || !coefs || steps <= 0 || !std::isfinite(eps) || eps < 0.f) return DP_ERR_INVALID_ARG;

@@ -9,6 +9,7 @@ Tolerances, with u = 2^-24 (an fp32 rounding) and half(t) = torch.finfo(t).eps /
   and the polynomial's slope, at most 1.8 in the two or three steps in which singular values are near one (before them error
   and value grow alike), give 5 * 3 * 1.8^3 d < 90 d.
 """
+import ctypes
 import math
 
 import numpy as np
@@ -583,6 +584,136 @@ def test_orthogonalize_one_dominant_direction(shapes, out, rest):
         want = O.orthogonalize(f64(m), QUINTIC)
         # no type takes more than three steps at once
         assert beyond_rounding(o, want) < dominated_room(m.shape, (3, 2)), (m.shape, beyond_rounding(o, want))
+
+
+# Sets of matrices and how they run in fp32 and in bf16 out: (CTA pairs, steps at once).  test_host_operators.py checks the same on the host.
+NS_FORMS = {
+    "single": ([(200, 330), (330, 200)], (False, 1), (False, 1)),
+    "single, bf16 three at once": ([(300, 1000)] * 3 + [(1000, 301)] * 2, (False, 1), (False, 3)),
+    "single, two and three at once": ([(700, 2100), (640, 640)], (False, 2), (False, 3)),
+    "pairs": ([(1001, 500)] * 10 + [(505, 2000)] * 12, (True, 1), (True, 3)),
+    "pairs, two and three at once": ([(650, 2100)] * 6 + [(2100, 651)] * 4 + [(700, 700)] * 2, (True, 2), (True, 3)),
+    "pairs, one size": ([(700, 1301)] * 8, (True, 2), (True, 3)),
+}
+
+
+def ns_form(mats, out, coefs=QUINTIC):
+    """(CTA pairs, steps at once) of a call; None: a CTA per matrix."""
+    flat = [c for step in coefs for c in step]
+    arr = (dp._MatrixDesc * len(mats))()
+    for D, m in zip(arr, mats):
+        D.p, D.d = m
+    f = dp.load().dp_debug_orthogonalize_form(arr, len(mats), {torch.float32: dp.DP_F32, torch.bfloat16: dp.DP_BF16}[out],
+                                              (ctypes.c_float * len(flat))(*flat), len(coefs))
+    assert f >= 0
+    return (bool(f & 1), f >> 1) if f else None
+
+
+def plain_products(m, coefs=QUINTIC):
+    """The iterate with products in fp32."""
+    x = m.float()
+    tall = x.shape[0] > x.shape[1]
+    x = x.T if tall else x
+    x = x / x.double().square().sum().sqrt().float()
+    for a, b, c in coefs:
+        A = x @ x.T
+        x = a * x + (b * A + c * (A @ A)) @ x
+    return x.T if tall else x
+
+
+@pytest.mark.parametrize("name", NS_FORMS)
+@pytest.mark.parametrize("dtype,out,pad", [("f32", "f32", 0), ("f32", "bf16", 0), ("bf16", "f32", 3), ("bf16", "bf16", 1)])
+def test_orthogonalize_in_every_form(name, dtype, out, pad):
+    """Single CTAs and pairs, steps one by one and several at once: as near to the definition as products in fp32 are.
+
+    Operands of 22 bits, where fp32 has 24, are off by 2^-22, and planes are rounded so twice a step and matrix; fp32 products round
+    K times a product by 2^-24.  With K of 300 at least, errors that add up as independent ones do, that is 2^-22 sqrt(2) against 2^-24 sqrt(300):
+    a third.  Two steps at once bring A's error times |B|^2 = 11.8 beside singular values that are left small; with the products' slope near one
+    (1.8, twice) that is 3.3 times the error of steps one by one.  2.5 holds both; three at once are for bf16, whose rounding is taken out."""
+    shapes, *forms = NS_FORMS[name]
+    assert ns_form(shapes, DT[out]) == forms[out == "bf16"]
+    mats = [tensor(s, DT[dtype], 30 + k, 0.7, pitch=s[1] + pad, offset=pad) for k, s in enumerate(shapes)]
+    outs = [tensor(s, DT[out], 1, pitch=s[1] + pad, offset=pad) for s in shapes]
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    dp.dp_orthogonalize(mats, outs, dev_status=st)
+    assert int(st.item()) == 0
+    for k in {0, 1, len(shapes) // 2, len(shapes) - 1}:
+        want = O.orthogonalize(f64(mats[k]), QUINTIC)
+        assert beyond_rounding(outs[k], want) < 2.5 * rel_norm(plain_products(mats[k]), want), shapes[k]
+        surroundings_untouched(outs[k], shapes[k][1] + pad, pad)
+    again = [torch.empty_like(o) for o in outs]
+    dp.dp_orthogonalize(mats, again)
+    assert all(torch.equal(a, b) for a, b in zip(outs, again))
+
+
+@pytest.mark.parametrize("name", ["single, bf16 three at once", "single, two and three at once", "pairs, one size"])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("coefs", [((1.5, -0.5, 0.0),) * 8, ((1.875, -1.25, 0.375),) * 6, ((1.9, -1.0, 0.02),) * 3,
+                                   ((1.9, -1.0, 0.02), QUINTIC[0], (1.5, -0.5, 0.0), (1.875, -1.25, 0.375), (1.5, 0.0, -0.4)),
+                                   (QUINTIC[0], (1.5, 0.0, -0.4), (2.0, 0.0, 0.0), (0.4, 0.1, 0.1))])
+def test_orthogonalize_other_polynomials_in_steps_at_once(name, out, coefs):
+    """Polynomials with and without a diagonal's copy, in each other's company."""
+    shapes = NS_FORMS[name][0]
+    mats = [tensor(s, torch.float32, 60 + k) for k, s in enumerate(shapes)]
+    outs = [torch.empty(s, device="cuda", dtype=DT[out]) for s in shapes]
+    dp.dp_orthogonalize(mats, outs, coefs=coefs)
+    for k in (0, len(shapes) - 1):
+        want = O.orthogonalize(f64(mats[k]), coefs)
+        assert beyond_rounding(outs[k], want) < 2 * ns_room([shapes[k]], torch.float32)
+
+
+EXTREME = {"a CTA": [(48, 80)], "single": [(200, 330)], "single, tall": [(330, 200)], "at once": [(300, 1000)], "at once, in fp32 too": [(700, 1301)]}
+
+
+@pytest.mark.parametrize("where", EXTREME)
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("eps", [0.0, 1e-37])
+def test_orthogonalize_extreme_inputs_in_every_form(where, out, eps):
+    """Zeros, tiny and huge values (whose squares fp32 does not hold), low rank, an infinity, NaN; in place."""
+    shape = EXTREME[where][0]
+    base = tensor(shape, torch.float32, 6)
+    m = [torch.zeros_like(base), base * 1e-30, base * 1e30, base[:, :1] @ base[:1], base[:, :3] @ base[:3], base.clone(), base.clone(), base]
+    m[5][3, 4], m[6][7, 1] = float("inf"), float("nan")
+    outs = [torch.full_like(v, 9.0, dtype=DT[out]) for v in m]
+    dp.dp_orthogonalize(m, outs, eps=eps)
+    assert torch.isnan(outs[0]).all() if eps == 0 else not outs[0].any()           # 0 / 0, 0 / eps
+    assert torch.isnan(outs[5]).any() and torch.isnan(outs[6]).any()
+    for k in (1, 2, 3, 4, 7):
+        want = O.orthogonalize(f64(m[k]), QUINTIC, eps)
+        assert beyond_rounding(outs[k], want) < dominated_room(shape, (3, 2)), k
+    # the finite ones do not know of the others
+    some = [torch.empty_like(outs[0]) for _ in m]
+    fresh = [v if k in (1, 2, 3, 4, 7) else base for k, v in enumerate(m)]
+    dp.dp_orthogonalize(fresh, some, eps=eps)
+    assert all(torch.equal(some[k], outs[k]) for k in (1, 2, 3, 4, 7)) and torch.equal(some[0], some[7])
+    if out == "f32":
+        z = [v.clone() for v in fresh]
+        dp.dp_orthogonalize(z, z, eps=eps)
+        assert all(torch.equal(a, b) for a, b in zip(z, some))
+
+
+@pytest.mark.parametrize("name", ["pairs", "pairs, one size"])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_orthogonalize_wait_limit_on_pairs(name, out):
+    shapes = NS_FORMS[name][0]
+    assert ns_form(shapes, DT[out])[0]
+    mats = [tensor(s, torch.float32, k) for k, s in enumerate(shapes)]
+    want, got = ([torch.empty_like(m, dtype=DT[out]) for m in mats] for _ in range(2))
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    dp.dp_orthogonalize(mats, want, dev_status=st)
+    assert int(st.item()) == 0
+    L = dp.load()
+    before = L.dp_debug_set_wait_limit(0)
+    try:
+        dp.dp_orthogonalize(mats, got, dev_status=st)
+        torch.cuda.synchronize()
+    finally:
+        L.dp_debug_set_wait_limit(before)
+    # a wait may still end at its one try, which the hardware may hold for a while: reported, or right
+    assert int(st.item()) == dp.DP_DEV_TIMEOUT or all(torch.equal(a, b) for a, b in zip(got, want))
+    st.zero_()
+    dp.dp_orthogonalize(mats, got, dev_status=st)
+    assert int(st.item()) == 0 and all(torch.equal(a, b) for a, b in zip(got, want))
 
 
 def test_orthogonalize_singular_values():

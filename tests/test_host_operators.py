@@ -122,6 +122,24 @@ def test_orthogonalize_workspace(lib):
     assert lib.dp_orthogonalize_ws_bytes(arr, 2) == 0
 
 
+def test_orthogonalize_forms(lib):
+    """The sets of matrices that the GPU tests take for their form have it on a B200's 148 SMs."""
+    import test_gpu_operators as T
+    for name, (shapes, *forms) in T.NS_FORMS.items():
+        for out, want in zip((torch.float32, torch.bfloat16), forms):
+            assert T.ns_form(shapes, out) == want, (name, out)
+    assert T.ns_form([(64, 256), (256, 3)], torch.float32) is None
+    assert T.ns_form([(65, 256)], torch.float32) == (False, 1)
+    # the linears of a GPT-2 block
+    block = lambda d: [(3 * d, d), (d, d), (4 * d, d), (d, 4 * d)]
+    assert T.ns_form(block(768) * 6, torch.float32) == (True, 2) and T.ns_form(block(1024) * 24, torch.bfloat16) == (True, 3)
+    bad = (binding._MatrixDesc * 1)()
+    f = lib.dp_debug_orthogonalize_form
+    assert f(bad, 1, 0, (C.c_float * 3)(1.5, -0.5, 0.0), 1) == -1 and f(None, 1, 0, (C.c_float * 3)(), 1) == -1
+    bad[0].p = bad[0].d = 8
+    assert f(bad, 1, 0, (C.c_float * 3)(NAN, 0, 0), 1) == -1 and f(bad, 1, 0, (C.c_float * 3)(1.5, -0.5, 0.0), 0) == -1
+
+
 def test_cpu_tensors_and_wrong_shapes_are_refused_by_the_binding():
     x = torch.zeros(2, 3, 8)
     with pytest.raises(binding.DpGhostError):
