@@ -358,7 +358,7 @@ dp_status dp_layernorm(const void* X, int64_t ldx, dp_dtype dt, int64_t rows, in
  *   gain_sums[i,:] = sum_t G[i,t,:]*h[i,t,:],  shift_sums[i,:] = sum_t G[i,t,:]                  [dev, (B, p) floats each, or NULL]
  *   sq[i] += ||gain_sums[i]||^2 + ||shift_sums[i]||^2   (both parameters' blocks of Eq. 6)         [dev, B floats, or NULL]
  * The sums are the v_i of dp_clip_accumulate_vectors, so their clipped sum is that call on them with T = 1 (DP_F32): G and X are
- * read once for dX, norms and sums.  dX may be G or X itself (same pitch).  Workspace: dp_layernorm_backward_ws_bytes (0
+ * read once for dX, norms and sums.  dX may be G or X itself (same pitch).  T <= 2^30.  Workspace: dp_layernorm_backward_ws_bytes (0
  * unless a few dozen examples or less have long sequences).  dev_status [dev, or NULL]: DP_DEV_TIMEOUT if a wait inside ran out. */
 dp_status dp_layernorm_backward(const void* G, int64_t ldg, const void* X, int64_t ldx, dp_dtype dt, int32_t B, int32_t T, int32_t p,
                                 const void* gain, dp_dtype param_dt, const float* mean, const float* rstd, void* dX, int64_t lddx,

@@ -39,6 +39,7 @@ namespace cg = cooperative_groups;
 constexpr int kLnMaxCols = 16384;          // 16 warps x 32 lanes x 32 columns
 constexpr int kLnMaxBuffers = 8;           // tiles in flight
 constexpr int kLnMaxParts = 16;            // CTAs of a cluster
+constexpr int kLnMaxTokens = 1 << 30;      // rows of an example: the backward pass counts them, a tile or two ahead, in 32 bits
 
 // Two columns.  (As fma.rn.f32x2 and the like these took longer: 66 us instead of 59 for the backward pass above.)
 struct F2 { float x, y; };
@@ -721,7 +722,7 @@ LnParts ln_parts(int B, int T, int blocks) {
   LnParts best{1, true};
   long long least = 0;
   for (int c = 1; c <= std::min(kLnMaxParts, ceil_div(T, 16)); c *= 2) {
-    const long long waves = ceil_div(B, blocks * at_once[c]), cost = waves * (ceil_div(T, c) + 128);
+    const long long n = blocks * at_once[c], waves = (B + n - 1) / n, cost = waves * (ceil_div(T, c) + 128);
     if (c == 1 || cost < least) { least = cost; best = {c, true}; }
   }
   const int through = std::min(std::min(blocks * sms / B, ceil_div(T, 16)), int(std::sqrt(double(T))));
@@ -846,7 +847,7 @@ dp_status dp_layernorm(const void* X, int64_t ldx, dp_dtype dt, int64_t rows, in
 }
 
 size_t dp_layernorm_backward_ws_bytes(int32_t B, int32_t T, int32_t p) try {
-  if (B <= 0 || T <= 0 || p <= 0 || p > kLnMaxCols) return 0;
+  if (B <= 0 || T <= 0 || p <= 0 || p > kLnMaxCols || T > kLnMaxTokens) return 0;
   size_t most = 0;                                    // of either type of G and X
   for (const int es : {2, 4}) {
     const LnParts parts = ln_parts_of(B, T, p, es);
@@ -868,7 +869,7 @@ dp_status dp_layernorm_backward(const void* G, int64_t ldg, const void* X, int64
   if ((dX == G && lddx != ldg) || (dX == X && lddx != ldx)) return DP_ERR_INVALID_ARG;
   const int es = dt == DP_F32 ? 4 : 2, ps = param_dt == DP_F32 ? 4 : 2;
   if (!on_boundary(es, G, X, dX) || !on_boundary(ps, gain) || !on_boundary(4, mean, rstd, gain_sums, shift_sums, sq)) return DP_ERR_ALIGNMENT;
-  if (p > kLnMaxCols) return DP_ERR_UNSUPPORTED;
+  if (p > kLnMaxCols || T > kLnMaxTokens) return DP_ERR_UNSUPPORTED;
   const LnParts parts = ln_parts_of(B, T, p, es);
   if ((long long)B * parts.parts > 0x7fffffffLL) return DP_ERR_UNSUPPORTED;
   float* partials = nullptr;

@@ -67,6 +67,16 @@ def test_layernorm_backward_needs_a_workspace_for_few_long_examples_only(lib):
     assert f(1, 100000, 768) > 32 * 2 * 768 * 4 and f(0, 5, 5) == 0 and f(1, 100000, 16385) == 0
 
 
+@pytest.mark.parametrize("T,want", [(1 << 30, WORKSPACE), ((1 << 30) + 1, UNSUPPORTED), ((1 << 31) - 1, UNSUPPORTED)])
+def test_layernorm_backward_of_more_tokens_than_it_counts(lib, T, want):
+    """Rows are counted in 32 bits, a tile or two ahead: past that no row would be read, or rows before the first."""
+    kw = dict(B=1, T=T, p=1, ldg=1, ldx=1, lddx=1)
+    assert backward(lib, **kw) == want
+    assert (lib.dp_layernorm_backward_ws_bytes(1, T, 1) > 0) == (want == WORKSPACE)
+    if want != UNSUPPORTED:
+        assert backward(lib, **dict(kw, ws=A[0], n=1 << 30)) == CUDA
+
+
 def preference(lib, **kw):
     a = dict(x=A[0], ldl=104, dt=1, B=3, T=20, V=100, targets=A[1], ref=A[2], beta=0.1, smoothing=0.0, scale=1.0, loss=A[3], logp=A[4],
              G=A[5], ldg=104, ws=A[6], n=1 << 20, status=A[7])
