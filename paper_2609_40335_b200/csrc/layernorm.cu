@@ -764,6 +764,7 @@ dp_status ln_fwd_launch(LnForward& P, cudaStream_t st) {
   const dp_status r = ln_smem_setup(kernel);
   if (r != DP_OK) return r;
   const long long blocks = std::min((P.rows + P.S.groups - 1) / P.S.groups, (long long)kBlock.blocks * sm_count());
+  if (P.rows / blocks / P.S.groups >= 0x7fffffffLL - 1) return DP_ERR_UNSUPPORTED;       // a block counts its tiles in 32 bits
   kernel<<<unsigned(blocks), (warps + (kAligned ? 1 : 0)) * 32, LnSmem(P.S, P.p, 1, false, warps).bytes, st>>>(P);
   DP_LAUNCH_OK();
   return DP_OK;

@@ -40,6 +40,17 @@ def test_layernorm(lib, kw, want):
     assert layernorm(lib, **kw) == want
 
 
+def test_layernorm_of_more_rows_than_a_block_counts(lib):
+    """2^36 rows on four blocks are 2^31 tiles each: counted in 32 bits, none would be read."""
+    kw = dict(rows=1 << 36, p=1, ldx=1, ldy=1, ldh=1, H=None, mean=None, rstd=None)
+    assert layernorm(lib, **kw) == CUDA
+    before = lib.dp_set_reserved_sms(146)
+    try:
+        assert layernorm(lib, **kw) == UNSUPPORTED and layernorm(lib, **dict(kw, rows=1 << 35)) == CUDA
+    finally:
+        lib.dp_set_reserved_sms(before)
+
+
 def backward(lib, **kw):
     a = dict(G=A[0], ldg=64, X=A[1], ldx=64, dt=1, B=3, T=20, p=64, gain=A[2], pdt=0, mean=A[3], rstd=A[4], dX=A[5], lddx=64, gs=A[6],
              ss=A[7], sq=A[8], ws=None, n=0, status=None)
