@@ -761,10 +761,10 @@ dp_status ln_fwd_launch(LnForward& P, cudaStream_t st) {
   const int warps = P.S.W > 1 ? kBlock.warps / P.S.W * P.S.W : kBlock.warps;
   P.S.columns = ln_columns(NP, sizeof(T));
   if (!ln_fit(P.S, P.p, 1, false, warps, kBlock.blocks, kAligned)) return DP_ERR_UNSUPPORTED;
-  const dp_status r = ln_smem_setup(kernel);
-  if (r != DP_OK) return r;
   const long long blocks = std::min((P.rows + P.S.groups - 1) / P.S.groups, (long long)kBlock.blocks * sm_count());
   if (P.rows / blocks / P.S.groups >= 0x7fffffffLL - 1) return DP_ERR_UNSUPPORTED;       // a block counts its tiles in 32 bits
+  const dp_status r = ln_smem_setup(kernel);
+  if (r != DP_OK) return r;
   kernel<<<unsigned(blocks), (warps + (kAligned ? 1 : 0)) * 32, LnSmem(P.S, P.p, 1, false, warps).bytes, st>>>(P);
   DP_LAUNCH_OK();
   return DP_OK;
