@@ -378,7 +378,7 @@ size_t dp_layernorm_backward_ws_bytes(int32_t B, int32_t T, int32_t p);
  * be logits itself (same pitch).  Columns past V are neither read nor written.  Any alignment of whole elements works.
  * A row that counts needs its largest logit between -2.3e38 and
  * 2.3e38 (its softmax is NaN otherwise; -inf and the type's lowest value are fine beside one).  A target at -inf makes its sequence's
- * log-probability -inf, h_i infinite and the loss 0 or inf (a term of weight 0 is not there); both sequences of a pair at -inf: NaN.  beta >= 0, 0 <= smoothing <= 1; 2*B*T < 2^31; ws on an
+ * log-probability -inf, h_i infinite and the loss 0 or inf (a term of weight 0 is not there); both sequences of a pair at -inf: NaN.  beta >= 0, 0 <= smoothing <= 1; 2*B*T < 2^31; V <= 2^30; ws on an
  * 8-byte boundary. */
 dp_status dp_preference_loss(const void* logits, int64_t ldl, dp_dtype dt, int32_t B, int32_t T, int32_t V, const int32_t* targets,
                              const float* ref_logp, float beta, float smoothing, float scale, float* loss, float* logp, void* G,

@@ -295,6 +295,7 @@ __device__ __forceinline__ double warp_sum(double v) {
 }
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kMaxVocabulary = 1 << 30;                 // a thread counts columns in 32 bits, up to a block of them behind the row
 
 // A warp per row and kWarps rows per CTA where rows are short and many, else a CTA per row.  Statistics and gradients of 4096 bf16 rows, warps
 // against CTAs: 14 us against 43 with 1024 logits each, 18 against 45 with 2048, 25 against 49 with 4096, 37 against 57 with 8192; of 128 rows,
@@ -308,7 +309,7 @@ struct Place {
   int pair, first;                         // the block's first row within the pair
   int at, who;                             // this thread's row within the pair (2T or above: none) and its number on it
   __device__ __forceinline__ Place(const PrefParams& P, unsigned block) {
-    const unsigned blocks = unsigned(2 * P.T + kRows - 1) / kRows;
+    const unsigned blocks = (2u * unsigned(P.T) + kRows - 1) / kRows;
     pair = int(block / blocks);
     first = int(block % blocks) * kRows;
     at = first + (kByWarp ? int(threadIdx.x >> 5) : 0);
@@ -384,7 +385,7 @@ __global__ void __launch_bounds__(kThreads) pair_loss_kernel(const PrefParams P)
 template <typename T, bool kByWarp>
 dp_status pref_launch(const PrefParams& P, cudaStream_t st) {
   constexpr int per = Place<kByWarp>::kRows;
-  const unsigned blocks = unsigned(P.B) * (unsigned(2 * P.T + per - 1) / per);
+  const unsigned blocks = unsigned(P.B) * ((2u * unsigned(P.T) + per - 1) / per);
   row_stats_kernel<T, kByWarp><<<blocks, kThreads, 0, st>>>(P);
   DP_LAUNCH_OK();
   cudaLaunchConfig_t cfg = {};
@@ -422,7 +423,7 @@ dp_status dp_preference_loss(const void* logits, int64_t ldl, dp_dtype dt, int32
   if (dt != DP_F32 && dt != DP_BF16) return DP_ERR_INVALID_ARG;
   if (!std::isfinite(beta) || beta < 0.f || !(smoothing >= 0.f && smoothing <= 1.f) || !std::isfinite(scale)) return DP_ERR_INVALID_ARG;
   if (G == logits && ldg != ldl) return DP_ERR_INVALID_ARG;
-  if (2LL * B * T > 0x7fffffffLL) return DP_ERR_UNSUPPORTED;
+  if (2LL * B * T > 0x7fffffffLL || V > kMaxVocabulary) return DP_ERR_UNSUPPORTED;
   const size_t es = dt == DP_F32 ? 4 : 2;
   if (!on_boundary(es, logits, G) || !on_boundary(4, targets, ref_logp, loss, logp)) return DP_ERR_ALIGNMENT;
   if (!ws || ws_bytes < dp_preference_loss_ws_bytes(B, T)) return DP_ERR_WORKSPACE;

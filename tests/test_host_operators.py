@@ -108,6 +108,12 @@ def test_preference_loss(lib, kw, want):
     assert preference(lib, **kw) == want
 
 
+@pytest.mark.parametrize("V,want", [(1 << 30, CUDA), ((1 << 30) + 1, UNSUPPORTED), ((1 << 31) - 1, UNSUPPORTED)])
+def test_preference_loss_of_more_words_than_it_counts(lib, V, want):
+    """Columns are counted in 32 bits, up to a block's threads behind the row: near 2^31 that reads before it."""
+    assert preference(lib, B=1, T=1, V=V, ldl=V, ldg=V) == want
+
+
 def orthogonalize(lib, n=1, dt=0, out_dt=0, coefs=((3.4445, -4.7750, 2.0315),) * 5, steps=None, eps=1e-7, ws=A[2], size=1 << 30, second=None, **kw):
     arr = (binding._MatrixDesc * 2)()
     for D in arr:
