@@ -11,6 +11,9 @@ Tolerances, with u = 2^-24 (an fp32 rounding) and half(t) = torch.finfo(t).eps /
 """
 import ctypes
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -901,3 +904,45 @@ def test_workspaces_of_the_calls_themselves_are_not_in_use_on_another_stream(cal
     assert all(torch.equal(a, b) for a, b in zip(out, want))
     torch.cuda.synchronize()
     assert (kept == 7).all()
+
+
+FIRST_CALLS = """
+import threading, torch
+from paper_2609_40335_b200 import binding as dp
+errors = []
+
+def at_once(calls):
+    gate = threading.Barrier(len(calls))
+
+    def run(call):
+        gate.wait()
+        try:
+            call()
+        except Exception as e:
+            errors.append(repr(e))
+    threads = [threading.Thread(target=run, args=(c,)) for c in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+
+for dtype in (torch.float32, torch.bfloat16):
+    for p in (64, 65, 512, 1024, 1025, 4096, 16384):
+        x = torch.ones(6, p, device="cuda", dtype=dtype)
+        outs = [torch.empty_like(x) for _ in range(6)]
+        at_once([lambda o=o: dp.dp_layernorm(x, None, None, 1e-5, Y=o) for o in outs])
+for n in (40, 300):
+    m = torch.eye(n, device="cuda")
+    outs = [torch.empty_like(m) for _ in range(6)]
+    work = [torch.empty(dp.dp_orthogonalize_ws_bytes([m]), dtype=torch.uint8, device="cuda") for _ in outs]
+    at_once([lambda o=o, w=w: dp.dp_orthogonalize([m], [o], ws=w) for o, w in zip(outs, work)])
+torch.cuda.synchronize()
+print("errors", len(errors), errors[:2])
+"""
+
+
+def test_first_calls_of_several_threads():
+    """A kernel's set-up is done before any thread launches it."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS], env=dict(os.environ, PYTHONPATH=root), capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "errors 0 " in r.stdout, (r.stdout + r.stderr)[-1500:]
