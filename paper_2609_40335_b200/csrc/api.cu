@@ -51,12 +51,20 @@ int sm_count() {
   return std::max(2, n & ~1);
 }
 
-bool first_use_on_this_device(const void* key) {
-  static std::set<std::pair<const void*, int>> seen;
+namespace {
+std::set<std::pair<const void*, int>> g_set_up;
+}
+bool set_up_on_this_device(const void* key) {
   int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return true;     // set up again rather than never
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;    // set up again rather than never
   std::lock_guard<std::mutex> lock(g_device_mutex);
-  return seen.insert(std::make_pair(key, dev)).second;
+  return g_set_up.count(std::make_pair(key, dev)) != 0;
+}
+void has_set_up_on_this_device(const void* key) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return;
+  std::lock_guard<std::mutex> lock(g_device_mutex);
+  g_set_up.insert(std::make_pair(key, dev));
 }
 
 // ---- planning of dp_ghost_norms ------------------------------------------------------------

@@ -45,10 +45,18 @@ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 int sm_count();
 int device_sm_count();               // all of them, reserved or not
 
-// One-time set-up that CUDA keeps PER DEVICE (function attributes such as the dynamic
-// shared-memory limit): true the first time `key` is seen with the current device, false
-// afterwards.  A process that drives several GPUs gets the set-up on each of them.
-bool first_use_on_this_device(const void* key);
+// One-time set-up that CUDA keeps PER DEVICE (function attributes such as the dynamic shared-memory limit): the statements run until
+// they have succeeded once with the current device, and no call goes on before.  Threads that come at the same time may each
+// run them; a process that drives several GPUs gets the set-up on each of them.
+bool set_up_on_this_device(const void* key);
+void has_set_up_on_this_device(const void* key);
+#define DP_SET_UP_ONCE(key, ...)                          \
+  do {                                                    \
+    if (!::dpg::set_up_on_this_device(key)) {             \
+      __VA_ARGS__;                                        \
+      ::dpg::has_set_up_on_this_device(key);              \
+    }                                                     \
+  } while (0)
 
 // Persistent TMA kernels and the small ones that run beside them on a second stream all ask for the
 // largest shared-memory carve-out: an SM changes its carve-out only when it is idle, so a kernel

@@ -733,14 +733,14 @@ dp_status launch_embed_norms(const int* ids, const void* G, int64_t ldg, dp_dtyp
                              cudaStream_t st) {
   const int slabs = ceil_div(d, kEmbedColsPerBlock);
   const size_t smem = group_smem_bytes(T);
-  if (first_use_on_this_device(reinterpret_cast<const void*>(&launch_embed_norms))) {
+  DP_SET_UP_ONCE(reinterpret_cast<const void*>(&launch_embed_norms), {
     DP_CUDA_OK(cudaFuncSetAttribute(embed_norm_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                     (int)group_smem_bytes(kEmbedMaxT)));
     DP_CUDA_OK(cudaFuncSetAttribute(embed_norm_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                     (int)group_smem_bytes(kEmbedMaxT)));
     DP_CUDA_OK(prefer_max_shared(embed_norm_kernel<float>));
     DP_CUDA_OK(prefer_max_shared(embed_norm_kernel<__nv_bfloat16>));
-  }
+  });
   const int grid = B * slabs * parts;
   if (dt == DP_F32)
     embed_norm_kernel<float><<<grid, kEmbedNormThreads, smem, st>>>(
@@ -759,8 +759,8 @@ dp_status launch_clear(void* p, size_t bytes, cudaStream_t st) {
   }
   const size_t n16 = bytes / 16;
   if (n16) {
-    if (first_use_on_this_device(reinterpret_cast<const void*>(&launch_clear)))
-      DP_CUDA_OK(prefer_max_shared(clear_kernel));
+    DP_SET_UP_ONCE(reinterpret_cast<const void*>(&launch_clear),
+      DP_CUDA_OK(prefer_max_shared(clear_kernel)));
     const size_t blocks = std::min((n16 + kSideThreads - 1) / kSideThreads, size_t(sm_count()) * 16);
     clear_kernel<<<(unsigned)blocks, kSideThreads, 0, st>>>(static_cast<uint4*>(p), n16);
     DP_LAUNCH_OK();
@@ -771,7 +771,7 @@ dp_status launch_clear(void* p, size_t bytes, cudaStream_t st) {
 
 dp_status launch_embed_sort(const int* ids, int n, int V, const EmbedSortWs& ws, int* dev_status,
                             cudaStream_t st) {
-  if (first_use_on_this_device(reinterpret_cast<const void*>(&launch_embed_sort))) {
+  DP_SET_UP_ONCE(reinterpret_cast<const void*>(&launch_embed_sort), {
     DP_CUDA_OK(cudaFuncSetAttribute(sort_one_block_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                     (int)group_smem_bytes(kSortOneBlock)));
     DP_CUDA_OK(allow_shared(sort_rank_kernel<kSideThreads>, group_smem_bytes(kSortChunk)));
@@ -780,7 +780,7 @@ dp_status launch_embed_sort(const int* ids, int n, int V, const EmbedSortWs& ws,
     DP_CUDA_OK(prefer_max_shared(sort_scan_kernel));
     DP_CUDA_OK(prefer_max_shared(sort_prefix_kernel));
     DP_CUDA_OK(prefer_max_shared(sort_place_kernel));
-  }
+  });
   if (sort_in_one_block(n, V)) {
     sort_one_block_kernel<<<1, kSortThreads, group_smem_bytes(n), st>>>(ids, n, V, ws.seg, ws.perm, dev_status);
     DP_LAUNCH_OK();
@@ -840,11 +840,11 @@ dp_status launch_embed_scatter(const int* ids, const void* G, int64_t ldg, dp_dt
     DP_CUDA_OK(cudaMemset2DAsync(out, size_t(ldo) * sizeof(float), 0, size_t(d) * sizeof(float),
                                  size_t(V), st));
   }
-  if (first_use_on_this_device(reinterpret_cast<const void*>(&launch_embed_scatter))) {
+  DP_SET_UP_ONCE(reinterpret_cast<const void*>(&launch_embed_scatter), {
     DP_CUDA_OK(prefer_max_shared(embed_scatter_kernel<float>));
     DP_CUDA_OK(prefer_max_shared(embed_scatter_kernel<__nv_bfloat16>));
     DP_CUDA_OK(prefer_max_shared(embed_scatter_combine_kernel));
-  }
+  });
   static_assert(kScatCols == kSideThreads, "both passes take 128 columns per block");
   const dim3 grid(ceil_div(n, kScatChunk), ceil_div(d, kScatCols));
   if (dt == DP_F32)

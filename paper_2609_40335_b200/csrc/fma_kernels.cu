@@ -517,8 +517,8 @@ dp_status launch_cross_term_fma(const int* ids, const void* Ge, int64_t ldge, co
 
 dp_status launch_clip_factors(const float* sq, int B, float C, float* clip, float* norms,
                               cudaStream_t st, const float* extra, float* sum) {
-  if (first_use_on_this_device(reinterpret_cast<const void*>(&launch_clip_factors)))
-    DP_CUDA_OK(prefer_max_shared(clip_factors_kernel));
+  DP_SET_UP_ONCE(reinterpret_cast<const void*>(&launch_clip_factors),
+    DP_CUDA_OK(prefer_max_shared(clip_factors_kernel)));
   clip_factors_kernel<<<ceil_div(B, 128), 128, 0, st>>>(sq, extra, sum, B, C, clip, norms);
   DP_LAUNCH_OK();
   return DP_OK;
@@ -526,8 +526,8 @@ dp_status launch_clip_factors(const float* sq, int B, float C, float* clip, floa
 
 dp_status launch_finish_norms(const NormSources& S, int B, float C, float* sq, float* clip, float* norms,
                               cudaStream_t st) {
-  if (first_use_on_this_device(reinterpret_cast<const void*>(&launch_finish_norms)))
-    DP_CUDA_OK(prefer_max_shared(finish_norms_kernel));
+  DP_SET_UP_ONCE(reinterpret_cast<const void*>(&launch_finish_norms),
+    DP_CUDA_OK(prefer_max_shared(finish_norms_kernel)));
   finish_norms_kernel<<<ceil_div(B, 4), 128, 0, st>>>(S, B, C, sq, clip, norms);
   DP_LAUNCH_OK();
   return DP_OK;

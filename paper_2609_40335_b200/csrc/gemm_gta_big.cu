@@ -497,8 +497,8 @@ gemm_gta_big_kernel(const __grid_constant__ BigParams P) {
 
 template <bool kSplit, bool kByRow, Epilogue kEpilogue>
 static dp_status launch_big(const BigParams& P, int units, cudaStream_t st) {
-  if (first_use_on_this_device(reinterpret_cast<const void*>(&gemm_gta_big_kernel<kSplit, kByRow, kEpilogue>)))
-    DP_CUDA_OK((allow_shared(gemm_gta_big_kernel<kSplit, kByRow, kEpilogue>, kSmemBytes)));
+  DP_SET_UP_ONCE(reinterpret_cast<const void*>(&gemm_gta_big_kernel<kSplit, kByRow, kEpilogue>),
+    DP_CUDA_OK((allow_shared(gemm_gta_big_kernel<kSplit, kByRow, kEpilogue>, kSmemBytes))));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * units, 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);

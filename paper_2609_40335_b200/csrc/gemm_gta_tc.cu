@@ -612,8 +612,8 @@ constexpr bool kUsePair = true;
 // Launch on `units` persistent CTAs (single) or CTA pairs (cluster of 2).
 template <bool kScale, bool kSqsum, bool kPair, bool kSplit, bool kByRow>
 dp_status launch_gta(const GtaParams& P, int units, cudaStream_t st) {
-  if (first_use_on_this_device(reinterpret_cast<const void*>(&gemm_gta_kernel<kScale, kSqsum, kPair, kSplit, kByRow>)))
-    DP_CUDA_OK(allow_shared(gemm_gta_kernel<kScale, kSqsum, kPair, kSplit, kByRow>, Geo<kPair>::kSmemBytes));
+  DP_SET_UP_ONCE(reinterpret_cast<const void*>(&gemm_gta_kernel<kScale, kSqsum, kPair, kSplit, kByRow>),
+    DP_CUDA_OK(allow_shared(gemm_gta_kernel<kScale, kSqsum, kPair, kSplit, kByRow>, Geo<kPair>::kSmemBytes)));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(kPair ? 2 * units : units, 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
@@ -712,8 +712,8 @@ dp_status launch_clip_accumulate_tc(const dp_linear_desc* layers, int n_layers, 
         pre += prescale_bytes(D, B, T);
         const long long rows = (long long)B * T;
         const int blocks = (int)std::min<long long>((rows * (cp >> 3) + 255) / 256, (long long)sms * 16);
-        if (first_use_on_this_device(reinterpret_cast<const void*>(&prescale_rows_kernel)))
-          DP_CUDA_OK(prefer_max_shared(prescale_rows_kernel));
+        DP_SET_UP_ONCE(reinterpret_cast<const void*>(&prescale_rows_kernel),
+          DP_CUDA_OK(prefer_max_shared(prescale_rows_kernel)));
         prescale_rows_kernel<<<blocks, 256, 0, st>>>(
             static_cast<const __nv_bfloat16*>(narrow_a ? D.A : D.G), narrow_a ? D.lda : D.ldg, copy, cp,
             rows, T, c, clip);

@@ -351,8 +351,8 @@ ghost_norm_pair_kernel(const __grid_constant__ PairParams P) {
 
 template <int kHalf, bool kDiag>
 dp_status launch_variant(const PairParams& P, cudaStream_t st) {
-  if (first_use_on_this_device(reinterpret_cast<const void*>(&ghost_norm_pair_kernel<kHalf, kDiag>)))
-    DP_CUDA_OK((allow_shared(ghost_norm_pair_kernel<kHalf, kDiag>, kSmemBytes)));
+  DP_SET_UP_ONCE(reinterpret_cast<const void*>(&ghost_norm_pair_kernel<kHalf, kDiag>),
+    DP_CUDA_OK((allow_shared(ghost_norm_pair_kernel<kHalf, kDiag>, kSmemBytes))));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * std::min(P.total_items, sm_count() / 2), 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);

@@ -368,8 +368,8 @@ bool ghost_norm_split_pays(const std::vector<int>& index, const GhostPlan& plan,
 // keep: the wider operand's is stored
 dp_status launch_ghost_norm_split(const dp_linear_desc* layers, const SplitJob* jobs, const std::vector<int>& index,
                                   const GhostPlan& plan, int B, int T, bool keep, float* partials, int* dev_status, cudaStream_t st) {
-  if (first_use_on_this_device(reinterpret_cast<const void*>(&ghost_norm_split_kernel)))
-    DP_CUDA_OK(allow_shared(ghost_norm_split_kernel, kSmemBytes));
+  DP_SET_UP_ONCE(reinterpret_cast<const void*>(&ghost_norm_split_kernel),
+    DP_CUDA_OK(allow_shared(ghost_norm_split_kernel, kSmemBytes)));
   const int rows = (plan.pack * T + 15) / 16 * 16, groups = ceil_div(B, plan.pack);
   for (size_t g0 = 0; g0 < index.size(); g0 += kMaxLayers) {
     const size_t g1 = std::min(index.size(), g0 + kMaxLayers);

@@ -397,8 +397,8 @@ __global__ void reduce_partials_kernel(const float* __restrict__ partials, int n
 
 dp_status launch_reduce_partials(const float* partials, int n_per, int B, float* sq,
                                  float factor, float* plain_out, cudaStream_t st, bool overwrite) {
-  if (first_use_on_this_device(reinterpret_cast<const void*>(&launch_reduce_partials)))
-    DP_CUDA_OK(prefer_max_shared(reduce_partials_kernel));
+  DP_SET_UP_ONCE(reinterpret_cast<const void*>(&launch_reduce_partials),
+    DP_CUDA_OK(prefer_max_shared(reduce_partials_kernel)));
   const int warps = 4;
   reduce_partials_kernel<<<ceil_div(B, warps), warps * 32, 0, st>>>(partials, n_per, B, sq,
                                                                   factor, plain_out, overwrite ? 1 : 0);
@@ -410,8 +410,8 @@ namespace {
 
 template <bool kDiagOnly, bool kSplit, Rows kRows, int kBoxes>
 dp_status launch_variant(const GhostParams& P, cudaStream_t st) {
-  if (first_use_on_this_device(reinterpret_cast<const void*>(&ghost_norm_tc_kernel<kDiagOnly, kSplit, kRows, kBoxes>)))
-    DP_CUDA_OK((allow_shared(ghost_norm_tc_kernel<kDiagOnly, kSplit, kRows, kBoxes>, kSmemBytes)));
+  DP_SET_UP_ONCE(reinterpret_cast<const void*>(&ghost_norm_tc_kernel<kDiagOnly, kSplit, kRows, kBoxes>),
+    DP_CUDA_OK((allow_shared(ghost_norm_tc_kernel<kDiagOnly, kSplit, kRows, kBoxes>, kSmemBytes))));
   const int grid = std::min(P.total_items, sm_count());
   ghost_norm_tc_kernel<kDiagOnly, kSplit, kRows, kBoxes><<<grid, kThreads, kSmemBytes, st>>>(P);
   DP_LAUNCH_OK();

@@ -648,10 +648,10 @@ int ln_pieces(const LnShape& S, int p, int es) {
 
 template <typename K>
 dp_status ln_smem_setup(K* kernel) {
-  if (first_use_on_this_device((const void*)kernel)) {
+  DP_SET_UP_ONCE((const void*)kernel, {
     DP_CUDA_OK(allow_shared(kernel, 227 * 1024));
     DP_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-  }
+  });
   return DP_OK;
 }
 

@@ -128,8 +128,8 @@ dp_status launch_add_noise(float* out, long long rows, int cols, long long ld, b
   const long long nq = (n + 3) >> 2;
   const NoiseKeys keys = expand_noise_keys(seed);
   if (fill && ld == cols && (reinterpret_cast<uintptr_t>(out) & 15) == 0) {
-    if (first_use_on_this_device(reinterpret_cast<const void*>(&launch_add_noise)))
-      DP_CUDA_OK(prefer_max_shared(fill_noise_kernel));
+    DP_SET_UP_ONCE(reinterpret_cast<const void*>(&launch_add_noise),
+      DP_CUDA_OK(prefer_max_shared(fill_noise_kernel)));
     for (long long q0 = 0; q0 < nq; q0 += kFillSlice) {
       const long long m = std::min(nq - q0, kFillSlice), q = first_quad + q0;
       const int tail = q0 + m == nq ? int(n & 3) : 0;

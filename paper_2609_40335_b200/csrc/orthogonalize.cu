@@ -823,7 +823,7 @@ dp_status ns_small_launch(const dp_matrix_desc* mats, int n, dp_dtype dt, dp_dty
   NsSmallParams P;
   P.steps = steps; P.dt = dt; P.out_dt = out_dt; P.eps = eps;
   std::memcpy(P.coef, coefs, sizeof(float) * 3 * size_t(steps));
-  if (first_use_on_this_device((const void*)ns_small_kernel)) DP_CUDA_OK(allow_shared(ns_small_kernel, sizeof(NsSmallSmem)));
+  DP_SET_UP_ONCE((const void*)ns_small_kernel, DP_CUDA_OK(allow_shared(ns_small_kernel, sizeof(NsSmallSmem))));
   for (int k0 = 0; k0 < n; k0 += kSmallMats) {
     const int here = std::min(kSmallMats, n - k0);
     for (int k = 0; k < here; ++k) {
@@ -924,7 +924,7 @@ int fused_steps(const std::vector<NsStep>& plan, size_t k, double most) {
 template <Product kProduct, bool kPair>
 dp_status ns_launch(const NsParams& P, cudaStream_t st) {
   auto* kernel = ns_product_kernel<kProduct, kPair>;
-  if (first_use_on_this_device((const void*)kernel)) DP_CUDA_OK(allow_shared(kernel, kSmemBytes));
+  DP_SET_UP_ONCE((const void*)kernel, DP_CUDA_OK(allow_shared(kernel, kSmemBytes)));
   const int units = kPair ? sm_count() / 2 : sm_count();
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((kPair ? 2 : 1) * std::min(P.total_items, units));

@@ -437,10 +437,10 @@ constexpr size_t kMostGramSmem = size_t(2) * kGramTile * 2 * (kMaxCols + 4) * si
 
 template <typename TL, typename TE>
 dp_status launch(const SmallParams& P, size_t smem, cudaStream_t st) {
-  if (first_use_on_this_device(reinterpret_cast<const void*>(&small_norms_kernel<TL, TE>))) {
+  DP_SET_UP_ONCE(reinterpret_cast<const void*>(&small_norms_kernel<TL, TE>), {
     DP_CUDA_OK((allow_shared(small_norms_kernel<TL, TE>, kMostGramSmem)));
     DP_CUDA_OK((prefer_max_shared(small_sums_kernel<TL, TE>)));
-  }
+  });
   small_norms_kernel<TL, TE><<<P.n_gram + P.B * P.slabs, kThreads, smem, st>>>(P);
   DP_LAUNCH_OK();
   cudaLaunchConfig_t cfg = {};

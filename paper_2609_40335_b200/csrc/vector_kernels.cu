@@ -356,8 +356,8 @@ size_t vector_keep_bytes(const dp_vector_desc* prm, int n, int B) {
 dp_status launch_vector_kept_sums(const dp_vector_desc* prm, int n, int B, int T, float* keep, const float* clip,
                                   float* const* outs, float beta, int with_noise, float amp, float scale, uint64_t seed,
                                   const uint32_t* tensor_ids, uint32_t step, cudaStream_t st) {
-  if (first_use_on_this_device(reinterpret_cast<const void*>(&vector_kept_sum_kernel)))
-    DP_CUDA_OK(prefer_max_shared(vector_kept_sum_kernel));
+  DP_SET_UP_ONCE(reinterpret_cast<const void*>(&vector_kept_sum_kernel),
+    DP_CUDA_OK(prefer_max_shared(vector_kept_sum_kernel)));
   const int n_per = vector_total_slabs(prm, n);
   // one block walks all examples as long as that is short; beyond, parts at least as long as there are parts.  Step of six biases of 768
   // at T = 8 and B = 256, 1024, 4096: 72, 167, 478 us with G read twice, 64, 151, 431 now.
