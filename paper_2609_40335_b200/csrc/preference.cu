@@ -27,7 +27,20 @@ namespace dpg {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr double kLog2e64 = 1.4426950408889634;
+constexpr float kLog2e = float(kLog2e64), kLog2eLow = float(kLog2e64 - double(kLog2e));
+// What kLog2e leaves out of x log2 e.  For logits past 2^20 that of 2^20: it only has to be alike in a row, whose logits there are 2^-3 apart at least,
+// and must not outgrow the exponents.
+__device__ __forceinline__ float exponent_rest(float x) { return fminf(fmaxf(x, -1048576.f), 1048576.f) * kLog2eLow; }
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// 2^d of a whole number up to 127; 0 below 2^-126, and of NaN
+__device__ __forceinline__ float exp2_whole(float d) { return d >= -126.f ? __int_as_float((int(d) + 127) << 23) : 0.f; }
 
 // 16 bytes of logits: eight bf16 or four fp32
 template <typename T> struct Quad;
@@ -50,6 +63,9 @@ template <> struct Quad<__nv_bfloat16> {
     return q;
   }
   static __device__ __forceinline__ __nv_bfloat16 round(float v) { return __float2bfloat16_rn(v); }
+  // 2^(x log2 e + minus)
+  static constexpr bool kRest = false;
+  static __device__ __forceinline__ float power(float x, float minus) { return exp2_fast(fmaf(x, kLog2e, minus)); }
   // largest of U pieces (NaN apart), two values at a time
   template <int U>
   static __device__ __forceinline__ float top(const uint4 (&q)[U]) {
@@ -73,6 +89,12 @@ template <> struct Quad<float> {
     return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
   }
   static __device__ __forceinline__ float round(float v) { return v; }
+  static constexpr bool kRest = true;                    // log2 e in two terms
+  static __device__ __forceinline__ float power(float x, float minus) {
+    constexpr float kMagic = 12582912.f;                 // 1.5 * 2^23: what is added to it is rounded to a whole number, in its low bits
+    const float r = fmaf(x, kLog2e, minus), u = fmaxf(r, -126.f) + kMagic;
+    return exp2_fast(r - (u - kMagic) + exponent_rest(x)) * __int_as_float((__float_as_int(u) << 23) + 0x3f800000);
+  }
   template <int U>
   static __device__ __forceinline__ float top(const uint4 (&q)[U]) {
     float m = -INFINITY;
@@ -86,32 +108,37 @@ template <> struct Quad<float> {
   }
 };
 
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
-// Sum of 2^(x log2 e - c) over the values seen so far; c a reference near their maximum * log2 e, -inf of none.  The reference moves
+// Sum of 2^(x log2 e - c) over the values seen so far; c a whole number near their maximum * log2 e, -inf of none.  The reference moves
 // only when a value exceeds it by 2: nearly every warp would meet a new maximum in every piece of a row otherwise.  An exponent is
 // one FMA, whose rounding is a term's error: 2^-24 of the exponent, which is at most 2 for the largest terms (a bound of 16 took the
-// same time and gave fp32 gradients twice the error).  The rounding of c cancels wherever the same c is used.
+// same time and gave fp32 gradients twice the error).  Whole references change by factors that are exact: ex2 is 5e-8 low on average where its
+// argument is negative, and a row's sum meets eight to ten joins of lanes and warps (2.6e-7 in all, the same way for every token).
+// fp32 logits give ex2 the part of the exponent between -0.5 and 0.5, where it is 8e-9 low, and log2 e in two terms; bf16 ones, whose own
+// rounding is 4e-3, take ex2 and one term, the same in the sum and at the target (the softmax of logits 1.3e-8 smaller); so do gradients, which
+// are not added up.  Error of a token's log-probability, 50257 words, on average and around it: fp32 2e-9 and 4.5e-8, bf16 1.4e-8 and
+// 4.9e-8; with references that are no whole numbers and fp32 logits treated like bf16 ones 2.0e-7 and 5.1e-8, which 300 tokens add up to 1e-6 of a
+// gradient (6e-8 now).  That costs the fp32 call 3 to 5 %: (8, 2 x 128, 50257) 210 us -> 217, statistics alone 87 -> 91; bf16 ones nothing that shows.
 struct Softmax {
   float c, s;
-  static __device__ __forceinline__ float exponent(float x, float c) { return fmaf(x, kLog2e, c == -INFINITY ? 0.f : -c); }
+  __device__ __forceinline__ float minus() const { return c == -INFINITY ? 0.f : -c; }
   __device__ __forceinline__ void reach(float top) {     // the largest of the next values, in units of c
-    if (top > c + 2.f) { s *= exp2_fast(c - top); c = top; }
+    if (top > c + 2.f) {
+      top = ceilf(top);
+      s *= exp2_whole(c - top);
+      c = top;
+    }
   }
+  template <typename T>
   __device__ __forceinline__ void add(float x) {
     reach(x * kLog2e);
-    s += exp2_fast(exponent(x, c));
+    s += Quad<T>::power(x, minus());
   }
   // pieces of 16 bytes
   template <typename T, int U>
   __device__ __forceinline__ void add(const uint4 (&q)[U]) {
     constexpr int N = Quad<T>::N;
     reach(Quad<T>::template top<U>(q) * kLog2e);
-    const float minus = c == -INFINITY ? 0.f : -c;
+    const float m = minus();
     float t[N];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -119,7 +146,7 @@ struct Softmax {
       Quad<T>::unpack(q[u], v);
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        const float p = exp2_fast(fmaf(v[e], kLog2e, minus));
+        const float p = Quad<T>::power(v[e], m);
         t[e] = u ? t[e] + p : p;
       }
     }
@@ -132,7 +159,7 @@ struct Softmax {
   __device__ __forceinline__ void join(float oc, float os) {
     const float top = fmaxf(c, oc);
     if (top == -INFINITY) { s += os; return; }       // nothing in either (or only NaN, which the sums carry)
-    s = s * exp2_fast(c - top) + os * exp2_fast(oc - top);
+    s = s * exp2_whole(c - top) + os * exp2_whole(oc - top);
     c = top;
   }
 };
@@ -183,8 +210,8 @@ __device__ __forceinline__ Softmax scan_row(const T* x, int V, int tid, int n) {
     const uint4 q[1] = {xq[k]};
     acc.add<T>(q);
   }
-  for (int c = tid; c < head; c += n) acc.add(to_f32(x[c]));
-  for (int c = head + quads * N + tid; c < V; c += n) acc.add(to_f32(x[c]));
+  for (int c = tid; c < head; c += n) acc.add<T>(to_f32(x[c]));
+  for (int c = head + quads * N + tid; c < V; c += n) acc.add<T>(to_f32(x[c]));
   return acc;
 }
 
@@ -198,9 +225,10 @@ __device__ __forceinline__ Softmax warp_join(Softmax a) {
 }
 
 // in 64 bits: thousands of these are added up, and the difference of two such sums is what the loss is of
+template <typename T>
 __device__ __forceinline__ double token_logp(float x, const Softmax& a) {
   const double c = a.c == -INFINITY ? 0.0 : double(a.c);
-  return (fma(double(x), double(kLog2e), -c) - log2(double(a.s))) * 0.6931471805599453;
+  return (fma(double(x), double(kLog2e), -c) + (Quad<T>::kRest ? double(exponent_rest(x)) : 0.0) - log2(double(a.s))) * 0.6931471805599453;
 }
 
 // 16 bytes from byte `off` of a and b, a multiple of two
@@ -221,9 +249,9 @@ __device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, uint32_
 template <typename T>
 __device__ __forceinline__ void write_gradient(const T* x, T* g, int V, int target, float c, float row_c, float inv, int tid, int n) {
   constexpr int N = Quad<T>::N, U = 4;
-  const float f = c * inv;
+  const float f = c * inv, minus = row_c == -INFINITY ? 0.f : -row_c;
   auto grad = [&](float v, int k) {
-    const float e = f * exp2_fast(Softmax::exponent(v, row_c));
+    const float e = f * exp2_fast(fmaf(v, kLog2e, minus));
     return k == target ? c - e : -e;
   };
   // quads of g, and the columns around them.  Where x lies otherwise on its 16 bytes (dense logits, a G whose rows are padded), a quad is put
@@ -243,7 +271,6 @@ __device__ __forceinline__ void write_gradient(const T* x, T* g, int V, int targ
     float v[N];
     Quad<T>::unpack(q, v);
     const int at = head + k * N, hit = target - at;
-    const float minus = row_c == -INFINITY ? 0.f : -row_c;
 #pragma unroll
     for (int e = 0; e < N; ++e) v[e] = -f * exp2_fast(fmaf(v[e], kLog2e, minus));
     if (hit >= 0 && hit < N) {
@@ -336,9 +363,10 @@ row_stats_kernel(const PrefParams P) {
     if (warp == 0) a = warp_join(lane < kWarps ? Softmax{sc[lane], ss[lane]} : Softmax{-INFINITY, 0.f});
   }
   if (here && p.who == 0) {
-    P.row_logp[row] = target < 0 ? 0.0 : token_logp(to_f32(x[target]), a);
+    P.row_logp[row] = target < 0 ? 0.0 : token_logp<T>(to_f32(x[target]), a);
     P.row_c[row] = a.c;
-    P.row_inv[row] = target < 0 ? 0.f : 1.f / a.s;
+    // the gradient's exponents leave the rest out: here it is that of the reference
+    P.row_inv[row] = target < 0 ? 0.f : (Quad<T>::kRest ? exp2f(exponent_rest(a.c / kLog2e)) : 1.f) / a.s;
   }
 }
 

@@ -414,6 +414,27 @@ def test_preference_loss_of_answers_that_cannot_be(dtype, smoothing, V):
     close(G, wg, room, DT[dtype])
 
 
+@pytest.mark.parametrize("dtype,room", [("f32", 3e-8), ("bf16", 1.2e-7)])
+@pytest.mark.parametrize("V", [4099, 16384, 50257])
+def test_preference_loss_token_errors_do_not_add_up(dtype, room, V):
+    """The mean error of a token's log-probability, which every token of a sequence has alike, read from the loss of a pair whose other sequence
+    and reference leave h small.  A row's sum is joined by exact powers of two, so that it has ex2's mean error only: on 2^20
+    arguments -0.8e-8 between -0.5 and 0.5 (what fp32 logits give it), -5.1e-8 below 0 (bf16 ones), and 1.3e-8 of a logit's distance from the mean logit (4 at
+    most here) from log2 e in one term; around it 5e-8 a token, 3e-9 of 300."""
+    B, T, beta = 6, 300, 100.0
+    x = tensor((B, 2 * T, V), DT[dtype], 40, std=1.5)
+    t = torch.full((B, 2, T), -1, dtype=torch.int32)
+    t[:, 0] = torch.randint(0, V, (B, T), generator=torch.Generator().manual_seed(1), dtype=torch.int32)
+    rows = torch.log_softmax(x[:, :T].double(), -1)
+    want = rows.gather(2, t[:, 0, :, None].long().cuda())[..., 0].sum(-1)
+    ref = torch.zeros(B, 2, device="cuda")
+    ref[:, 0] = want.float()
+    loss = torch.empty(B, device="cuda")
+    dp.dp_preference_loss(x, t.cuda(), ref, beta, loss=loss)
+    got = -torch.log(torch.expm1(loss.double())) / beta + ref[:, 0].double()         # loss = log(1 + exp(-h))
+    assert ((got - want) / T).abs().max() < room, ((got - want) / T).tolist()
+
+
 @pytest.mark.parametrize("shift", [3e4, -2e5])
 def test_preference_loss_large_logits(shift):
     """The maximum's rounding cancels: logits far from zero give what the same logits near zero give, as far as they are the same."""
