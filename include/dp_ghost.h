@@ -376,8 +376,8 @@ size_t dp_layernorm_backward_ws_bytes(int32_t B, int32_t T, int32_t p);
  * (s the logistic function), logp [dev, (B, 2) floats] = l, and G [dev, (2*B*T, V) of dt] = scale * d loss / d logits, the G of an
  * LM head in dp_ghost_norms and dp_clip_accumulate* with sequences of 2*T tokens.  loss, logp, G: each may be NULL, not all; G may
  * be logits itself (same pitch).  Columns past V are neither read nor written.  Any alignment of whole elements works.
- * A row that counts needs its largest logit between -2.3e38 and
- * 2.3e38 (its softmax is NaN otherwise; -inf and the type's lowest value are fine beside one).  A target at -inf makes its sequence's
+ * A row that counts needs its largest logit between -7.4e8 and 7.4e8: its softmax is NaN otherwise, of a row of nothing but -inf and
+ * the type's lowest value too.  Beside one such logit, -inf and the lowest value are words that cannot be.  A target at -inf makes its sequence's
  * log-probability -inf, h_i infinite and the loss 0 or inf (a term of weight 0 is not there); both sequences of a pair at -inf: NaN.  beta >= 0, 0 <= smoothing <= 1; 2*B*T < 2^31; V <= 2^30; ws on an
  * 8-byte boundary. */
 dp_status dp_preference_loss(const void* logits, int64_t ldl, dp_dtype dt, int32_t B, int32_t T, int32_t V, const int32_t* targets,

@@ -192,6 +192,8 @@ __device__ __forceinline__ int head_of(const T* x, int V) {
   return min(V, int(((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / sizeof(T)));
 }
 
+constexpr float kMostReference = 1073741824.f;
+
 // This thread's share of a row's statistics, one thread of n.
 template <typename T>
 __device__ __forceinline__ Softmax scan_row(const T* x, int V, int tid, int n) {
@@ -363,6 +365,8 @@ row_stats_kernel(const PrefParams P) {
     if (warp == 0) a = warp_join(lane < kWarps ? Softmax{sc[lane], ss[lane]} : Softmax{-INFINITY, 0.f});
   }
   if (here && p.who == 0) {
+    // past 2^30 a reference's rounding outgrows the exponents that fp32 holds; no finite logit at all, or none but the lowest
+    if (!(fabsf(a.c) < kMostReference)) a.s = NAN;
     P.row_logp[row] = target < 0 ? 0.0 : token_logp<T>(to_f32(x[target]), a);
     P.row_c[row] = a.c;
     // the gradient's exponents leave the rest out: here it is that of the reference

@@ -453,6 +453,45 @@ def test_preference_loss_large_logits(shift):
     assert np.abs(out[0][1] - out[1][1]).max() < 1e-6
 
 
+@pytest.mark.parametrize("V", [50, 20000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("top", [1e6, -1e6, 3e7, -3e7, 7e8, -7e8])
+def test_preference_loss_of_huge_logits(dtype, top, V):
+    """Two words alike at the top, a step of the type below it and far below: probabilities of the logits as they are held."""
+    x, t, ref = pref_inputs(2, 3, V, dtype, 12)
+    t[:] = 5
+    x.copy_((x.float() + top * (2 if top < 0 else 0.5)).to(DT[dtype]))
+    peak = torch.tensor(top, dtype=DT[dtype])
+    x[..., 5], x[..., V - 1] = peak, peak
+    x[1, 2, 5] = torch.nextafter(peak.float(), torch.tensor(-1e38)) if dtype == "f32" else peak - abs(peak) * 2.0 ** -7
+    loss, logp, G = torch.empty(2, device="cuda"), torch.empty(2, 2, device="cuda"), torch.empty_like(x)
+    beta = 1e-9                                                        # (a step below the top is up to 5e6)
+    dp.dp_preference_loss(x, t, None, beta, loss=loss, logp=logp, G=G)
+    wl, wp, wg = O.preference_loss(f64(x), t.cpu().numpy(), None, beta)
+    # a row's reference is off by 2^-24 of itself, 64 at most, and so exponents at the top are up to 64, rounded by 64 U; log2 e in one term is
+    # 1.4e-8 off, of the distance from the top
+    close(logp, wp, 3 * (64 * U + 2 ** -20) + 2e-8 * np.abs(wp))
+    close(loss, wl, beta * 1e-3 + beta * 2e-8 * np.abs(wp).sum(-1) + 4 * U)
+    close(G, wg, beta * 1e-4, DT[dtype])
+
+
+@pytest.mark.parametrize("V", [50, 20000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_preference_loss_past_the_logits_it_takes_is_nan_in_its_pair(dtype, V):
+    lowest = torch.finfo(DT[dtype]).min
+    x, t, ref = pref_inputs(9, 3, V, dtype, 13)
+    t[:] = 5
+    good = [torch.empty(9, device="cuda"), torch.empty(9, 2, device="cuda"), torch.empty_like(x)]
+    dp.dp_preference_loss(x, t, ref, 0.1, loss=good[0], logp=good[1], G=good[2])
+    for i, v in enumerate((1e12, -1e12, 1e20, -1e30, 3e38, lowest, float("-inf"), float("inf"))):
+        x[i, 1] = v
+    x[7, 1, : V // 2] = lowest
+    loss, logp, G = (torch.empty_like(v) for v in good)
+    dp.dp_preference_loss(x, t, ref, 0.1, loss=loss, logp=logp, G=G)
+    assert torch.isnan(loss[:8]).all() and torch.isnan(logp[:8, 0]).all() and torch.isnan(G[:8]).all()
+    assert torch.equal(loss[8], good[0][8]) and torch.equal(logp[8], good[1][8]) and torch.equal(G[8], good[2][8])
+
+
 def test_preference_gradient_by_differences():
     B, T, V = 2, 3, 40
     x, t, ref = pref_inputs(B, T, V, "f32", 21)
