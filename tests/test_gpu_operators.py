@@ -203,6 +203,36 @@ def test_layernorm_backward_parts_of_the_outputs():
         assert torch.equal(out, dx) and torch.equal(again, gs)
 
 
+@pytest.mark.parametrize("p", [7, 768, 1001, 2049])
+def test_layernorm_backward_by_differences(p):
+    """dX, gain and shift sums against differences of the forward pass along random directions."""
+    B, T, step = 2, 5, 2.0 ** -5
+    x, g = tensor((B, T, p), torch.float32, 1, 1.0, 0.3), tensor((B, T, p), torch.float32, 2)
+    gain, shift = tensor((1, p), torch.float32, 3, 0.3, 1.0)[0], tensor((1, p), torch.float32, 4)[0]
+    mean, rstd = torch.empty(B, T, device="cuda"), torch.empty(B, T, device="cuda")
+
+    def value(x, gain, shift):
+        y = torch.empty_like(x)
+        dp.dp_layernorm(x, gain, shift, 1e-5, Y=y, mean=mean, rstd=rstd)
+        return (y.double() * g.double()).sum(-1)
+    value(x, gain, shift)
+    dx, gs, ss = torch.empty_like(x), torch.empty(B, p, device="cuda"), torch.empty(B, p, device="cuda")
+    dp.dp_layernorm_backward(g, x, gain, mean, rstd, dX=dx, gain_sums=gs, shift_sums=ss)
+    size = rstd.double()
+    dirs = [tensor(t.shape, torch.float32, 5 + k) for k, t in enumerate((x, gain[None], shift[None]))]
+    d, dg, db = dirs[0], dirs[1][0], dirs[2][0]
+    y_size = float((g.abs().double().sum(-1)).max()) * 8                # sums of |g| |y|
+    up, down = value(x + step * d, gain, shift), value(x - step * d, gain, shift)
+    # roundings of y (45 U of its size at most) over the step; the third derivative of a norm, below 15 |d rstd|^3 sqrt(p)'s share of each row
+    bend = 15 * step ** 2 / 6 * (d.double().abs().amax(-1) * size) ** 3 * g.double().abs().sum(-1) * float(gain.abs().max())
+    got = (dx.double() * d.double()).sum(-1)
+    assert ((up - down) / (2 * step) - got).abs().le(bend + 45 * U * y_size / step).all()
+    # y is linear in gain and shift
+    up, down = value(x, gain + step * dg, shift + step * db), value(x, gain - step * dg, shift - step * db)
+    got = (gs.double() * dg.double() + ss.double() * db.double()).sum(-1)
+    assert (((up - down) / (2 * step)).sum(-1) - got).abs().max() <= T * 45 * U * y_size / step + 100 * U * T * y_size
+
+
 @pytest.mark.parametrize("B,T,p,dtype", [(8, 300, 768, "bf16"), (2, 500, 4096, "f32"), (1, 4100, 64, "f32"), (3, 40, 7, "bf16")])
 def test_layernorm_wait_limit_leaves_the_context_usable(B, T, p, dtype):
     """Waits that run out are reported, or the result is right; the same call is right afterwards."""

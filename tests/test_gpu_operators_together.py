@@ -170,3 +170,27 @@ def test_orthogonal_updates_of_a_step(dtype):
     made = pipeline.orthogonal_updates(ds, scale=0.5)
     assert set(made) == {f"linear{k}" for k in range(len(ds.linears))} and int(ds.dev_status.item()) == 0
     assert all(m.dtype == torch.float32 for m in made.values())
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_orthogonal_updates_on_another_stream_are_tensors_of_it(raw):
+    """Updates that the call makes do not lie where the current stream still reads."""
+    ds = pipeline.upload(make_workload("updates", B=3, T=16, dtype="f32", block_shapes=[(256, 512)], n_blocks=1, d_model=256, V=97, lm_head=True))
+    pipeline.allocate(ds)
+    pipeline.dp_step(ds, seed=1, step=2)
+    want = {n: u.clone() for n, u in pipeline.orthogonal_updates(ds).items()}
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    bait = torch.full_like(want["linear0"], 7.0)
+    kept = torch.empty_like(bait)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)                               # some 100 ms
+    kept.copy_(bait)
+    del bait
+    got = pipeline.orthogonal_updates(ds, stream=side.cuda_stream if raw else side)
+    side.synchronize()
+    with torch.cuda.stream(side):
+        assert all(torch.equal(got[n], want[n]) for n in want)
+    torch.cuda.synchronize()
+    assert (kept == 7.0).all()
