@@ -951,8 +951,8 @@ int tiles_of(Product product, int m, int n, int tile) {
 // How a group of matrices runs: on CTA pairs or single CTAs, the same for all products, since symmetric matrices are stored by the tile; and
 // how far A's error may grow in fused steps, 1 where each is by itself.  Whichever takes less time in whole waves of K steps, a launch counting
 // three more.  A pair's K step is 1.7 times as long for twice the work per CTA: a single CTA's reads 64 KB of shared memory's tiles anew for half
-// of the MMAs (tensor pipe at 45 %).  Pairs against single CTAs: layers of 6 blocks of width 768 1.43 ms against 1.56, of 24 of 1024 13.3
-// against 14.5; of one of 768, which leave pairs without work, 0.52 against 0.40.
+// of the MMAs (tensor pipe at 45 %).  Pairs against single CTAs: layers of 6 blocks of width 768 in fp32 1.61 ms against 1.88, of 24 of 1024 to bf16
+// 11.9 against 12.9; of one of 768 in fp32, which leave pairs without work, 0.66 against 0.58.
 struct NsForm { bool pair; double growth; };
 NsForm choose_form(const std::vector<NsShape>& shapes, const std::vector<NsStep>& plan, bool bf16_out) {
   int least_m = shapes[0].m;

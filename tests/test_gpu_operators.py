@@ -996,6 +996,23 @@ def test_workspaces_of_the_calls_themselves_are_not_in_use_on_another_stream(cal
     assert (kept == 7).all()
 
 
+@pytest.mark.parametrize("stream", [0, "default", "current"])
+def test_workspaces_of_the_calls_themselves_on_the_default_stream(stream):
+    """The default stream, by its number and as an object, while another one is current and while not."""
+    m = tensor((200, 300), torch.float32, 1)
+    want, got = torch.empty_like(m), torch.empty_like(m)
+    dp.dp_orthogonalize([m], [want])
+    torch.cuda.synchronize()
+    s = {0: 0, "default": torch.cuda.default_stream(), "current": torch.cuda.current_stream()}[stream]
+    for current in (torch.cuda.default_stream(), torch.cuda.Stream()):
+        got.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(current):
+            dp.dp_orthogonalize([m], [got], stream=s)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+
+
 FIRST_CALLS = """
 import threading, torch
 from paper_2609_40335_b200 import binding as dp
