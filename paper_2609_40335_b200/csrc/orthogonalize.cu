@@ -853,10 +853,11 @@ struct NsShape {
   size_t bytes() const { return 2 * x_bytes + 7 * a_bytes; }
 };
 
-// The power of two that brings values of at most `bound` below half of fp16's largest.
+// The power of two that brings values of at most `bound` below half of fp16's largest.  (Bounds below 1e-30 are those of results that fp32
+// does not hold.)
 float scale_for(double bound) {
   int e = 0;
-  frexp(std::max(bound, 1e-6), &e);                  // bound < 2^e
+  frexp(std::max(bound, 1e-30), &e);                 // bound < 2^e
   return float(ldexp(1.0, 15 - e));
 }
 

@@ -755,6 +755,21 @@ def test_orthogonalize_other_polynomials_in_steps_at_once(name, out, coefs):
         assert beyond_rounding(outs[k], want) < 2 * ns_room([shapes[k]], torch.float32)
 
 
+@pytest.mark.parametrize("name", ["single", "single, bf16 three at once", "pairs, one size"])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("coefs", [((1e-3, 0.0, 0.0),) * 8, ((1e-2, 1e-3, 1e-3),) * 10, ((0.0, 1e-2, 0.0),), ((1e-3, 0.0, 0.0),) * 3 + ((1e3, 0.0, 0.0),) * 3])
+def test_orthogonalize_polynomials_that_shrink(name, out, coefs):
+    """Results down to 1e-27 have the digits that others have."""
+    shapes = NS_FORMS[name][0]
+    mats = [tensor(s, torch.float32, 70 + k) for k, s in enumerate(shapes)]
+    outs = [torch.empty(s, device="cuda", dtype=DT[out]) for s in shapes]
+    dp.dp_orthogonalize(mats, outs, coefs=coefs)
+    for k in (0, len(shapes) - 1):
+        want = O.orthogonalize(f64(mats[k]), coefs)
+        # a product's error is at most that of the powers that it takes of A, three of them here
+        assert 1e-35 < np.linalg.norm(want) and beyond_rounding(outs[k], want) < 3 * ns_room([shapes[k]], torch.float32)
+
+
 EXTREME = {"a CTA": [(48, 80)], "single": [(200, 330)], "single, tall": [(330, 200)], "at once": [(300, 1000)], "at once, in fp32 too": [(700, 1301)]}
 
 
