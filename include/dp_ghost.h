@@ -390,7 +390,8 @@ size_t dp_preference_loss_ws_bytes(int32_t B, int32_t T);
  *   X = M / (||M||_F + eps);  `steps` times  A = X X^T, X <- a X + (b A + c A A) X  with (a, b, c) = coefs[3*k..]  [host, 3*steps];
  *   out [dev, (p, d) of out_dt, pitch ldo] = scale * X
  * (of the transpose where p > d: the same X).  All matrices run together.  Products are taken on fp16 operands of two terms (22 bits) with fp32
- * accumulation; matrices of at most 64 by 256 in fp32.  out may be M; an output that is another matrix's output or M is
+ * accumulation, 64 numbers at a time, whose sums are added up one after the
+ * other (1e-5 off for 2^20 of them); matrices of at most 64 by 256 in fp32.  out may be M; an output that is another matrix's output or M is
  * DP_ERR_INVALID_ARG, and none may overlap another's otherwise.  coefs whose polynomials exceed 1e6 on the singular values that can occur are DP_ERR_INVALID_ARG.
  * ws: dp_orthogonalize_ws_bytes (M, out and scale are not looked at), on a 16-byte boundary.  p, d <= 2^20. */
 typedef struct {

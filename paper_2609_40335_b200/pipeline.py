@@ -529,7 +529,7 @@ def orthogonal_updates(ds: DeviceStep, updates: Optional[Dict[str, torch.Tensor]
     if not names:
         return {}
     if updates is None:
-        with torch.cuda.stream(stream if stream is None or isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream)):
+        with torch.cuda.stream(stream if stream is None or isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(dp._stream(stream))):
             updates = {n: torch.empty_like(ds.outs[n]) for n in names}
     mats = [ds.outs[n] for n in names]
     dp.dp_orthogonalize(mats, [updates[n] for n in names], scales=[scale * max(1.0, m.shape[0] / m.shape[1]) ** 0.5 for m in mats],
